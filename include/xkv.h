@@ -375,6 +375,65 @@ XKV_API xkv_status xkv_sr_decode_absorbed_q4(const xkv_shape *shape, int32_t lay
                                              int32_t *idx_out, float *score_out, void *workspace,
                                              size_t workspace_bytes, void *hip_stream);
 
+/*
+ * An uncompressed cache that grows and shrinks, next to xkv_dense_decode on a full one: the tokens that a serving loop keeps
+ * uncompressed (Sec. 4 "Implementation details", Sec. 7), or the whole context of a model that is not factorized.  K, V
+ * [batch][H_kv][L][d_h] have room for L = shape->L rows; lengths [batch] int32 (device, nullable: all L) says how many of a
+ * sequence's rows are in use, from 0 to L (other values count as the nearer end).  Rows that are not in use may hold anything and are
+ * not read into any result.  shape->G, r_k, r_v are ignored (any positive numbers).  Results do not depend on the order in which
+ * workgroups run.  Softmax statistics and sums are fp32; out is rounded once.
+ *
+ * xkv_tree_decode: N drafted tokens of every sequence, whose keys and values are not in the cache yet, attend to the cache and to one
+ *   another (the verification of a speculated tree).  q, out [batch][N][H_q][d_h], K_draft, V_draft [batch][H_kv][N][d_h]; tree
+ *   [batch][N][ceil(N / 32)] int32: bit j % 32 of word j / 32 of token i's row says that i sees drafted token j (its ancestors and
+ *   itself; nothing is implied; bits from N on are ignored), NULL: token i sees the drafted tokens 0 .. i.
+ *     out_ih = softmax(scale [K_rho(h)[:n] ; K_draft_rho(h)[seen by i]] q_ih)^T [V_rho(h)[:n] ; V_draft_rho(h)[seen by i]].
+ *   A token that sees nothing at all gets zeros.  Drafted tokens that no token sees may hold anything (padding).  1 <= N <= 1024.
+ *
+ * xkv_block_decode: sparse attention over blocks of c rows that a cheap score selects for each query and KV head.  Query i of
+ *   sequence b, q [batch][N][H_q][d_h], sees the first visible[b][i] rows (device int32 [batch][N], nullable: all L, clamped like
+ *   lengths): one token after a cache, or the tokens of a prompt, each with the rows up to its own.  landmarks
+ *   [batch][H_kv][n_c][d_h], n_c = ceil(L / c), are the blocks' mean keys from xkv_landmarks or xkv_landmarks_update.  With own
+ *   block e = (visible - 1) / c (rounded down), the blocks of KV head g are e and those k_ch - 1 of 0 .. e - 1 with the largest
+ *     S_j = max over rho(h) = g of <q_h, landmark_gj>  (sums in double precision, rounded once to fp32; ties: smaller block),
+ *   k_ch = min(ceil(k / c), n_c) with the token budget k = shape->k, all of them where there are fewer.  out [batch][N][H_q][d_h] is
+ *   softmax attention over the visible rows of those blocks, zeros where nothing is visible.  The landmarks of e and of blocks
+ *   behind it are not used.  blocks_out (nullable) [batch][N][H_kv][k_ch] int32: the blocks, ascending; where fewer than k_ch
+ *   exist they are followed by the next block numbers, which the query does not see.  N >= 1.
+ * xkv_landmarks_update: after N rows were appended to (or changed at the end of) every sequence, the means of the blocks that hold
+ *   the last N rows in use, in landmarks [batch][H_kv][n_c][d_h]: over the rows in use, fp32 sums, rounded once.  lengths are those
+ *   after the append.  Needs no workspace.
+ *
+ * xkv_dense_decode_weights: xkv_dense_decode over the rows in use that also adds up how much attention every row gets:
+ *   weights [batch][H_kv][L] fp32 += the sum over the query heads of a KV head of their softmax weights.  Weights of rows that are
+ *   not in use are left as they are; a sequence with no rows gets zeros in out.
+ * xkv_evict: keeps m = min(rows in use, k) rows of every KV head, k = shape->k: its first `sink` rows, its last `recent` rows and
+ *   then those with the largest weights (the order of xkv_topk; ties: smaller row); sink + recent <= k.  Kept rows stay in
+ *   order: K_out, V_out [batch][H_kv][L_out][d_h] and weights_out [batch][H_kv][L_out] receive them from row 0 on, L_out >= k; rows
+ *   from m on are left as they are.  rows_out (nullable) [batch][H_kv][k] int32: where each row came from, -1 from m on; lengths_out
+ *   (nullable) [batch]: m, may be `lengths` itself.  In place: K_out = K, V_out = V, weights_out = weights and L_out = L, all
+ *   together; otherwise outputs must not overlap inputs.  (Landmarks of an evicted cache are to be made again.)
+ * workspace: xkv_cache_workspace_bytes(shape, N, c) bytes, 256-byte aligned, for any of these calls with this shape, N query tokens
+ *   and blocks of c rows (c = 0: no xkv_block_decode).
+ * XKV_ERR_INVALID_ARG for N < 1, c < 1 (xkv_block_decode, xkv_landmarks_update), sink or recent < 0, sink + recent > k, L_out < k, or only
+ * part of an eviction in place; XKV_ERR_UNSUPPORTED where batch * N * H_kv > 65535, or for more drafted tokens than above.
+ */
+XKV_API xkv_status xkv_cache_workspace_bytes(const xkv_shape *shape, int32_t N, int32_t c, size_t *bytes);
+XKV_API xkv_status xkv_tree_decode(const xkv_shape *shape, const void *K, const void *V, const int32_t *lengths, const void *q,
+                                   const void *K_draft, const void *V_draft, const int32_t *tree, int32_t N, void *out,
+                                   void *workspace, size_t workspace_bytes, void *hip_stream);
+XKV_API xkv_status xkv_block_decode(const xkv_shape *shape, const void *K, const void *V, const int32_t *visible, const void *q,
+                                    int32_t N, const void *landmarks, int32_t c, void *out, int32_t *blocks_out, void *workspace,
+                                    size_t workspace_bytes, void *hip_stream);
+XKV_API xkv_status xkv_landmarks_update(const xkv_shape *shape, const void *K, const int32_t *lengths, int32_t N, int32_t c,
+                                        void *landmarks, void *hip_stream);
+XKV_API xkv_status xkv_dense_decode_weights(const xkv_shape *shape, const void *K, const void *V, const int32_t *lengths,
+                                            const void *q, void *out, float *weights, void *workspace, size_t workspace_bytes,
+                                            void *hip_stream);
+XKV_API xkv_status xkv_evict(const xkv_shape *shape, const void *K, const void *V, const float *weights, const int32_t *lengths,
+                             int32_t sink, int32_t recent, int32_t L_out, void *K_out, void *V_out, float *weights_out,
+                             int32_t *rows_out, int32_t *lengths_out, void *workspace, size_t workspace_bytes, void *hip_stream);
+
 /* Measurement aid for callers that want the duration of one kernel rather than of a whole call.
  * Not part of the method.  For stage = 0 (low-rank score kernel), 1 (gather-reconstruct + sparse
  * attention kernel), 2 (dense decode kernel), 3 (the Gram-matrix product X_cat^T X_cat of xkv_factorize, all

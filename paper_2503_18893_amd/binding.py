@@ -26,6 +26,8 @@ ENTRY_POINTS = ("xkv_workspace_bytes", "xkv_sr_decode", "xkv_sr_decode_static", 
                 "xkv_quantized_row_bytes", "xkv_quantize_rows", "xkv_attend_absorbed_q4", "xkv_head_scores_q4",
                 "xkv_sr_decode_absorbed_q4", "xkv_gather_attend_q", "xkv_sr_decode_landmark_q", "xkv_sr_decode_q4",
                 "xkv_sr_decode_landmark_packed", "xkv_sr_decode_tail_packed",
+                "xkv_cache_workspace_bytes", "xkv_tree_decode", "xkv_block_decode", "xkv_landmarks_update",
+                "xkv_dense_decode_weights", "xkv_evict",
                 "xkv_profile_kernel", "xkv_status_string", "xkv_version")
 
 
@@ -116,6 +118,12 @@ def load() -> ctypes.CDLL:
                                                  i32, vp, vp, vp, vp, vp, sz, vp]
         lib.xkv_sr_decode_q4.argtypes = [sp, i32, vp, vp, vp, vp, vp, ctypes.c_float, vp, vp, i32, vp, vp, vp, vp, sz, vp]
         lib.xkv_sr_decode_landmark_packed.argtypes = lib.xkv_sr_decode_landmark_q.argtypes
+        lib.xkv_cache_workspace_bytes.argtypes = [sp, i32, i32, ctypes.POINTER(sz)]
+        lib.xkv_tree_decode.argtypes = [sp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, sz, vp]
+        lib.xkv_block_decode.argtypes = [sp, vp, vp, vp, vp, i32, vp, i32, vp, vp, vp, sz, vp]
+        lib.xkv_landmarks_update.argtypes = [sp, vp, vp, i32, i32, vp, vp]
+        lib.xkv_dense_decode_weights.argtypes = [sp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        lib.xkv_evict.argtypes = [sp, vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp]
         lib.xkv_profile_kernel.argtypes = [i32, vp, vp]
         lib.xkv_status_string.argtypes = [ctypes.c_int]
         lib.xkv_status_string.restype = ctypes.c_char_p
@@ -391,6 +399,42 @@ def xkv_sr_decode_q4(shape, layer_in_group, Aq_k, Aq_v, B_k, B_v, q, out, idx_ou
                                    _ptr(q), float(rope_theta), _ptr(K_tail), _ptr(V_tail), int(T), _ptr(out),
                                    _ptr(idx_out), _ptr(score_out), _ptr(workspace),
                                    workspace.numel() * workspace.element_size(), _stream(stream)), "xkv_sr_decode_q4")
+
+
+def xkv_cache_workspace_bytes(shape: Shape, N: int = 1, c: int = 0) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().xkv_cache_workspace_bytes(ctypes.byref(shape.c()), int(N), int(c), ctypes.byref(n)), "xkv_cache_workspace_bytes")
+    return int(n.value)
+
+
+def xkv_tree_decode(shape, K, V, lengths, q, K_draft, V_draft, tree, N, out, workspace, stream=None):
+    _check(load().xkv_tree_decode(ctypes.byref(shape.c()), _ptr(K), _ptr(V), _ptr(lengths), _ptr(q), _ptr(K_draft), _ptr(V_draft),
+                                  _ptr(tree), int(N), _ptr(out), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                  _stream(stream)), "xkv_tree_decode")
+
+
+def xkv_block_decode(shape, K, V, visible, q, N, landmarks, c, out, blocks_out, workspace, stream=None):
+    _check(load().xkv_block_decode(ctypes.byref(shape.c()), _ptr(K), _ptr(V), _ptr(visible), _ptr(q), int(N), _ptr(landmarks), int(c),
+                                   _ptr(out), _ptr(blocks_out), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                   _stream(stream)), "xkv_block_decode")
+
+
+def xkv_landmarks_update(shape, K, lengths, N, c, landmarks, stream=None):
+    _check(load().xkv_landmarks_update(ctypes.byref(shape.c()), _ptr(K), _ptr(lengths), int(N), int(c), _ptr(landmarks),
+                                       _stream(stream)), "xkv_landmarks_update")
+
+
+def xkv_dense_decode_weights(shape, K, V, lengths, q, out, weights, workspace, stream=None):
+    _check(load().xkv_dense_decode_weights(ctypes.byref(shape.c()), _ptr(K), _ptr(V), _ptr(lengths), _ptr(q), _ptr(out),
+                                           _ptr(weights), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                           _stream(stream)), "xkv_dense_decode_weights")
+
+
+def xkv_evict(shape, K, V, weights, lengths, sink, recent, L_out, K_out, V_out, weights_out, rows_out, lengths_out, workspace,
+              stream=None):
+    _check(load().xkv_evict(ctypes.byref(shape.c()), _ptr(K), _ptr(V), _ptr(weights), _ptr(lengths), int(sink), int(recent),
+                            int(L_out), _ptr(K_out), _ptr(V_out), _ptr(weights_out), _ptr(rows_out), _ptr(lengths_out),
+                            _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)), "xkv_evict")
 
 
 STAGE_SCORE, STAGE_GATHER_ATTEND, STAGE_DENSE, STAGE_FACTORIZE_GRAM, STAGE_ABSORB_ROWS = 0, 1, 2, 3, 4

@@ -116,6 +116,7 @@ constexpr int kTopkLevels = 4;   // 8-bit digits of the 32-bit order key
 constexpr int kTopkBins = 256;
 constexpr int kStateWords = 8;   // per row: (prefix, k_rem) for each resolved level
 
+xkv_status validate(const xkv_shape *s);  // the checks of a shape that every entry point makes
 xkv_status make_plan(const xkv_shape &s, Plan &p);
 
 // Optional event pair recorded around the main kernel of a stage (0 score, 1 gather-attend, 2 dense,
