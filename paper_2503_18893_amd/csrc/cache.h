@@ -21,6 +21,7 @@ struct CacheArgs {
     float *part_o, *part_ml, *logits; // partials [batch][N][H_q][splits][d_h], [..][2]; weights: logits [batch][H_q][L]
     void *out;
     int L, H_kv, H_q, d_h, batch, N, words, c, k_ch, splits, chunk;
+    int rows;  // rows (query token, head) per workgroup of the matrix-core kernel, 0: the general one
     float scale;
 };
 
@@ -44,7 +45,7 @@ __device__ __forceinline__ int cache_tokens(const CacheArgs &a, CacheMode mode, 
 struct CachePlan {
     int n_rep, words, n_c, k_ch;
     float scale;
-    int chunk, splits;  // tokens per workgroup, partials per query head
+    int chunk, splits, rows;  // tokens per workgroup, partials per query head, and as in CacheArgs
     xkv_shape sel_shape;  // the selection as a problem of launch_topk: rows of blocks, or rows of the cache
     Plan sel_plan;
     size_t off_hist, off_state, off_keys, off_sel, off_n, off_logits, off_part_o, off_part_ml, total;

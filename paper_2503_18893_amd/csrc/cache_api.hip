@@ -52,11 +52,15 @@ xkv_status plan_cache_attend(const xkv_shape &s, CacheMode mode, int N, int c, C
         p.sel_shape = xkv_shape{1, s.H_kv, s.H_kv, 1, 1, 1, p.n_c, p.k_ch, (int32_t)(batch * N), XKV_F32, 1.0f};
         off = plan_selection(p, off);
     }
-    // about four workgroups per compute unit; a round of the general kernel is 64 tokens
-    const int tiles = mode == CacheMode::blocks ? 1 : ceil_div((long long)N * p.n_rep, 16);
-    const long long units = batch * s.H_kv * tiles * (mode == CacheMode::blocks ? N : 1);
-    const int splits = clampi(ceil_div(1024, units), 1, clampi(ceil_div(most, 64), 1, 128));
-    p.chunk = ceil_div(ceil_div(most, splits), 64) * 64;
+    // The matrix-core kernel: as many rows per workgroup as there are, up to 128; its workgroups come two (one, with up to 32 rows) to
+    // a compute unit.  The general one: rounds of 64 tokens, four workgroups.
+    const int M = mode == CacheMode::blocks ? p.n_rep : N * p.n_rep;
+    const bool mfma = s.dtype == XKV_BF16 && s.d_h == 128;
+    p.rows = !mfma ? 0 : mode != CacheMode::tree || M <= 32 ? 32 : M <= 64 ? 64 : 128;
+    const int per_wg = mfma ? p.rows : 16, round = !mfma || p.rows > 32 ? 64 : 128, want = !mfma ? 1024 : 512;
+    const long long units = batch * s.H_kv * ceil_div(M, per_wg) * (mode == CacheMode::blocks ? N : 1);
+    const int splits = clampi(ceil_div(want, units), 1, clampi(ceil_div(most, round), 1, 128));
+    p.chunk = ceil_div(ceil_div(most, splits), round) * round;
     p.splits = ceil_div(most, p.chunk);
     if (mode == CacheMode::weights) {
         p.off_logits = off;
@@ -107,6 +111,7 @@ CacheArgs attend_args(const xkv_shape &s, const CachePlan &p, const void *K, con
     a.k_ch = p.k_ch;
     a.splits = p.splits;
     a.chunk = p.chunk;
+    a.rows = p.rows;
     a.scale = p.scale;
     return a;
 }

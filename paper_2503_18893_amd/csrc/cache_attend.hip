@@ -2,13 +2,36 @@
 //   z_t = scale <q, k_t>,  out = sum_t exp(z_t - max) v_t / sum_t exp(z_t - max)
 // over the tokens that the query sees, split over the tokens: every workgroup leaves (maximum, sum, unnormalised output) of its
 // part, and a second kernel merges them.
-#include "cache.h"
+#include "cache_tile.h"
 
 namespace xkv {
 namespace {
 
+using namespace cache_tile;
+
 constexpr int kGenTokens = 64;  // tokens a round of the general kernel, a lane each
 constexpr int kGenRows = 16;    // its rows (query token, head) per workgroup, four per wavefront
+
+// Bits of the drafted tokens 32 k .. 32 k + 31 that `token` of a sequence sees; k < 0: rows of the cache, all of them.
+__device__ __forceinline__ uint32_t draft_word(const CacheArgs &a, int seq, int token, int k)
+{
+    uint32_t x;
+    if (a.tree) {  // (the same in every lane)
+        const int kc = k < 0 ? 0 : k < a.words ? k : a.words - 1;
+        x = a.tree[((size_t)seq * a.N + token) * a.words + kc];
+    } else {
+        const int up = token - 32 * k;
+        x = up >= 31 ? 0xFFFFFFFFu : up >= 0 ? (2u << up) - 1u : 0u;
+    }
+    return k < 0 ? 0xFFFFFFFFu : k < a.words ? x : 0u;
+}
+
+// The same for the 32 places from drafted token j on (j < 0: they begin in the cache).
+__device__ __forceinline__ uint32_t draft_bits(const CacheArgs &a, int seq, int token, int j)
+{
+    const uint32_t lo = draft_word(a, seq, token, j >> 5), hi = draft_word(a, seq, token, (j >> 5) + 1);
+    return (uint32_t)(((uint64_t)hi << 32 | lo) >> (j & 31));
+}
 
 // ------------------------------------------------------------------------------------------
 // General path, any type, width and alignment.  A round takes 64 tokens: their keys go to LDS in single precision and a lane
@@ -81,9 +104,7 @@ __global__ __launch_bounds__(256) void cache_attend_general_kernel(CacheArgs a)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             bool sees = real;
-            if (MODE == CacheMode::tree && t >= n)
-                sees = real && (a.tree ? a.tree[((size_t)seq * a.N + token[r]) * a.words + ((t - n) >> 5)] >> ((t - n) & 31) & 1u
-                                       : (uint32_t)(t - n <= token[r]));
+            if (MODE == CacheMode::tree && t0 + kGenTokens > n) sees = real && (draft_bits(a, seq, token[r], t - n) & 1u);
             const float z = a.scale * p[r];
             if (MODE == CacheMode::weights && real && m0 + r < M) a.logits[row_id[r] * a.L + t] = z;
             const float m_new = fmaxf(mx[r], wave_max(sees ? z : -INFINITY));
@@ -132,6 +153,242 @@ __global__ __launch_bounds__(256) void cache_attend_general_kernel(CacheArgs a)
         if (lane == 0) {
             a.part_ml[2 * slot] = mx[r];
             a.part_ml[2 * slot + 1] = den[r];
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------
+// Matrix-core path: bf16, 128 channels.  A workgroup has WR x WT wavefronts: WR groups of 32 rows (query token, head), WT groups of
+// tokens.  Tiles of 32 SUB WT tokens of K and V go from memory straight to LDS, two of them in turn, and all row groups read them:
+//   S^T [tokens x rows] = K tile x Q^T (registers),  P^T = exp2(c S^T - c m),  O^T [channels x rows] += V^T x P^T
+// A lane holds one row of S^T, P^T and O^T: the softmax statistics are its own (with the lane 32 further), rescaling needs no exchange, and
+// P^T is the second product's operand as it comes.  V^T is read from its tile by the transposing LDS read.
+// The maximum m is only raised when a row's logits outgrow it by a factor of 2^8: until then weights reach 2^8, sums stay exact to
+// single precision, and the accumulators need not be rescaled.
+// LDS: row t of a tile is 256 B; its 16-byte piece p of K sits at (p + t) % 16, its 32-byte piece u of V at (u + t) % 8, so that
+// neither the fragment reads (32 rows, one piece each) nor the transposing reads (8 rows, 64 B each) meet in a bank.
+// ------------------------------------------------------------------------------------------
+__device__ const u32x4_t kZeroRow[16] = {};  // stands for drafted tokens that nothing sees, and for places behind the last token
+
+template <CacheMode MODE, int WR, int WT, int SUB>
+__global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(CacheArgs a)
+{
+    constexpr int WAVES = WR * WT, TILE = 32 * SUB * WT, STAGE = 512 * TILE, RPW = TILE / WAVES, LOADS = RPW / 4;
+    static_assert(RPW % 16 == 0 && 2 * STAGE >= WAVES * 16384, "rotations by i; room for the merge");
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE];
+    __shared__ float sm_m[WT][32 * WR], sm_l[WT][32 * WR];
+    __shared__ uint32_t sm_seen[32];
+    const int split = blockIdx.x % a.splits, tile = blockIdx.x / a.splits, g = blockIdx.y;
+    const int lane = lane_id(), w = wave_id(), rg = w % WR, tg = w / WR, n32 = lane & 31, hf = lane >> 5, n_rep = a.H_q / a.H_kv;
+    const int seq = MODE == CacheMode::blocks ? blockIdx.z / a.N : blockIdx.z;
+    const int first_token = MODE == CacheMode::blocks ? blockIdx.z % a.N : 0;
+    const int M = MODE == CacheMode::blocks ? n_rep : a.N * n_rep;
+    const int n = cache_rows(a, blockIdx.z), n_tok = cache_tokens(a, MODE, n);
+    const int t_begin = split * a.chunk, t_end = t_begin + a.chunk < n_tok ? t_begin + a.chunk : n_tok;
+    if (t_begin >= t_end) return;  // (the merge knows)
+    const float c = a.scale * 1.44269504088896340736f;
+
+    const bf16_t *Kg = (const bf16_t *)a.K + ((size_t)seq * a.H_kv + g) * a.L * 128, *Vg = (const bf16_t *)a.V + ((size_t)seq * a.H_kv + g) * a.L * 128;
+    const bf16_t *Kd = (const bf16_t *)a.K_draft + ((size_t)seq * a.H_kv + g) * a.N * 128;
+    const bf16_t *Vd = (const bf16_t *)a.V_draft + ((size_t)seq * a.H_kv + g) * a.N * 128;
+    const int32_t *sel = MODE == CacheMode::blocks ? a.sel + ((size_t)blockIdx.z * a.H_kv + g) * a.k_ch : nullptr;
+
+    // Q^T fragments: lane (row n32, hf), fragment f, position e: channel 16 f + 8 hf + e
+    const int m_row = (tile * WR + rg) * 32 + n32, m_in = m_row < M ? m_row : M - 1;
+    const int token = first_token + m_in / n_rep;
+    const size_t q_row = ((size_t)seq * a.N + token) * a.H_q + g * n_rep + m_in % n_rep;
+    bf16x8_t Qf[8];
+#pragma unroll
+    for (int f = 0; f < 8; ++f) Qf[f] = __builtin_bit_cast(bf16x8_t, reinterpret_cast<const u32x4_t *>((const bf16_t *)a.q + q_row * 128)[2 * f + hf]);
+
+    if (MODE == CacheMode::tree && t_end > n) {  // which drafted tokens any token sees
+        if (threadIdx.x < 32) sm_seen[threadIdx.x] = a.tree ? 0u : 0xFFFFFFFFu;
+        __syncthreads();
+        if (a.tree)
+            for (int i = threadIdx.x; i < a.N * a.words; i += 64 * WAVES) {
+                const uint32_t x = a.tree[(size_t)seq * a.N * a.words + i];
+                if (x) atomicOr(&sm_seen[i % a.words], x);
+            }
+        __syncthreads();
+    }
+
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem;
+    const int r4 = lane >> 4, x16 = lane & 15;
+    uint32_t koff[4], voff[2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) koff[i] = 256 * r4 + 16 * ((x16 - 4 * i - r4) & 15);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) voff[i] = 256 * r4 + 32 * (((x16 >> 1) - 4 * i - r4) & 7) + 16 * (x16 & 1);
+    auto stage = [&](int t0, int buf) __attribute__((always_inline)) {
+        const uint32_t at = lds0 + buf * STAGE + 256 * RPW * w;
+        const int first = t0 + RPW * w;
+        const int plain_end = MODE == CacheMode::tree ? (n < t_end ? n : t_end) : t_end;
+        if (MODE != CacheMode::blocks && first + RPW <= plain_end) {  // (wave-uniform) rows of the cache, one after the other
+            const unsigned char *kb = (const unsigned char *)(Kg + (size_t)first * 128), *vb = (const unsigned char *)(Vg + (size_t)first * 128);
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) copy16_to_lds(kb + 1024 * i, koff[i & 3], at + 1024 * i);
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) copy16_to_lds(vb + 1024 * i, voff[i & 1], at + 256 * TILE + 1024 * i);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            int t = first + 4 * i + r4;
+            const unsigned char *k, *v;
+            if (MODE == CacheMode::tree) {
+                const int j = t - n;
+                const bool draft = t < t_end && j >= 0 && (sm_seen[(j >> 5) & 31] >> (j & 31) & 1u);
+                k = (const unsigned char *)(t < n ? Kg + (size_t)t * 128 : draft ? Kd + (size_t)j * 128 : (const bf16_t *)kZeroRow);
+                v = (const unsigned char *)(t < n ? Vg + (size_t)t * 128 : draft ? Vd + (size_t)j * 128 : (const bf16_t *)kZeroRow);
+            } else {
+                t = t < t_end ? t : t_end - 1;  // (its weight will be zero)
+                if (MODE == CacheMode::blocks) t = sel[t / a.c] * a.c + t % a.c;
+                k = (const unsigned char *)(Kg + (size_t)t * 128);
+                v = (const unsigned char *)(Vg + (size_t)t * 128);
+            }
+            copy16_global_to_lds(k + (koff[i & 3] - 256 * r4), at + 1024 * i);
+            copy16_global_to_lds(v + (voff[i & 1] - 256 * r4), at + 256 * TILE + 1024 * i);
+        }
+    };
+
+    // this lane's places in a tile: fragment f of K, block of 32 channels db of V
+    uint32_t kat[8], vat[4];
+#pragma unroll
+    for (int f = 0; f < 8; ++f) kat[f] = 256 * (32 * SUB * tg + n32) + 16 * ((2 * f + hf + n32) & 15);
+    {
+        const int rl = 4 * hf + ((lane & 15) >> 2);
+#pragma unroll
+        for (int db = 0; db < 4; ++db)
+            vat[db] = 256 * TILE + 256 * (32 * SUB * tg + rl) + 32 * ((2 * db + ((lane >> 4) & 1) + rl) & 7) + 8 * (lane & 3);
+    }
+
+    f32x16_t O[4];
+#pragma unroll
+    for (int db = 0; db < 4; ++db) O[db] = f32x16_t(0.0f);
+    float m_run = -INFINITY, l_run = 0.0f;
+    stage(t_begin, 0);
+    int buf = 0;
+    for (int t0 = t_begin; t0 < t_end; t0 += TILE, buf ^= 1) {
+        XKV_WAIT_VMCNT(0);
+        __syncthreads();  // this tile is there, and nobody reads the other one any more
+        if (t0 + TILE < t_end) stage(t0 + TILE, buf ^ 1);
+        const unsigned char *lds = smem + buf * STAGE;
+        f32x16_t S[SUB];
+#pragma unroll
+        for (int s = 0; s < SUB; ++s) {
+            S[s] = f32x16_t(0.0f);
+#pragma unroll
+            for (int f = 0; f < 8; ++f) {
+                const u32x4_t kf = *reinterpret_cast<const u32x4_t *>(lds + kat[f] + 8192 * s);
+                S[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf), Qf[f], S[s], 0, 0, 0);
+            }
+        }
+        // register v of part s is token t0 + 32 (SUB tg + s) + 8 (v / 4) + 4 hf + v % 4
+        const int tw = t0 + 32 * SUB * tg, plain_end = MODE == CacheMode::tree ? (n < t_end ? n : t_end) : t_end;
+        if (tw + 32 * SUB > plain_end) {
+#pragma unroll
+            for (int s = 0; s < SUB; ++s) {
+                const int t = tw + 32 * s, left = t_end - t;
+                uint32_t sees = left >= 32 ? 0xFFFFFFFFu : left > 0 ? (1u << left) - 1u : 0u;
+                if (MODE == CacheMode::tree) sees &= draft_bits(a, seq, token, t - n);
+                sees >>= 4 * hf;
+#pragma unroll
+                for (int v = 0; v < 16; ++v) S[s][v] = sees >> (8 * (v / 4) + v % 4) & 1u ? S[s][v] : -INFINITY;
+            }
+        }
+        if (MODE == CacheMode::weights && m_row < M) {
+            float *to = a.logits + q_row * a.L + tw + 4 * hf;
+#pragma unroll
+            for (int s = 0; s < SUB; ++s)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const int t = 32 * s + 8 * (v / 4) + v % 4;
+                    if (tw + t + 4 * hf < t_end) to[t] = a.scale * S[s][v];
+                }
+        }
+        float m_loc = S[0][0];
+#pragma unroll
+        for (int s = 0; s < SUB; ++s)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) m_loc = fmaxf(m_loc, S[s][v]);
+        float lo, hi;
+        halves(m_loc, lo, hi);
+        m_loc = fmaxf(lo, hi);
+        if (__ballot((m_loc - m_run) * c > 8.0f)) {
+            const float m_new = fmaxf(m_run, m_loc), alpha = m_run == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m_run - m_new) * c);
+            l_run *= alpha;
+#pragma unroll
+            for (int db = 0; db < 4; ++db)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) O[db][v] *= alpha;
+            m_run = m_new;
+        }
+        const float less = m_run == -INFINITY ? 0.0f : -m_run * c;
+        float l_add = 0.0f;
+#pragma unroll
+        for (int s = 0; s < SUB; ++s)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                S[s][v] = __builtin_amdgcn_exp2f(fmaf(S[s][v], c, less));
+                l_add += S[s][v];
+            }
+        l_run += l_add;
+#pragma unroll
+        for (int s = 0; s < SUB; ++s)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const bf16x8_t P = pack8(S[s], j);
+#pragma unroll
+                for (int db = 0; db < 4; ++db) {
+                    // position e of lane (channel, hf): token 16 j + 8 (e / 4) + 4 hf + e % 4, as in P
+                    const unsigned char *from = lds + vat[db] + 8192 * s + 4096 * j;
+                    const s16x4_t a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)from);
+                    const s16x4_t a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(from + 2048));
+                    O[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                        __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7)), P, O[db], 0, 0, 0);
+                }
+            }
+    }
+
+    // merge the token groups through LDS, where rows come together as well: 16-byte piece p of row n32 sits at (p + n32) % 32
+    {
+        float lo, hi;
+        halves(l_run, lo, hi);
+        if (hf == 0) {
+            sm_m[tg][32 * rg + n32] = m_run;
+            sm_l[tg][32 * rg + n32] = lo + hi;
+        }
+    }
+    __syncthreads();
+    float M_all = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < WT; ++i) M_all = fmaxf(M_all, sm_m[i][32 * rg + n32]);
+    const float f = m_run == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m_run - M_all) * c);
+    f32x4_t *ot = reinterpret_cast<f32x4_t *>(smem) + 1024 * w;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int v = 0; v < 16; v += 4) {
+            const f32x4_t x = {f * O[db][v], f * O[db][v + 1], f * O[db][v + 2], f * O[db][v + 3]};
+            ot[32 * n32 + ((8 * db + v / 2 + hf + n32) & 31)] = x;
+        }
+    __syncthreads();
+    for (int item = threadIdx.x; item < WR * 1024; item += 64 * WAVES) {
+        const int row = item >> 5, p = item & 31, m = tile * WR * 32 + row;
+        if (m >= M) continue;
+        f32x4_t x = f32x4_t(0.0f);
+#pragma unroll
+        for (int i = 0; i < WT; ++i) x += reinterpret_cast<const f32x4_t *>(smem)[1024 * (i * WR + (row >> 5)) + 32 * (row & 31) + ((p + row) & 31)];
+        const size_t slot = (((size_t)seq * a.N + first_token + m / n_rep) * a.H_q + g * n_rep + m % n_rep) * a.splits + split;
+        *reinterpret_cast<f32x4_t *>(a.part_o + slot * 128 + 4 * p) = x;
+        if (p == 0) {
+            float top = -INFINITY, den = 0.0f;
+#pragma unroll
+            for (int i = 0; i < WT; ++i) top = fmaxf(top, sm_m[i][row]);
+#pragma unroll
+            for (int i = 0; i < WT; ++i) den += sm_m[i][row] == -INFINITY ? 0.0f : sm_l[i][row] * __builtin_amdgcn_exp2f((sm_m[i][row] - top) * c);
+            a.part_ml[2 * slot] = top * a.scale;
+            a.part_ml[2 * slot + 1] = den;
         }
     }
 }
@@ -229,9 +486,25 @@ hipError_t launch_general(const CacheArgs &a, hipStream_t st)
 }
 
 template <CacheMode MODE>
+hipError_t launch_mfma(const CacheArgs &a, hipStream_t st)
+{
+    const int M = MODE == CacheMode::blocks ? a.H_q / a.H_kv : a.N * (a.H_q / a.H_kv);
+    const dim3 grid(a.splits * ((M + a.rows - 1) / a.rows), a.H_kv, MODE == CacheMode::blocks ? a.batch * a.N : a.batch);
+    if (MODE == CacheMode::tree && a.rows == 128)
+        hipLaunchKernelGGL((cache_attend_mfma_kernel<CacheMode::tree, 4, 1, 2>), grid, dim3(256), 0, st, a);
+    else if (MODE == CacheMode::tree && a.rows == 64)
+        hipLaunchKernelGGL((cache_attend_mfma_kernel<CacheMode::tree, 2, 2, 1>), grid, dim3(256), 0, st, a);
+    else
+        hipLaunchKernelGGL((cache_attend_mfma_kernel<MODE, 1, 4, 1>), grid, dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+
+template <CacheMode MODE>
 hipError_t launch_mode(const xkv_shape &s, const CacheArgs &a, hipStream_t st)
 {
-    hipError_t e = s.dtype == XKV_F32 ? launch_general<MODE, float>(a, st) : launch_general<MODE, bf16_t>(a, st);
+    const uintptr_t bits = (uintptr_t)a.K | (uintptr_t)a.V | (uintptr_t)a.q | (uintptr_t)a.K_draft | (uintptr_t)a.V_draft;
+    hipError_t e = a.rows > 0 && bits % 16 == 0 ? launch_mfma<MODE>(a, st)
+                 : s.dtype == XKV_F32 ? launch_general<MODE, float>(a, st) : launch_general<MODE, bf16_t>(a, st);
     if (e != hipSuccess) return e;
     const dim3 grid(a.H_q, a.batch * a.N);
     if (s.dtype == XKV_F32)
