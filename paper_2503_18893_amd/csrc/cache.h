@@ -18,10 +18,16 @@ struct CacheArgs {
     const int32_t *lengths;           // tree, weights: [batch], blocks: [batch][N] visible rows (nullable: L)
     const uint32_t *tree;             // tree: [batch][N][words] (nullable: token i sees the drafted tokens up to i)
     const int32_t *sel;               // blocks: [batch][N][H_kv][k_ch]
-    float *part_o, *part_ml, *logits; // partials [batch][N][H_q][splits][d_h], [..][2]; weights: logits [batch][H_q][L]
+    // Partials, [part][N][H_q] rows of d_h numbers and of (maximum, sum); the parts of all sequences stand one after the other.
+    float *part_o, *part_ml;
+    int32_t *table;                   // [batch + 1]: the first part of every sequence, and behind the last one
+    float *logits;                    // weights: [batch][H_q][L]
     void *out;
-    int L, H_kv, H_q, d_h, batch, N, words, c, k_ch, splits, chunk;
-    int rows;  // rows (query token, head) per workgroup of the matrix-core kernel, 0: the general one
+    int L, H_kv, H_q, d_h, batch, N, words, c, k_ch;
+    int rows;    // rows (query token, head) per workgroup
+    int round;   // tokens that a workgroup takes at a time: parts are multiples of it
+    int parts;   // room: parts of all sequences (tree, weights), of one query (blocks)
+    bool mfma;
     float scale;
 };
 
@@ -42,13 +48,147 @@ __device__ __forceinline__ int cache_tokens(const CacheArgs &a, CacheMode mode, 
     return listed > 0 ? (listed - 1) * a.c + n - (blocks - 1) * a.c : 0;
 }
 
+// ------------------------------------------------------------------------------------------
+// Which workgroup takes what.  How many tokens a sequence has is known on the device only, and a cache may have far more room than
+// rows in use: every workgroup reads the lengths and finds for itself the smallest part, a multiple of `round` tokens, with which the
+// parts of all sequences are at most a.parts.  So any lengths fill the chip once, evenly.  One lane per sequence, then one per
+// candidate; about 1 us.
+// ------------------------------------------------------------------------------------------
+struct CacheUnit {
+    int seq, g, tile;    // sequence (blocks: of batch N queries), KV head, row tile
+    int part, first;     // place among all parts, and of the sequence's first one
+    int t_begin, t_end;  // its tokens
+    int n, n_tok;        // rows in use, tokens of the sequence
+    bool some;           // whether there is anything to do
+};
+
+__device__ __forceinline__ int ceil_div_dev(int a, int b) { return (int)(((unsigned)a + (unsigned)b - 1u) / (unsigned)b); }
+
+// Tokens per part.  All lanes of a wavefront call it together.
+__device__ __forceinline__ int cache_chunk(const CacheArgs &a, CacheMode mode)
+{
+    const int lane = lane_id();
+    long long total = 0;
+    int most = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += kWave) {
+        int t = b0 + lane < a.batch ? cache_tokens(a, mode, cache_rows(a, b0 + lane)) : 0;
+        long long s = t;
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) {
+            s += __shfl_xor(s, off, kWave);
+            const int o = __shfl_xor(t, off, kWave);
+            t = t > o ? t : o;
+        }
+        total += s;
+        most = most > t ? most : t;
+    }
+    const int whole = ceil_div_dev(most > 0 ? most : 1, a.round) * a.round;  // (a part per sequence is always allowed)
+    if (a.parts <= a.batch || total == 0) return whole;
+    const int top = whole / a.round;  // candidates, in rounds
+    const long long enough = (total + (long long)(a.parts - a.batch) * a.round - 1) / ((long long)(a.parts - a.batch) * a.round);
+    const long long least = (total + (long long)a.parts * a.round - 1) / ((long long)a.parts * a.round);
+    const int hi = enough < top ? (int)enough : top, lo = least < hi ? (int)least : hi;
+    const int step = ceil_div_dev(hi - lo, kWave - 1), chunk = (lo + lane * step) * a.round;
+    long long used = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += kWave) {
+        const int t = b0 + lane < a.batch ? cache_tokens(a, mode, cache_rows(a, b0 + lane)) : 0;
+        for (int i = 0; i < kWave && b0 + i < a.batch; ++i) used += ceil_div_dev(__builtin_amdgcn_readlane(t, i), chunk);
+    }
+    const uint64_t fits = __ballot(used <= a.parts);  // (the last candidate is at least hi)
+    const int best = (lo + (fits ? __builtin_ctzll(fits) : kWave - 1) * step) * a.round;
+    return best > 0 && best < whole ? best : whole;
+}
+
+__device__ __forceinline__ CacheUnit cache_unit(const CacheArgs &a, CacheMode mode, int tiles)
+{
+    CacheUnit u{};
+    const int lane = lane_id();
+    // workgroups go to the eight XCDs in turn: the row tiles of a part, which share its rows of K and V, to one XCD, one after the other
+    const int x = (int)blockIdx.x;
+    int id = x / tiles;
+    u.tile = x % tiles;
+    if ((int)gridDim.x % (8 * tiles) == 0) {
+        u.tile = x / 8 % tiles;
+        id = x / (8 * tiles) * 8 + x % 8;
+    }
+    if (mode == CacheMode::blocks) {
+        const int p = id % a.parts;
+        id /= a.parts;
+        u.g = id % a.H_kv;
+        u.seq = id / a.H_kv;
+        u.n = cache_rows(a, u.seq);
+        u.n_tok = cache_tokens(a, mode, u.n);
+        const int chunk = ceil_div_dev(ceil_div_dev(u.n_tok > 0 ? u.n_tok : 1, a.parts), a.round) * a.round;
+        u.first = u.seq * a.parts;
+        u.part = u.first + p;
+        u.t_begin = p * chunk;
+        u.t_end = u.t_begin + chunk < u.n_tok ? u.t_begin + chunk : u.n_tok;
+        u.some = u.t_begin < u.t_end;
+        return u;
+    }
+    u.g = id % a.H_kv;
+    u.part = id / a.H_kv;
+    const int chunk = __builtin_amdgcn_readfirstlane(cache_chunk(a, mode));
+    int before = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += kWave) {
+        const int n = b0 + lane < a.batch ? cache_rows(a, b0 + lane) : 0, t = b0 + lane < a.batch ? cache_tokens(a, mode, n) : 0;
+        const int mine = ceil_div_dev(t, chunk);
+        int upto = mine;
+#pragma unroll
+        for (int off = 1; off < kWave; off <<= 1) {
+            const int o = __shfl_up(upto, off, kWave);
+            upto += lane >= off ? o : 0;
+        }
+        if (x == 0 && threadIdx.x < kWave) {  // for the merge
+            if (b0 + lane < a.batch) a.table[b0 + lane] = before + upto - mine;
+            if (b0 + lane == a.batch - 1) a.table[a.batch] = before + upto;
+        }
+        const uint64_t in = __ballot(u.part >= before + upto - mine && u.part < before + upto);
+        if (in) {
+            const int l = __builtin_ctzll(in);
+            u.seq = b0 + l;
+            u.n = __builtin_amdgcn_readlane(n, l);
+            u.n_tok = __builtin_amdgcn_readlane(t, l);
+            u.first = before + __builtin_amdgcn_readlane(upto - mine, l);
+            u.t_begin = (u.part - u.first) * chunk;
+            u.t_end = u.t_begin + chunk < u.n_tok ? u.t_begin + chunk : u.n_tok;
+            u.some = true;
+        }
+        before += __builtin_amdgcn_readlane(upto, kWave - 1);
+    }
+    return u;
+}
+
+// The parts of a sequence (blocks: of a query), for what follows the attention.
+__device__ __forceinline__ void cache_parts(const CacheArgs &a, CacheMode mode, int i, int &first, int &count)
+{
+    if (mode == CacheMode::blocks) {
+        const int n_tok = cache_tokens(a, mode, cache_rows(a, i));
+        const int chunk = ceil_div_dev(ceil_div_dev(n_tok > 0 ? n_tok : 1, a.parts), a.round) * a.round;
+        first = i * a.parts;
+        count = ceil_div_dev(n_tok, chunk);
+    } else {
+        first = a.table[i];
+        count = a.table[i + 1] - first;
+    }
+}
+
+// Row of a partial: blocks have one query token per part.
+__device__ __forceinline__ size_t part_row(const CacheArgs &a, CacheMode mode, int part, int token, int head)
+{
+    return ((size_t)part * (mode == CacheMode::blocks ? 1 : a.N) + (mode == CacheMode::blocks ? 0 : token)) * a.H_q + head;
+}
+
+constexpr int kMaxCacheParts = 256;  // parts of a sequence that the merge takes
+
 struct CachePlan {
     int n_rep, words, n_c, k_ch;
     float scale;
-    int chunk, splits, rows;  // tokens per workgroup, partials per query head, and as in CacheArgs
+    int rows, round, parts;  // as in CacheArgs
+    bool mfma;
     xkv_shape sel_shape;  // the selection as a problem of launch_topk: rows of blocks, or rows of the cache
     Plan sel_plan;
-    size_t off_hist, off_state, off_keys, off_sel, off_n, off_logits, off_part_o, off_part_ml, total;
+    size_t off_hist, off_state, off_keys, off_sel, off_n, off_logits, off_table, off_part_o, off_part_ml, total;
 };
 
 // The plan of one call.  N: query tokens of a sequence; c: rows of a block.

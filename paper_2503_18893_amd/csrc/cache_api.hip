@@ -52,24 +52,33 @@ xkv_status plan_cache_attend(const xkv_shape &s, CacheMode mode, int N, int c, C
         p.sel_shape = xkv_shape{1, s.H_kv, s.H_kv, 1, 1, 1, p.n_c, p.k_ch, (int32_t)(batch * N), XKV_F32, 1.0f};
         off = plan_selection(p, off);
     }
-    // The matrix-core kernel: as many rows per workgroup as there are, up to 128; its workgroups come two (one, with up to 32 rows) to
-    // a compute unit.  The general one: rounds of 64 tokens, four workgroups.
+    // The matrix-core kernel: as many rows per workgroup as there are, up to 128, and two workgroups (one, with up to 32 rows) to a
+    // compute unit.  The general one: 16 rows, rounds of 64 tokens, four workgroups.
     const int M = mode == CacheMode::blocks ? p.n_rep : N * p.n_rep;
-    const bool mfma = s.dtype == XKV_BF16 && s.d_h == 128;
-    p.rows = !mfma ? 0 : mode != CacheMode::tree || M <= 32 ? 32 : M <= 64 ? 64 : 128;
-    const int per_wg = mfma ? p.rows : 16, round = !mfma || p.rows > 32 ? 64 : 128, want = !mfma ? 1024 : 512;
-    const long long units = batch * s.H_kv * ceil_div(M, per_wg) * (mode == CacheMode::blocks ? N : 1);
-    const int splits = clampi(ceil_div(want, units), 1, clampi(ceil_div(most, round), 1, 128));
-    p.chunk = ceil_div(ceil_div(most, splits), round) * round;
-    p.splits = ceil_div(most, p.chunk);
+    p.mfma = s.dtype == XKV_BF16 && s.d_h == 128;
+    p.rows = !p.mfma ? 16 : mode != CacheMode::tree || M <= 32 ? 32 : M <= 64 ? 64 : 128;
+    p.round = p.mfma && p.rows == 32 ? 128 : 64;
+    const int want = !p.mfma ? 1024 : p.rows == 32 ? 256 : 512;
+    const long long tiles = (long long)s.H_kv * ceil_div(M, p.rows);
+    const int longest = ceil_div(most, p.round);  // parts that the longest sequence can have
+    if (mode == CacheMode::blocks) {
+        p.parts = clampi(ceil_div(want, tiles * batch * N), 1, clampi(longest, 1, kMaxCacheParts));
+    } else {
+        const long long all = batch * longest;
+        p.parts = clampi(ceil_div(want, tiles), (int)batch, (int)(all < (1 << 30) ? all : 1 << 30));
+        if (p.parts > batch + kMaxCacheParts - 1) p.parts = (int)batch + kMaxCacheParts - 1;
+    }
+    const long long part_rows = mode == CacheMode::blocks ? batch * N * p.parts * s.H_q : (long long)p.parts * N * s.H_q;
+    p.off_table = off;
+    off = align_up(off + ((size_t)batch + 1) * sizeof(int32_t), 256);
     if (mode == CacheMode::weights) {
         p.off_logits = off;
         off = align_up(off + (size_t)batch * s.H_q * s.L * sizeof(float), 256);
     }
     p.off_part_o = off;
-    off = align_up(off + (size_t)batch * N * s.H_q * p.splits * s.d_h * sizeof(float), 256);
+    off = align_up(off + (size_t)part_rows * s.d_h * sizeof(float), 256);
     p.off_part_ml = off;
-    p.total = align_up(off + (size_t)batch * N * s.H_q * p.splits * 2 * sizeof(float), 256);
+    p.total = align_up(off + (size_t)part_rows * 2 * sizeof(float), 256);
     return XKV_OK;
 }
 
@@ -109,9 +118,11 @@ CacheArgs attend_args(const xkv_shape &s, const CachePlan &p, const void *K, con
     a.N = N;
     a.words = p.words;
     a.k_ch = p.k_ch;
-    a.splits = p.splits;
-    a.chunk = p.chunk;
+    a.table = at<int32_t>(ws, p.off_table);
     a.rows = p.rows;
+    a.round = p.round;
+    a.parts = p.parts;
+    a.mfma = p.mfma;
     a.scale = p.scale;
     return a;
 }

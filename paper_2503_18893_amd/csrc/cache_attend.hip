@@ -2,6 +2,8 @@
 //   z_t = scale <q, k_t>,  out = sum_t exp(z_t - max) v_t / sum_t exp(z_t - max)
 // over the tokens that the query sees, split over the tokens: every workgroup leaves (maximum, sum, unnormalised output) of its
 // part, and a second kernel merges them.
+#include <type_traits>
+
 #include "cache_tile.h"
 
 namespace xkv {
@@ -42,20 +44,18 @@ template <typename T, CacheMode MODE, int JP>
 __global__ __launch_bounds__(256) void cache_attend_general_kernel(CacheArgs a)
 {
     extern __shared__ float smem_f[];
-    const int split = blockIdx.x % a.splits, tile = blockIdx.x / a.splits, g = blockIdx.y;
     const int lane = lane_id(), w = wave_id(), n_rep = a.H_q / a.H_kv, d = a.d_h, pitch = d | 1;
-    // blocks: one query token per z; else all query tokens of a sequence
-    const int seq = MODE == CacheMode::blocks ? blockIdx.z / a.N : blockIdx.z;
-    const int first_token = MODE == CacheMode::blocks ? blockIdx.z % a.N : 0;
     const int M = MODE == CacheMode::blocks ? n_rep : a.N * n_rep;
-    const int n = cache_rows(a, blockIdx.z), n_tok = cache_tokens(a, MODE, n);
-    const int t_begin = split * a.chunk, t_end = t_begin + a.chunk < n_tok ? t_begin + a.chunk : n_tok;
-    if (t_begin >= t_end) return;  // (the merge knows)
+    const CacheUnit u = cache_unit(a, MODE, (M + kGenRows - 1) / kGenRows);
+    if (!u.some) return;  // (the merge knows)
+    const int tile = u.tile, g = u.g, n = u.n, t_begin = u.t_begin, t_end = u.t_end;
+    // blocks: one query token; else all query tokens of a sequence
+    const int seq = MODE == CacheMode::blocks ? u.seq / a.N : u.seq, first_token = MODE == CacheMode::blocks ? u.seq % a.N : 0;
     float *kt = smem_f, *qs = kt + kGenTokens * pitch;
 
     const T *Kg = (const T *)a.K + ((size_t)seq * a.H_kv + g) * a.L * d, *Vg = (const T *)a.V + ((size_t)seq * a.H_kv + g) * a.L * d;
     const T *Kd = (const T *)a.K_draft + ((size_t)seq * a.H_kv + g) * a.N * d, *Vd = (const T *)a.V_draft + ((size_t)seq * a.H_kv + g) * a.N * d;
-    const int32_t *sel = MODE == CacheMode::blocks ? a.sel + ((size_t)blockIdx.z * a.H_kv + g) * a.k_ch : nullptr;
+    const int32_t *sel = MODE == CacheMode::blocks ? a.sel + ((size_t)u.seq * a.H_kv + g) * a.k_ch : nullptr;
 
     // row m of this workgroup: query token first_token + m / n_rep, head g n_rep + m % n_rep
     const int m0 = tile * kGenRows + 4 * w;
@@ -144,7 +144,7 @@ __global__ __launch_bounds__(256) void cache_attend_general_kernel(CacheArgs a)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         if (m0 + r >= M) break;
-        const size_t slot = row_id[r] * a.splits + split;
+        const size_t slot = part_row(a, MODE, u.part, token[r], g * n_rep + (m0 + r) % n_rep);
 #pragma unroll
         for (int jj = 0; jj < JP; ++jj) {
             const int j = lane + jj * kWave;
@@ -159,7 +159,8 @@ __global__ __launch_bounds__(256) void cache_attend_general_kernel(CacheArgs a)
 
 // ------------------------------------------------------------------------------------------
 // Matrix-core path: bf16, 128 channels.  A workgroup has WR x WT wavefronts: WR groups of 32 rows (query token, head), WT groups of
-// tokens.  Tiles of 32 SUB WT tokens of K and V go from memory straight to LDS, two of them in turn, and all row groups read them:
+// tokens.  Tiles of 32 SUB WT tokens of K and V go from memory straight to LDS, two of them in turn; all row groups read them, or, where
+// there is one, every wavefront its own part alone, without barriers:
 //   S^T [tokens x rows] = K tile x Q^T (registers),  P^T = exp2(c S^T - c m),  O^T [channels x rows] += V^T x P^T
 // A lane holds one row of S^T, P^T and O^T: the softmax statistics are its own (with the lane 32 further), rescaling needs no exchange, and
 // P^T is the second product's operand as it comes.  V^T is read from its tile by the transposing LDS read.
@@ -173,25 +174,25 @@ __device__ const u32x4_t kZeroRow[16] = {};  // stands for drafted tokens that n
 template <CacheMode MODE, int WR, int WT, int SUB>
 __global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(CacheArgs a)
 {
-    constexpr int WAVES = WR * WT, TILE = 32 * SUB * WT, STAGE = 512 * TILE, RPW = TILE / WAVES, LOADS = RPW / 4;
+    constexpr bool OWN = WR == 1;  // tiles that only one wavefront reads
+    constexpr int WAVES = WR * WT, TILE = 32 * SUB * WT, STAGE = 512 * TILE, RPW = TILE / WAVES, LOADS = RPW / 4, VBASE = OWN ? 8192 : 256 * TILE;
+    static_assert(!OWN || SUB == 1, "a wavefront's tile is 32 tokens");
     static_assert(RPW % 16 == 0 && 2 * STAGE >= WAVES * 16384, "rotations by i; room for the merge");
     __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE];
     __shared__ float sm_m[WT][32 * WR], sm_l[WT][32 * WR];
     __shared__ uint32_t sm_seen[32];
-    const int split = blockIdx.x % a.splits, tile = blockIdx.x / a.splits, g = blockIdx.y;
     const int lane = lane_id(), w = wave_id(), rg = w % WR, tg = w / WR, n32 = lane & 31, hf = lane >> 5, n_rep = a.H_q / a.H_kv;
-    const int seq = MODE == CacheMode::blocks ? blockIdx.z / a.N : blockIdx.z;
-    const int first_token = MODE == CacheMode::blocks ? blockIdx.z % a.N : 0;
     const int M = MODE == CacheMode::blocks ? n_rep : a.N * n_rep;
-    const int n = cache_rows(a, blockIdx.z), n_tok = cache_tokens(a, MODE, n);
-    const int t_begin = split * a.chunk, t_end = t_begin + a.chunk < n_tok ? t_begin + a.chunk : n_tok;
-    if (t_begin >= t_end) return;  // (the merge knows)
+    const CacheUnit u = cache_unit(a, MODE, (M + 32 * WR - 1) / (32 * WR));
+    if (!u.some) return;  // (the merge knows)
+    const int tile = u.tile, g = u.g, n = u.n, t_begin = u.t_begin, t_end = u.t_end;
+    const int seq = MODE == CacheMode::blocks ? u.seq / a.N : u.seq, first_token = MODE == CacheMode::blocks ? u.seq % a.N : 0;
     const float c = a.scale * 1.44269504088896340736f;
 
     const bf16_t *Kg = (const bf16_t *)a.K + ((size_t)seq * a.H_kv + g) * a.L * 128, *Vg = (const bf16_t *)a.V + ((size_t)seq * a.H_kv + g) * a.L * 128;
     const bf16_t *Kd = (const bf16_t *)a.K_draft + ((size_t)seq * a.H_kv + g) * a.N * 128;
     const bf16_t *Vd = (const bf16_t *)a.V_draft + ((size_t)seq * a.H_kv + g) * a.N * 128;
-    const int32_t *sel = MODE == CacheMode::blocks ? a.sel + ((size_t)blockIdx.z * a.H_kv + g) * a.k_ch : nullptr;
+    const int32_t *sel = MODE == CacheMode::blocks ? a.sel + ((size_t)u.seq * a.H_kv + g) * a.k_ch : nullptr;
 
     // Q^T fragments: lane (row n32, hf), fragment f, position e: channel 16 f + 8 hf + e
     const int m_row = (tile * WR + rg) * 32 + n32, m_in = m_row < M ? m_row : M - 1;
@@ -212,68 +213,68 @@ __global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(Cach
         __syncthreads();
     }
 
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem;
+    // Where this wavefront puts rows: its share of a tile that all read (WR > 1), or tiles of 32 rows of its own.
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem + (OWN ? 32768 * w : 256 * RPW * w);
     const int r4 = lane >> 4, x16 = lane & 15;
     uint32_t koff[4], voff[2];
 #pragma unroll
     for (int i = 0; i < 4; ++i) koff[i] = 256 * r4 + 16 * ((x16 - 4 * i - r4) & 15);
 #pragma unroll
     for (int i = 0; i < 2; ++i) voff[i] = 256 * r4 + 32 * (((x16 >> 1) - 4 * i - r4) & 7) + 16 * (x16 & 1);
-    auto stage = [&](int t0, int buf) __attribute__((always_inline)) {
-        const uint32_t at = lds0 + buf * STAGE + 256 * RPW * w;
-        const int first = t0 + RPW * w;
-        const int plain_end = MODE == CacheMode::tree ? (n < t_end ? n : t_end) : t_end;
-        if (MODE != CacheMode::blocks && first + RPW <= plain_end) {  // (wave-uniform) rows of the cache, one after the other
-            const unsigned char *kb = (const unsigned char *)(Kg + (size_t)first * 128), *vb = (const unsigned char *)(Vg + (size_t)first * 128);
+    const int plain_end = MODE == CacheMode::tree && n < t_end ? n : t_end;  // rows of the cache end here
+    auto stage = [&](int first, int buf, auto values) __attribute__((always_inline)) {  // RPW tokens from `first` on
+        constexpr bool is_v = decltype(values)::value;
+        const uint32_t at = lds0 + buf * (OWN ? 16384 : STAGE) + (is_v ? VBASE : 0);
+        const bf16_t *rows = is_v ? Vg : Kg;
+        if (MODE != CacheMode::blocks && first + RPW <= plain_end) {  // (wave-uniform) one after the other
+            const unsigned char *base = (const unsigned char *)(rows + (size_t)first * 128);
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) copy16_to_lds(kb + 1024 * i, koff[i & 3], at + 1024 * i);
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) copy16_to_lds(vb + 1024 * i, voff[i & 1], at + 256 * TILE + 1024 * i);
+            for (int i = 0; i < LOADS; ++i) {
+                if (OWN)
+                    copy16_to_lds_once(base + 1024 * i, is_v ? voff[i & 1] : koff[i & 3], at + 1024 * i);
+                else
+                    copy16_to_lds(base + 1024 * i, is_v ? voff[i & 1] : koff[i & 3], at + 1024 * i);
+            }
             return;
         }
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             int t = first + 4 * i + r4;
-            const unsigned char *k, *v;
+            const bf16_t *from;
             if (MODE == CacheMode::tree) {
                 const int j = t - n;
                 const bool draft = t < t_end && j >= 0 && (sm_seen[(j >> 5) & 31] >> (j & 31) & 1u);
-                k = (const unsigned char *)(t < n ? Kg + (size_t)t * 128 : draft ? Kd + (size_t)j * 128 : (const bf16_t *)kZeroRow);
-                v = (const unsigned char *)(t < n ? Vg + (size_t)t * 128 : draft ? Vd + (size_t)j * 128 : (const bf16_t *)kZeroRow);
+                from = t < n ? rows + (size_t)t * 128 : draft ? (is_v ? Vd : Kd) + (size_t)j * 128 : (const bf16_t *)kZeroRow;
             } else {
                 t = t < t_end ? t : t_end - 1;  // (its weight will be zero)
                 if (MODE == CacheMode::blocks) t = sel[t / a.c] * a.c + t % a.c;
-                k = (const unsigned char *)(Kg + (size_t)t * 128);
-                v = (const unsigned char *)(Vg + (size_t)t * 128);
+                from = rows + (size_t)t * 128;
             }
-            copy16_global_to_lds(k + (koff[i & 3] - 256 * r4), at + 1024 * i);
-            copy16_global_to_lds(v + (voff[i & 1] - 256 * r4), at + 256 * TILE + 1024 * i);
+            copy16_global_to_lds((const unsigned char *)from + ((is_v ? voff[i & 1] : koff[i & 3]) - 256 * r4), at + 1024 * i);
         }
     };
+    constexpr std::false_type keys{};
+    constexpr std::true_type values{};
 
     // this lane's places in a tile: fragment f of K, block of 32 channels db of V
+    constexpr int TG = OWN ? 0 : 1;
+    const unsigned char *lds_w = smem + (OWN ? 32768 * w : 0);
     uint32_t kat[8], vat[4];
 #pragma unroll
-    for (int f = 0; f < 8; ++f) kat[f] = 256 * (32 * SUB * tg + n32) + 16 * ((2 * f + hf + n32) & 15);
+    for (int f = 0; f < 8; ++f) kat[f] = 256 * (32 * SUB * TG * tg + n32) + 16 * ((2 * f + hf + n32) & 15);
     {
         const int rl = 4 * hf + ((lane & 15) >> 2);
 #pragma unroll
         for (int db = 0; db < 4; ++db)
-            vat[db] = 256 * TILE + 256 * (32 * SUB * tg + rl) + 32 * ((2 * db + ((lane >> 4) & 1) + rl) & 7) + 8 * (lane & 3);
+            vat[db] = VBASE + 256 * (32 * SUB * TG * tg + rl) + 32 * ((2 * db + ((lane >> 4) & 1) + rl) & 7) + 8 * (lane & 3);
     }
 
     f32x16_t O[4];
 #pragma unroll
     for (int db = 0; db < 4; ++db) O[db] = f32x16_t(0.0f);
     float m_run = -INFINITY, l_run = 0.0f;
-    stage(t_begin, 0);
-    int buf = 0;
-    for (int t0 = t_begin; t0 < t_end; t0 += TILE, buf ^= 1) {
-        XKV_WAIT_VMCNT(0);
-        __syncthreads();  // this tile is there, and nobody reads the other one any more
-        if (t0 + TILE < t_end) stage(t0 + TILE, buf ^ 1);
-        const unsigned char *lds = smem + buf * STAGE;
-        f32x16_t S[SUB];
+    f32x16_t S[SUB];
+    auto logits = [&](const unsigned char *lds) __attribute__((always_inline)) {
 #pragma unroll
         for (int s = 0; s < SUB; ++s) {
             S[s] = f32x16_t(0.0f);
@@ -283,8 +284,9 @@ __global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(Cach
                 S[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf), Qf[f], S[s], 0, 0, 0);
             }
         }
-        // register v of part s is token t0 + 32 (SUB tg + s) + 8 (v / 4) + 4 hf + v % 4
-        const int tw = t0 + 32 * SUB * tg, plain_end = MODE == CacheMode::tree ? (n < t_end ? n : t_end) : t_end;
+    };
+    auto weigh = [&](int tw) __attribute__((always_inline)) {
+        // register v of part s is token tw + 32 s + 8 (v / 4) + 4 hf + v % 4
         if (tw + 32 * SUB > plain_end) {
 #pragma unroll
             for (int s = 0; s < SUB; ++s) {
@@ -333,6 +335,8 @@ __global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(Cach
                 l_add += S[s][v];
             }
         l_run += l_add;
+    };
+    auto add_values = [&](const unsigned char *lds) __attribute__((always_inline)) {
 #pragma unroll
         for (int s = 0; s < SUB; ++s)
 #pragma unroll
@@ -348,6 +352,64 @@ __global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(Cach
                         __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7)), P, O[db], 0, 0, 0);
                 }
             }
+    };
+    if constexpr (OWN) {
+        // A wavefront keeps two tiles of its own and waits for nobody: the keys of the tile after the next are requested as soon as the
+        // logits are there, its values as soon as the products are.  (Counted waits: requests are answered in order; others in between,
+        // of logits that are stored, make a wait longer, not shorter.)
+        const int t_first = t_begin + 32 * w;
+        if (t_first < t_end) {
+            stage(t_first, 0, keys);
+            stage(t_first, 0, values);
+        }
+        if (t_first + TILE < t_end) {
+            stage(t_first + TILE, 1, keys);
+            stage(t_first + TILE, 1, values);
+        }
+        int buf = 0;
+        for (int t = t_first; t < t_end; t += TILE, buf ^= 1) {
+            const unsigned char *lds = lds_w + 16384 * buf;
+            const bool next = t + TILE < t_end, then = t + 2 * TILE < t_end;
+            if (next)
+                XKV_WAIT_VMCNT(3 * LOADS);
+            else
+                XKV_WAIT_VMCNT(LOADS);
+            asm volatile("" : : : "memory");
+            logits(lds);
+            if (then) {
+                wait_lds();
+                stage(t + 2 * TILE, buf, keys);
+            }
+            weigh(t);
+            if (then)
+                XKV_WAIT_VMCNT(3 * LOADS);
+            else if (next)
+                XKV_WAIT_VMCNT(2 * LOADS);
+            else
+                XKV_WAIT_VMCNT(0);
+            asm volatile("" : : : "memory");
+            add_values(lds);
+            if (then) {
+                wait_lds();
+                stage(t + 2 * TILE, buf, values);
+            }
+        }
+    } else {
+        stage(t_begin + RPW * w, 0, keys);
+        stage(t_begin + RPW * w, 0, values);
+        int buf = 0;
+        for (int t0 = t_begin; t0 < t_end; t0 += TILE, buf ^= 1) {
+            XKV_WAIT_VMCNT(0);
+            __syncthreads();  // this tile is there, and nobody reads the other one any more
+            if (t0 + TILE < t_end) {
+                stage(t0 + TILE + RPW * w, buf ^ 1, keys);
+                stage(t0 + TILE + RPW * w, buf ^ 1, values);
+            }
+            const unsigned char *lds = lds_w + buf * STAGE;
+            logits(lds);
+            weigh(t0 + 32 * SUB * tg);
+            add_values(lds);
+        }
     }
 
     // merge the token groups through LDS, where rows come together as well: 16-byte piece p of row n32 sits at (p + n32) % 32
@@ -379,7 +441,7 @@ __global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(Cach
         f32x4_t x = f32x4_t(0.0f);
 #pragma unroll
         for (int i = 0; i < WT; ++i) x += reinterpret_cast<const f32x4_t *>(smem)[1024 * (i * WR + (row >> 5)) + 32 * (row & 31) + ((p + row) & 31)];
-        const size_t slot = (((size_t)seq * a.N + first_token + m / n_rep) * a.H_q + g * n_rep + m % n_rep) * a.splits + split;
+        const size_t slot = part_row(a, MODE, u.part, m / n_rep, g * n_rep + m % n_rep);
         *reinterpret_cast<f32x4_t *>(a.part_o + slot * 128 + 4 * p) = x;
         if (p == 0) {
             float top = -INFINITY, den = 0.0f;
@@ -396,40 +458,39 @@ __global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(Cach
 // ------------------------------------------------------------------------------------------
 // Merge: one workgroup per (query token, head).  Partials that no token went to were not written and are not read.
 // ------------------------------------------------------------------------------------------
-constexpr int kMaxCacheParts = 256;
-
 template <typename T, CacheMode MODE>
 __global__ __launch_bounds__(256) void cache_merge_kernel(CacheArgs a)
 {
     __shared__ float sm_w[kMaxCacheParts], sm_o[4][256];
     const int lane = lane_id(), w = wave_id(), d = a.d_h;
-    const size_t row = (size_t)blockIdx.y * a.H_q + blockIdx.x;  // y: (sequence, query token)
-    const int n = cache_rows(a, MODE == CacheMode::tree ? blockIdx.y / a.N : blockIdx.y);
-    const int n_tok = cache_tokens(a, MODE, n), parts = (n_tok + a.chunk - 1) / a.chunk;
-    const float *ml = a.part_ml + row * a.splits * 2;
+    const int z = blockIdx.y, head = blockIdx.x;  // z: (sequence, query token)
+    int first, parts;
+    cache_parts(a, MODE, MODE == CacheMode::blocks ? z : z / a.N, first, parts);
+    const size_t row = part_row(a, MODE, first, z % a.N, head), stride = part_row(a, MODE, 1, 0, 0);  // of its first part, to the next one
+    const float *ml = a.part_ml + row * 2;
     float M = -INFINITY;
-    for (int s = lane; s < parts; s += kWave) M = fmaxf(M, ml[2 * s]);
+    for (int s = lane; s < parts; s += kWave) M = fmaxf(M, ml[2 * s * stride]);
     M = wave_max(M);
     float den = 0.0f;
     for (int s = lane; s < parts; s += kWave) {
-        const float wt = ml[2 * s] == -INFINITY ? 0.0f : expf(ml[2 * s] - M);
+        const float m = ml[2 * s * stride], wt = m == -INFINITY ? 0.0f : expf(m - M);
         if (w == 0) sm_w[s] = wt;
-        den = fmaf(wt, ml[2 * s + 1], den);
+        den = fmaf(wt, ml[2 * s * stride + 1], den);
     }
     den = wave_sum(den);
     __syncthreads();
-    const float *po = a.part_o + row * a.splits * d;
+    const float *po = a.part_o + row * d;
     for (int j = lane; j < d; j += kWave) {
         float acc = 0.0f;
 #pragma unroll 4
-        for (int s = w; s < parts; s += 4) acc = fmaf(sm_w[s], po[(size_t)s * d + j], acc);
+        for (int s = w; s < parts; s += 4) acc = fmaf(sm_w[s], po[s * stride * d + j], acc);
         sm_o[w][j] = acc;
     }
     __syncthreads();
     const int j = threadIdx.x;
     if (j < d) {
         const float num = (sm_o[0][j] + sm_o[1][j]) + (sm_o[2][j] + sm_o[3][j]);
-        ((T *)a.out)[row * d + j] = from_f32<T>(den > 0.0f ? num / den : 0.0f);  // (a query that sees nothing: zeros)
+        ((T *)a.out)[((size_t)z * a.H_q + head) * d + j] = from_f32<T>(den > 0.0f ? num / den : 0.0f);  // (a query that sees nothing: zeros)
     }
 }
 
@@ -441,16 +502,17 @@ __global__ __launch_bounds__(256) void cache_weights_kernel(CacheArgs a, float *
 {
     __shared__ float sm_m[16], sm_r[16];
     const int lane = lane_id(), w = wave_id(), n_rep = a.H_q / a.H_kv, g = blockIdx.y, b = blockIdx.z;
-    const int n = cache_rows(a, b), parts = (n + a.chunk - 1) / a.chunk;
-    const int t0 = blockIdx.x * 1024;
+    const int n = cache_rows(a, b), t0 = blockIdx.x * 1024;
     if (t0 >= n) return;
-    const size_t head = (size_t)b * a.H_q + g * n_rep;
+    const size_t head = (size_t)b * a.H_q + g * n_rep, stride = a.H_q;
+    int first, parts;
+    cache_parts(a, CacheMode::weights, b, first, parts);
     for (int h = w; h < n_rep; h += 4) {
-        const float *ml = a.part_ml + (head + h) * a.splits * 2;
+        const float *ml = a.part_ml + part_row(a, CacheMode::weights, first, 0, g * n_rep + h) * 2;
         float M = -INFINITY, den = 0.0f;
-        for (int s = lane; s < parts; s += kWave) M = fmaxf(M, ml[2 * s]);
+        for (int s = lane; s < parts; s += kWave) M = fmaxf(M, ml[2 * s * stride]);
         M = wave_max(M);
-        for (int s = lane; s < parts; s += kWave) den = fmaf(expf(ml[2 * s] - M), ml[2 * s + 1], den);
+        for (int s = lane; s < parts; s += kWave) den = fmaf(expf(ml[2 * s * stride] - M), ml[2 * s * stride + 1], den);
         den = wave_sum(den);
         if (lane == 0) {
             sm_m[h] = M;
@@ -468,11 +530,16 @@ __global__ __launch_bounds__(256) void cache_weights_kernel(CacheArgs a, float *
     }
 }
 
+dim3 unit_grid(const CacheArgs &a, CacheMode mode, int M)
+{
+    return dim3((unsigned)a.parts * a.H_kv * ((M + a.rows - 1) / a.rows) * (mode == CacheMode::blocks ? a.batch * a.N : 1));
+}
+
 template <CacheMode MODE, typename T>
 hipError_t launch_general(const CacheArgs &a, hipStream_t st)
 {
     const int M = MODE == CacheMode::blocks ? a.H_q / a.H_kv : a.N * (a.H_q / a.H_kv);
-    const dim3 grid(a.splits * ((M + kGenRows - 1) / kGenRows), a.H_kv, MODE == CacheMode::blocks ? a.batch * a.N : a.batch);
+    const dim3 grid = unit_grid(a, MODE, M);
     const size_t lds = ((size_t)kGenTokens * (a.d_h | 1) + (size_t)kGenRows * a.d_h) * sizeof(float);
     auto launch = [&](auto kernel, DynamicLdsOnce &attr) {
         const hipError_t e = attr.ensure((const void *)kernel, lds > 65536 ? 160 * 1024 : lds);
@@ -489,7 +556,7 @@ template <CacheMode MODE>
 hipError_t launch_mfma(const CacheArgs &a, hipStream_t st)
 {
     const int M = MODE == CacheMode::blocks ? a.H_q / a.H_kv : a.N * (a.H_q / a.H_kv);
-    const dim3 grid(a.splits * ((M + a.rows - 1) / a.rows), a.H_kv, MODE == CacheMode::blocks ? a.batch * a.N : a.batch);
+    const dim3 grid = unit_grid(a, MODE, M);
     if (MODE == CacheMode::tree && a.rows == 128)
         hipLaunchKernelGGL((cache_attend_mfma_kernel<CacheMode::tree, 4, 1, 2>), grid, dim3(256), 0, st, a);
     else if (MODE == CacheMode::tree && a.rows == 64)
@@ -503,8 +570,10 @@ template <CacheMode MODE>
 hipError_t launch_mode(const xkv_shape &s, const CacheArgs &a, hipStream_t st)
 {
     const uintptr_t bits = (uintptr_t)a.K | (uintptr_t)a.V | (uintptr_t)a.q | (uintptr_t)a.K_draft | (uintptr_t)a.V_draft;
-    hipError_t e = a.rows > 0 && bits % 16 == 0 ? launch_mfma<MODE>(a, st)
-                 : s.dtype == XKV_F32 ? launch_general<MODE, float>(a, st) : launch_general<MODE, bf16_t>(a, st);
+    CacheArgs gen = a;
+    gen.rows = kGenRows;  // (its rounds divide those of the plan)
+    hipError_t e = a.mfma && bits % 16 == 0 ? launch_mfma<MODE>(a, st)
+                 : s.dtype == XKV_F32 ? launch_general<MODE, float>(gen, st) : launch_general<MODE, bf16_t>(gen, st);
     if (e != hipSuccess) return e;
     const dim3 grid(a.H_q, a.batch * a.N);
     if (s.dtype == XKV_F32)

@@ -18,49 +18,89 @@ __global__ __launch_bounds__(256) void evict_keys_kernel(EvictArgs a)
 }
 
 // Rows to their new places.  A row's new place is never behind its old one, so that a workgroup which takes the rows in order and
-// reads a step's rows before it writes any of them may work in place; elsewhere steps are workgroups of their own.
+// reads a step's rows (and those of the next one, which lie behind everything it writes) before it writes any of them may work in
+// place; elsewhere steps are workgroups of their own.  z: keys or values, and slices of `width` pieces of the rows, which move
+// independently of each other and make four workgroups of a KV head whose 256-byte rows are moved in place.
+// A use of a loaded value: it is waited for here.
+__device__ __forceinline__ void arrived(uint4 &x) { asm volatile("" : "+v"(x.x), "+v"(x.y), "+v"(x.z), "+v"(x.w)); }
+__device__ __forceinline__ void arrived(uint32_t &x) { asm volatile("" : "+v"(x)); }
+__device__ __forceinline__ void arrived(uint16_t &x) { asm volatile("" : "+v"(x)); }
+__device__ __forceinline__ void arrived(float &x) { asm volatile("" : "+v"(x)); }
+
+constexpr int kMoveRows = 8;  // rows per thread and step
 template <typename P>
-__global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, int pieces)
+__global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, int pieces, int width, int log_threads)
 {
-    constexpr int STEP = 8;  // pieces per thread and step
     const int row = blockIdx.y, b = row / a.H_kv, n = a.n[b], m = n < a.k ? n : a.k;
+    const bool of_v = blockIdx.z & 1;
+    const int piece = (int)(blockIdx.z >> 1) * width + ((int)threadIdx.x & ((1 << log_threads) - 1));
+    const bool mine = ((int)threadIdx.x & ((1 << log_threads) - 1)) < width && piece < pieces;
+    const int at_once = 256 >> log_threads, step = at_once * kMoveRows, r0 = (int)threadIdx.x >> log_threads;
     const int32_t *sel = a.sel + (size_t)row * a.k;
-    const P *Ks = (const P *)a.K + (size_t)row * a.L * pieces, *Vs = (const P *)a.V + (size_t)row * a.L * pieces;
-    P *Kd = (P *)a.K_out + (size_t)row * a.L_out * pieces, *Vd = (P *)a.V_out + (size_t)row * a.L_out * pieces;
-    const long long all = (long long)m * pieces;
-    for (long long p0 = (long long)blockIdx.x * 256 * STEP; p0 < all; p0 += (long long)gridDim.x * 256 * STEP) {
-        P k[STEP], v[STEP];
+    const P *from = (const P *)(of_v ? a.V : a.K) + (size_t)row * a.L * pieces + piece;
+    P *to = (P *)(of_v ? a.V_out : a.K_out) + (size_t)row * a.L_out * pieces + piece;
+    const bool in_place = (const void *)to == (const void *)from;
+    const bool head = blockIdx.z == 0;  // weights and row numbers are moved here
+    P x[2][kMoveRows];
+    int src[2][kMoveRows];  // -1: nothing to move
+    float w[2][kMoveRows];  // of rows i0 + 256 u + threadIdx.x of a step
+    int wsrc[2][kMoveRows];
+    auto read = [&](int i0, int s) __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < STEP; ++u) {
-            const long long p = p0 + u * 256 + threadIdx.x;
-            if (p < all) {
-                const size_t from = (size_t)sel[p / pieces] * pieces + p % pieces;
-                k[u] = Ks[from];
-                v[u] = Vs[from];
+        for (int u = 0; u < kMoveRows; ++u) {
+            const int i = i0 + u * at_once + r0;
+            src[s][u] = mine && i < m ? sel[i] : -1;
+            if (in_place && src[s][u] == i) src[s][u] = -1;
+        }
+#pragma unroll
+        for (int u = 0; u < kMoveRows; ++u) {
+            x[s][u] = P{};
+            if (src[s][u] >= 0) x[s][u] = from[(size_t)src[s][u] * pieces];
+        }
+        if (head) {
+#pragma unroll
+            for (int u = 0; u < kMoveRows; ++u) {
+                const int r = 256 * u + (int)threadIdx.x, i = i0 + r;
+                wsrc[s][u] = r < step && i < m ? sel[i] : -1;
+                w[s][u] = wsrc[s][u] >= 0 ? a.weights[(size_t)row * a.L + wsrc[s][u]] : 0.0f;
             }
         }
-        XKV_WAIT_VMCNT(0);
-        __syncthreads();
+    };
+    auto write = [&](int i0, int s) __attribute__((always_inline)) {
+        // every thread has what it reads in this step before any of them writes (the requests of the next step may be on their way)
 #pragma unroll
-        for (int u = 0; u < STEP; ++u) {
-            const long long p = p0 + u * 256 + threadIdx.x;
-            if (p < all) {
-                Kd[p] = k[u];
-                Vd[p] = v[u];
+        for (int u = 0; u < kMoveRows; ++u) arrived(x[s][u]);
+        if (head) {
+#pragma unroll
+            for (int u = 0; u < kMoveRows; ++u) arrived(w[s][u]);
+        }
+        lds_barrier();
+#pragma unroll
+        for (int u = 0; u < kMoveRows; ++u)
+            if (src[s][u] >= 0) to[(size_t)(i0 + u * at_once + r0) * pieces] = x[s][u];
+        if (head) {
+#pragma unroll
+            for (int u = 0; u < kMoveRows; ++u) {
+                const int r = 256 * u + (int)threadIdx.x, i = i0 + r;
+                if (r >= step || i >= a.k) continue;
+                if (wsrc[s][u] >= 0) a.weights_out[(size_t)row * a.L_out + i] = w[s][u];
+                if (a.rows_out) a.rows_out[(size_t)row * a.k + i] = wsrc[s][u];
             }
         }
+    };
+    const int stride = (int)gridDim.x * step;
+    int i0 = (int)blockIdx.x * step;
+    if (i0 < a.k) read(i0, 0);
+    for (; i0 < a.k; i0 += 2 * stride) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const int at = i0 + s * stride;
+            if (at >= a.k) break;
+            if (a.k - at > stride) read(at + stride, s ^ 1);
+            write(at, s);
+        }
     }
-    if (blockIdx.x > 0) return;
-    for (int i0 = 0; i0 < a.k; i0 += 256) {
-        const int i = i0 + threadIdx.x;
-        const bool real = i < m;
-        const float x = real ? a.weights[(size_t)row * a.L + sel[i]] : 0.0f;
-        XKV_WAIT_VMCNT(0);
-        __syncthreads();
-        if (real) a.weights_out[(size_t)row * a.L_out + i] = x;
-        if (i < a.k && a.rows_out) a.rows_out[(size_t)row * a.k + i] = real ? sel[i] : -1;
-    }
-    if (threadIdx.x == 0 && row == b * a.H_kv && a.lengths_out) a.lengths_out[b] = m;
+    if (blockIdx.x == 0 && head && threadIdx.x == 0 && row == b * a.H_kv && a.lengths_out) a.lengths_out[b] = m;
 }
 
 }  // namespace
@@ -77,8 +117,12 @@ hipError_t launch_evict(const xkv_shape &s, const CachePlan &p, const EvictArgs 
     const bool in_place = a.K_out == a.K || a.V_out == a.V || a.weights_out == a.weights;
     auto launch = [&](auto kernel, int piece) {
         const int pieces = (int)(row_bytes / piece);
-        const long long steps = ((long long)a.k * pieces + 2047) / 2048;
-        hipLaunchKernelGGL(kernel, dim3(in_place ? 1 : (unsigned)steps, rows), dim3(256), 0, st, a, pieces);
+        // in place: slices of whole 128-byte lines, so that more than two workgroups work on a KV head
+        const int width = in_place && row_bytes % 128 == 0 ? 128 / piece : pieces, slices = (pieces + width - 1) / width;
+        int log_threads = 0;
+        while ((1 << log_threads) < width) ++log_threads;
+        const int step = (256 >> log_threads) * kMoveRows;
+        hipLaunchKernelGGL(kernel, dim3(in_place ? 1 : (a.k + step - 1) / step, rows, 2 * slices), dim3(256), 0, st, a, pieces, width, log_threads);
         return hipGetLastError();
     };
     return bits % 16 == 0 ? launch(evict_move_kernel<uint4>, 16) : s.dtype == XKV_F32 ? launch(evict_move_kernel<uint32_t>, 4)
