@@ -180,6 +180,7 @@ __device__ __forceinline__ size_t part_row(const CacheArgs &a, CacheMode mode, i
 }
 
 constexpr int kMaxCacheParts = 256;  // parts of a sequence that the merge takes
+constexpr int kPartBlocks = 2048;    // blocks of a part (its first and its last one may be shared with its neighbours)
 
 struct CachePlan {
     int n_rep, words, n_c, k_ch;

@@ -63,6 +63,10 @@ xkv_status plan_cache_attend(const xkv_shape &s, CacheMode mode, int N, int c, C
     const int longest = ceil_div(most, p.round);  // parts that the longest sequence can have
     if (mode == CacheMode::blocks) {
         p.parts = clampi(ceil_div(want, tiles * batch * N), 1, clampi(longest, 1, kMaxCacheParts));
+        // (a part is a multiple of the round: blocks of few rows, up to a round more of them)
+        const int least = ceil_div(p.k_ch, kPartBlocks - p.round);
+        if (least > kMaxCacheParts) return XKV_ERR_UNSUPPORTED;
+        if (p.parts < least) p.parts = least;
     } else {
         const long long all = batch * longest;
         p.parts = clampi(ceil_div(want, tiles), (int)batch, (int)(all < (1 << 30) ? all : 1 << 30));

@@ -181,6 +181,7 @@ __global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(Cach
     __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE];
     __shared__ float sm_m[WT][32 * WR], sm_l[WT][32 * WR];
     __shared__ uint32_t sm_seen[32];
+    __shared__ int sm_rows[MODE == CacheMode::blocks ? kPartBlocks + 2 : 1];  // blocks: first rows of this part's blocks
     const int lane = lane_id(), w = wave_id(), rg = w % WR, tg = w / WR, n32 = lane & 31, hf = lane >> 5, n_rep = a.H_q / a.H_kv;
     const int M = MODE == CacheMode::blocks ? n_rep : a.N * n_rep;
     const CacheUnit u = cache_unit(a, MODE, (M + 32 * WR - 1) / (32 * WR));
@@ -192,7 +193,6 @@ __global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(Cach
     const bf16_t *Kg = (const bf16_t *)a.K + ((size_t)seq * a.H_kv + g) * a.L * 128, *Vg = (const bf16_t *)a.V + ((size_t)seq * a.H_kv + g) * a.L * 128;
     const bf16_t *Kd = (const bf16_t *)a.K_draft + ((size_t)seq * a.H_kv + g) * a.N * 128;
     const bf16_t *Vd = (const bf16_t *)a.V_draft + ((size_t)seq * a.H_kv + g) * a.N * 128;
-    const int32_t *sel = MODE == CacheMode::blocks ? a.sel + ((size_t)u.seq * a.H_kv + g) * a.k_ch : nullptr;
 
     // Q^T fragments: lane (row n32, hf), fragment f, position e: channel 16 f + 8 hf + e
     const int m_row = (tile * WR + rg) * 32 + n32, m_in = m_row < M ? m_row : M - 1;
@@ -213,6 +213,26 @@ __global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(Cach
         __syncthreads();
     }
 
+    // Blocks: a load of a block's number between the requests of rows would be waited for together with them, so the numbers go to LDS first.
+    // A lane's next tokens are TILE further on: `ahead` whole blocks and `rest` rows.
+    int in_list[8], in_block[8], rows_of[8], ahead = 0, rest = 0, last_row = 0;
+    if constexpr (MODE == CacheMode::blocks) {
+        static_assert(OWN, "rows of eight requests");
+        const int32_t *sel = a.sel + ((size_t)u.seq * a.H_kv + g) * a.k_ch;
+        const int b0 = t_begin / a.c, b1 = (t_end - 1) / a.c;  // b1 - b0 <= kPartBlocks
+        for (int i = threadIdx.x; i <= b1 - b0; i += 64 * WAVES) sm_rows[i] = sel[b0 + i] * a.c;
+        __syncthreads();
+        ahead = TILE / a.c;
+        rest = TILE % a.c;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int t = t_begin + 32 * w + 4 * i + (lane >> 4), j = t / a.c;
+            in_list[i] = j - b0;
+            in_block[i] = t - j * a.c;
+        }
+        last_row = sm_rows[b1 - b0] + (t_end - 1) - b1 * a.c;
+    }
+
     // Where this wavefront puts rows: its share of a tile that all read (WR > 1), or tiles of 32 rows of its own.
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem + (OWN ? 32768 * w : 256 * RPW * w);
     const int r4 = lane >> 4, x16 = lane & 15;
@@ -226,7 +246,27 @@ __global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(Cach
         constexpr bool is_v = decltype(values)::value;
         const uint32_t at = lds0 + buf * (OWN ? 16384 : STAGE) + (is_v ? VBASE : 0);
         const bf16_t *rows = is_v ? Vg : Kg;
-        if (MODE != CacheMode::blocks && first + RPW <= plain_end) {  // (wave-uniform) one after the other
+        if constexpr (MODE == CacheMode::blocks) {  // called for the tiles in turn, keys before values
+            if constexpr (!is_v) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const bool real = first + 4 * i + r4 < t_end;  // (else the last row again, with weight zero)
+                    rows_of[i] = real ? sm_rows[real ? in_list[i] : 0] + in_block[i] : last_row;
+                    in_list[i] += ahead;
+                    in_block[i] += rest;
+                    if (in_block[i] >= a.c) {
+                        in_block[i] -= a.c;
+                        ++in_list[i];
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i)
+                copy16_global_to_lds((const unsigned char *)(rows + (size_t)rows_of[i] * 128) + ((is_v ? voff[i & 1] : koff[i & 3]) - 256 * r4),
+                                     at + 1024 * i);
+            return;
+        }
+        if (first + RPW <= plain_end) {  // (wave-uniform) one after the other
             const unsigned char *base = (const unsigned char *)(rows + (size_t)first * 128);
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {
@@ -247,7 +287,6 @@ __global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(Cach
                 from = t < n ? rows + (size_t)t * 128 : draft ? (is_v ? Vd : Kd) + (size_t)j * 128 : (const bf16_t *)kZeroRow;
             } else {
                 t = t < t_end ? t : t_end - 1;  // (its weight will be zero)
-                if (MODE == CacheMode::blocks) t = sel[t / a.c] * a.c + t % a.c;
                 from = rows + (size_t)t * 128;
             }
             copy16_global_to_lds((const unsigned char *)from + ((is_v ? voff[i & 1] : koff[i & 3]) - 256 * r4), at + 1024 * i);
