@@ -62,25 +62,41 @@ struct CacheUnit {
     bool some;           // whether there is anything to do
 };
 
+// Over the 64 lanes of a wavefront, in all of them, without LDS: neighbours, then rows of 16, halves.
+template <int CTRL> __device__ __forceinline__ uint32_t lanes_by(uint32_t x) { return __builtin_amdgcn_update_dpp(0u, x, CTRL, 0xF, 0xF, true); }
+template <typename T, typename OP> __device__ __forceinline__ T wave_all(T v, OP op)
+{
+    static_assert(sizeof(T) == 4, "one register");
+    auto with = [&](uint32_t o) { v = op(v, __builtin_bit_cast(T, o)); };
+    with(lanes_by<0xB1>(__builtin_bit_cast(uint32_t, v)));
+    with(lanes_by<0x4E>(__builtin_bit_cast(uint32_t, v)));
+    with(lanes_by<0x141>(__builtin_bit_cast(uint32_t, v)));
+    with(lanes_by<0x140>(__builtin_bit_cast(uint32_t, v)));
+    const auto r16 = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+    v = op(__builtin_bit_cast(T, (uint32_t)r16[0]), __builtin_bit_cast(T, (uint32_t)r16[1]));
+    const auto r32 = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+    return op(__builtin_bit_cast(T, (uint32_t)r32[0]), __builtin_bit_cast(T, (uint32_t)r32[1]));
+}
+struct AddOp {
+    template <typename T> __device__ __forceinline__ T operator()(T x, T y) const { return x + y; }
+};
+struct MaxOp {
+    __device__ __forceinline__ float operator()(float x, float y) const { return fmaxf(x, y); }
+    __device__ __forceinline__ int operator()(int x, int y) const { return x > y ? x : y; }
+};
+
 __device__ __forceinline__ int ceil_div_dev(int a, int b) { return (int)(((unsigned)a + (unsigned)b - 1u) / (unsigned)b); }
 
 // Tokens per part.  All lanes of a wavefront call it together.
 __device__ __forceinline__ int cache_chunk(const CacheArgs &a, CacheMode mode)
 {
     const int lane = lane_id();
-    long long total = 0;
+    long long total = 0;  // (of 64 sequences: in whole 4096s and the rest)
     int most = 0;
     for (int b0 = 0; b0 < a.batch; b0 += kWave) {
-        int t = b0 + lane < a.batch ? cache_tokens(a, mode, cache_rows(a, b0 + lane)) : 0;
-        long long s = t;
-#pragma unroll
-        for (int off = 32; off > 0; off >>= 1) {
-            s += __shfl_xor(s, off, kWave);
-            const int o = __shfl_xor(t, off, kWave);
-            t = t > o ? t : o;
-        }
-        total += s;
-        most = most > t ? most : t;
+        const int t = b0 + lane < a.batch ? cache_tokens(a, mode, cache_rows(a, b0 + lane)) : 0;
+        total += ((long long)wave_all(t >> 12, AddOp()) << 12) + wave_all(t & 4095, AddOp());
+        most = MaxOp()(most, wave_all(t, MaxOp()));
     }
     const int whole = ceil_div_dev(most > 0 ? most : 1, a.round) * a.round;  // (a part per sequence is always allowed)
     if (a.parts <= a.batch || total == 0) return whole;
@@ -128,6 +144,19 @@ __device__ __forceinline__ CacheUnit cache_unit(const CacheArgs &a, CacheMode mo
     }
     u.g = id % a.H_kv;
     u.part = id / a.H_kv;
+    if (a.batch == 1) {
+        u.n = cache_rows(a, 0);
+        u.n_tok = cache_tokens(a, mode, u.n);
+        const int chunk = ceil_div_dev(ceil_div_dev(u.n_tok > 0 ? u.n_tok : 1, a.parts), a.round) * a.round;
+        u.t_begin = u.part * chunk;
+        u.t_end = u.t_begin + chunk < u.n_tok ? u.t_begin + chunk : u.n_tok;
+        u.some = u.t_begin < u.t_end;
+        if (x == 0 && threadIdx.x == 0) {
+            a.table[0] = 0;
+            a.table[1] = ceil_div_dev(u.n_tok, chunk);
+        }
+        return u;
+    }
     const int chunk = __builtin_amdgcn_readfirstlane(cache_chunk(a, mode));
     int before = 0;
     for (int b0 = 0; b0 < a.batch; b0 += kWave) {
@@ -136,6 +165,7 @@ __device__ __forceinline__ CacheUnit cache_unit(const CacheArgs &a, CacheMode mo
         int upto = mine;
 #pragma unroll
         for (int off = 1; off < kWave; off <<= 1) {
+            if (off >= a.batch) break;
             const int o = __shfl_up(upto, off, kWave);
             upto += lane >= off ? o : 0;
         }

@@ -36,26 +36,53 @@ __device__ __forceinline__ uint32_t draft_bits(const CacheArgs &a, int seq, int 
 }
 
 // ------------------------------------------------------------------------------------------
-// General path, any type, width and alignment.  A round takes 64 tokens: their keys go to LDS in single precision and a lane
-// multiplies one of them with the four queries of its wavefront, which are there, too; for the values lanes run over the
-// columns, and the weights come from the lanes that hold them.
+// General path, any type, width and alignment.  A round takes 64 tokens, whose keys and values go to LDS in single precision (the
+// next round's are requested before this one is computed).  For the logits a lane multiplies one of the keys with the four queries
+// of its wavefront, four channels a time; for the sums lanes run over the channels, and the weights come from the lanes that
+// hold them.  With few rows its time is that of one round, latencies: 8 drafted tokens of 4 heads after 512 tokens, fp32.
 // ------------------------------------------------------------------------------------------
+__host__ __device__ inline int general_pitch(int d) { return ((d + 3) / 4 | 1) * 4; }  // floats; an odd number of 16-byte pieces
+
 template <typename T, CacheMode MODE, int JP>
 __global__ __launch_bounds__(256) void cache_attend_general_kernel(CacheArgs a)
 {
-    extern __shared__ float smem_f[];
-    const int lane = lane_id(), w = wave_id(), n_rep = a.H_q / a.H_kv, d = a.d_h, pitch = d | 1;
+    extern __shared__ __attribute__((aligned(16))) float smem_f[];
+    constexpr int PER_WAVE = kGenTokens / 4;
+    const int lane = lane_id(), w = wave_id(), n_rep = a.H_q / a.H_kv, d = a.d_h, d4 = (d + 3) / 4 * 4, pitch = general_pitch(d);
     const int M = MODE == CacheMode::blocks ? n_rep : a.N * n_rep;
     const CacheUnit u = cache_unit(a, MODE, (M + kGenRows - 1) / kGenRows);
     if (!u.some) return;  // (the merge knows)
     const int tile = u.tile, g = u.g, n = u.n, t_begin = u.t_begin, t_end = u.t_end;
     // blocks: one query token; else all query tokens of a sequence
     const int seq = MODE == CacheMode::blocks ? u.seq / a.N : u.seq, first_token = MODE == CacheMode::blocks ? u.seq % a.N : 0;
-    float *kt = smem_f, *qs = kt + kGenTokens * pitch;
+    float *kt = smem_f, *vt = kt + kGenTokens * pitch, *qs = vt + kGenTokens * pitch;
 
     const T *Kg = (const T *)a.K + ((size_t)seq * a.H_kv + g) * a.L * d, *Vg = (const T *)a.V + ((size_t)seq * a.H_kv + g) * a.L * d;
     const T *Kd = (const T *)a.K_draft + ((size_t)seq * a.H_kv + g) * a.N * d, *Vd = (const T *)a.V_draft + ((size_t)seq * a.H_kv + g) * a.N * d;
     const int32_t *sel = MODE == CacheMode::blocks ? a.sel + ((size_t)u.seq * a.H_kv + g) * a.k_ch : nullptr;
+
+    // The row of this lane's token of a round (beyond the last one: that one again); drafted tokens are rows L, L + 1, ..
+    auto row_of = [&](int t0) __attribute__((always_inline)) {
+        const int t = t0 + lane < t_end ? t0 + lane : t_end - 1;
+        if (MODE == CacheMode::blocks) return sel[t / a.c] * a.c + t % a.c;
+        return MODE == CacheMode::tree && t >= n ? a.L + t - n : t;
+    };
+    T kr[PER_WAVE][JP], vr[PER_WAVE][JP];
+    auto request = [&](int row) __attribute__((always_inline)) {  // tokens w, w + 4, .. of a round
+#pragma unroll
+        for (int i = 0; i < PER_WAVE; ++i) {
+            const int rw = __builtin_amdgcn_readlane(row, 4 * i + w);
+            const bool draft = MODE == CacheMode::tree && rw >= a.L;
+            const T *k = draft ? Kd + (size_t)(rw - a.L) * d : Kg + (size_t)rw * d, *v = draft ? Vd + (size_t)(rw - a.L) * d : Vg + (size_t)rw * d;
+#pragma unroll
+            for (int jj = 0; jj < JP; ++jj) {
+                const int j = lane + jj * kWave, jc = j < d ? j : 0;
+                kr[i][jj] = k[jc];
+                vr[i][jj] = v[jc];
+            }
+        }
+    };
+    request(row_of(t_begin));
 
     // row m of this workgroup: query token first_token + m / n_rep, head g n_rep + m % n_rep
     const int m0 = tile * kGenRows + 4 * w;
@@ -73,71 +100,83 @@ __global__ __launch_bounds__(256) void cache_attend_general_kernel(CacheArgs a)
         for (int jj = 0; jj < JP; ++jj) {
             const int j = lane + jj * kWave;
             o[r][jj] = 0.0f;
-            if (j < d) qs[(4 * w + r) * d + j] = to_f32(((const T *)a.q)[row_id[r] * d + j]);
+            if (j < d4) qs[(4 * w + r) * d4 + j] = j < d ? to_f32(((const T *)a.q)[row_id[r] * d + j]) : 0.0f;
         }
     }
     for (int t0 = t_begin; t0 < t_end; t0 += kGenTokens) {
-        // this lane's token (beyond the last one: that one again) and its row; drafted tokens are rows L, L + 1, ..
         const int t = t0 + lane < t_end ? t0 + lane : t_end - 1;
         const bool real = t0 + lane < t_end;
-        int row = t;
-        if (MODE == CacheMode::tree && t >= n) row = a.L + t - n;
-        if (MODE == CacheMode::blocks) row = sel[t / a.c] * a.c + t % a.c;
         __syncthreads();
-        for (int i = w; i < kGenTokens; i += 4) {
-            const int rw = __builtin_amdgcn_readlane(row, i);
-            const T *k = MODE == CacheMode::tree && rw >= a.L ? Kd + (size_t)(rw - a.L) * d : Kg + (size_t)rw * d;
+#pragma unroll
+        for (int i = 0; i < PER_WAVE; ++i)
 #pragma unroll
             for (int jj = 0; jj < JP; ++jj) {
                 const int j = lane + jj * kWave;
-                if (j < d) kt[i * pitch + j] = to_f32(k[j]);
+                if (j < d4) {
+                    kt[(4 * i + w) * pitch + j] = j < d ? to_f32(kr[i][jj]) : 0.0f;
+                    vt[(4 * i + w) * pitch + j] = to_f32(vr[i][jj]);
+                }
+            }
+        __syncthreads();
+        if (t0 + kGenTokens < t_end) request(row_of(t0 + kGenTokens));
+        float p[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int j = 0; j < d4; j += 4) {
+            const float4 x = *reinterpret_cast<const float4 *>(kt + lane * pitch + j);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float4 y = *reinterpret_cast<const float4 *>(qs + (4 * w + r) * d4 + j);
+                p[r] = fmaf(x.w, y.w, fmaf(x.z, y.z, fmaf(x.y, y.y, fmaf(x.x, y.x, p[r]))));
             }
         }
-        __syncthreads();
-        float p[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int j = 0; j < d; ++j) {
-            const float x = kt[lane * pitch + j];
+        float z[4], top[4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) p[r] = fmaf(x, qs[(4 * w + r) * d + j], p[r]);
+        for (int r = 0; r < 4; ++r) {
+            z[r] = a.scale * p[r];
+            if (MODE == CacheMode::weights && real && m0 + r < M) a.logits[row_id[r] * a.L + t] = z[r];
+            if (!real) z[r] = -INFINITY;
+        }
+        if (MODE == CacheMode::tree && t0 + kGenTokens > n) {
+            uint32_t bits[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) bits[r] = draft_bits(a, seq, token[r], t - n);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) z[r] = bits[r] & 1u ? z[r] : -INFINITY;
         }
         int used = 0;
 #pragma unroll
+        for (int r = 0; r < 4; ++r) top[r] = wave_all(z[r], MaxOp());
+#pragma unroll
         for (int r = 0; r < 4; ++r) {
-            bool sees = real;
-            if (MODE == CacheMode::tree && t0 + kGenTokens > n) sees = real && (draft_bits(a, seq, token[r], t - n) & 1u);
-            const float z = a.scale * p[r];
-            if (MODE == CacheMode::weights && real && m0 + r < M) a.logits[row_id[r] * a.L + t] = z;
-            const float m_new = fmaxf(mx[r], wave_max(sees ? z : -INFINITY));
+            const float m_new = fmaxf(mx[r], top[r]);
             const float alpha = m_new == -INFINITY ? 1.0f : expf(mx[r] - m_new);
-            p[r] = sees ? expf(z - m_new) : 0.0f;
-            used |= sees;
-            den[r] = den[r] * alpha + wave_sum(p[r]);
+            p[r] = z[r] == -INFINITY ? 0.0f : expf(z[r] - m_new);
+            used |= z[r] != -INFINITY;
+            den[r] = den[r] * alpha + wave_all(p[r], AddOp());
             mx[r] = m_new;
 #pragma unroll
             for (int jj = 0; jj < JP; ++jj) o[r][jj] *= alpha;
         }
         const int count = t_end - t0 < kGenTokens ? t_end - t0 : kGenTokens;
-        for (int i0 = 0; i0 < count; i0 += 4) {
-            float v[4][JP];
+        for (int i0 = 0; i0 < count; i0 += 8) {  // (lanes from `count` on hold the last token again, with weight zero)
+            float v[8][JP];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {  // (lanes from `count` on hold the last token again, with weight zero)
-                const int rw = __builtin_amdgcn_readlane(row, i0 + u);
-                const T *x = MODE == CacheMode::tree && rw >= a.L ? Vd + (size_t)(rw - a.L) * d : Vg + (size_t)rw * d;
+            for (int x = 0; x < 8; ++x) {
                 // a drafted token that none of these rows sees may be padding with anything in it
-                const bool use = __builtin_amdgcn_readlane(used, i0 + u) != 0;
+                const bool use = __builtin_amdgcn_readlane(used, i0 + x) != 0;
 #pragma unroll
                 for (int jj = 0; jj < JP; ++jj) {
                     const int j = lane + jj * kWave;
-                    v[u][jj] = j < d && use ? to_f32(x[j]) : 0.0f;
+                    const float y = vt[(i0 + x) * pitch + (j < d ? j : 0)];
+                    v[x][jj] = use ? y : 0.0f;
                 }
             }
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
+            for (int x = 0; x < 8; ++x)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const float pw = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(p[r]), i0 + u));
+                    const float pw = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(p[r]), i0 + x));
 #pragma unroll
-                    for (int jj = 0; jj < JP; ++jj) o[r][jj] = fmaf(pw, v[u][jj], o[r][jj]);
+                    for (int jj = 0; jj < JP; ++jj) o[r][jj] = fmaf(pw, v[x][jj], o[r][jj]);
                 }
         }
     }
@@ -509,14 +548,14 @@ __global__ __launch_bounds__(256) void cache_merge_kernel(CacheArgs a)
     const float *ml = a.part_ml + row * 2;
     float M = -INFINITY;
     for (int s = lane; s < parts; s += kWave) M = fmaxf(M, ml[2 * s * stride]);
-    M = wave_max(M);
+    M = wave_all(M, MaxOp());
     float den = 0.0f;
     for (int s = lane; s < parts; s += kWave) {
         const float m = ml[2 * s * stride], wt = m == -INFINITY ? 0.0f : expf(m - M);
         if (w == 0) sm_w[s] = wt;
         den = fmaf(wt, ml[2 * s * stride + 1], den);
     }
-    den = wave_sum(den);
+    den = wave_all(den, AddOp());
     __syncthreads();
     const float *po = a.part_o + row * d;
     for (int j = lane; j < d; j += kWave) {
@@ -550,9 +589,9 @@ __global__ __launch_bounds__(256) void cache_weights_kernel(CacheArgs a, float *
         const float *ml = a.part_ml + part_row(a, CacheMode::weights, first, 0, g * n_rep + h) * 2;
         float M = -INFINITY, den = 0.0f;
         for (int s = lane; s < parts; s += kWave) M = fmaxf(M, ml[2 * s * stride]);
-        M = wave_max(M);
+        M = wave_all(M, MaxOp());
         for (int s = lane; s < parts; s += kWave) den = fmaf(expf(ml[2 * s * stride] - M), ml[2 * s * stride + 1], den);
-        den = wave_sum(den);
+        den = wave_all(den, AddOp());
         if (lane == 0) {
             sm_m[h] = M;
             sm_r[h] = 1.0f / den;
@@ -579,9 +618,9 @@ hipError_t launch_general(const CacheArgs &a, hipStream_t st)
 {
     const int M = MODE == CacheMode::blocks ? a.H_q / a.H_kv : a.N * (a.H_q / a.H_kv);
     const dim3 grid = unit_grid(a, MODE, M);
-    const size_t lds = ((size_t)kGenTokens * (a.d_h | 1) + (size_t)kGenRows * a.d_h) * sizeof(float);
+    const size_t lds = (2 * (size_t)kGenTokens * general_pitch(a.d_h) + (size_t)kGenRows * ((a.d_h + 3) / 4 * 4)) * sizeof(float);
     auto launch = [&](auto kernel, DynamicLdsOnce &attr) {
-        const hipError_t e = attr.ensure((const void *)kernel, lds > 65536 ? 160 * 1024 : lds);
+        const hipError_t e = attr.ensure((const void *)kernel, 160 * 1024);  // (at most 146 KiB, at 256 channels)
         if (e != hipSuccess) return e;
         hipLaunchKernelGGL(kernel, grid, dim3(256), lds, st, a);
         return hipGetLastError();
