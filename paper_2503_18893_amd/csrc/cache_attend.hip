@@ -214,7 +214,7 @@ template <CacheMode MODE, int WR, int WT, int SUB>
 __global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(CacheArgs a)
 {
     constexpr bool OWN = WR == 1;  // tiles that only one wavefront reads
-    constexpr int WAVES = WR * WT, TILE = 32 * SUB * WT, STAGE = 512 * TILE, RPW = TILE / WAVES, LOADS = RPW / 4, VBASE = OWN ? 8192 : 256 * TILE;
+    constexpr int WAVES = WR * WT, TILE = 32 * SUB * WT, STAGE = 512 * TILE, RPW = TILE / WAVES, LOADS = RPW / 4, KTILE = OWN ? 8192 : 256 * TILE, VBASE = OWN ? KTILE : 2 * KTILE;
     static_assert(!OWN || SUB == 1, "a wavefront's tile is 32 tokens");
     static_assert(RPW % 16 == 0 && 2 * STAGE >= WAVES * 16384, "rotations by i; room for the merge");
     __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE];
@@ -281,9 +281,21 @@ __global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(Cach
 #pragma unroll
     for (int i = 0; i < 2; ++i) voff[i] = 256 * r4 + 32 * (((x16 >> 1) - 4 * i - r4) & 7) + 16 * (x16 & 1);
     const int plain_end = MODE == CacheMode::tree && n < t_end ? n : t_end;  // rows of the cache end here
+    auto stage_plain = [&](int first, int buf, auto values) __attribute__((always_inline)) {  // RPW rows of the cache
+        constexpr bool is_v = decltype(values)::value;
+        const uint32_t at = lds0 + buf * (OWN ? 2 * KTILE : KTILE) + (is_v ? VBASE : 0);
+        const unsigned char *base = (const unsigned char *)((is_v ? Vg : Kg) + (size_t)first * 128);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            if (OWN)
+                copy16_to_lds_once(base + 1024 * i, is_v ? voff[i & 1] : koff[i & 3], at + 1024 * i);
+            else
+                copy16_to_lds(base + 1024 * i, is_v ? voff[i & 1] : koff[i & 3], at + 1024 * i);
+        }
+    };
     auto stage = [&](int first, int buf, auto values) __attribute__((always_inline)) {  // RPW tokens from `first` on
         constexpr bool is_v = decltype(values)::value;
-        const uint32_t at = lds0 + buf * (OWN ? 16384 : STAGE) + (is_v ? VBASE : 0);
+        const uint32_t at = lds0 + buf * (OWN ? 2 * KTILE : KTILE) + (is_v ? VBASE : 0);
         const bf16_t *rows = is_v ? Vg : Kg;
         if constexpr (MODE == CacheMode::blocks) {  // called for the tiles in turn, keys before values
             if constexpr (!is_v) {
@@ -305,15 +317,8 @@ __global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(Cach
                                      at + 1024 * i);
             return;
         }
-        if (first + RPW <= plain_end) {  // (wave-uniform) one after the other
-            const unsigned char *base = (const unsigned char *)(rows + (size_t)first * 128);
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                if (OWN)
-                    copy16_to_lds_once(base + 1024 * i, is_v ? voff[i & 1] : koff[i & 3], at + 1024 * i);
-                else
-                    copy16_to_lds(base + 1024 * i, is_v ? voff[i & 1] : koff[i & 3], at + 1024 * i);
-            }
+        if (first + RPW <= plain_end) {  // (wave-uniform)
+            stage_plain(first, buf, values);
             return;
         }
 #pragma unroll
@@ -351,20 +356,20 @@ __global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(Cach
 #pragma unroll
     for (int db = 0; db < 4; ++db) O[db] = f32x16_t(0.0f);
     float m_run = -INFINITY, l_run = 0.0f;
-    f32x16_t S[SUB];
-    auto logits = [&](const unsigned char *lds) __attribute__((always_inline)) {
+    // logits of a tile of keys
+    auto logits = [&](const unsigned char *lds, f32x16_t (&S)[SUB]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int s = 0; s < SUB; ++s) {
-            S[s] = f32x16_t(0.0f);
+        for (int s = 0; s < SUB; ++s) S[s] = f32x16_t(0.0f);
 #pragma unroll
-            for (int f = 0; f < 8; ++f) {
+        for (int f = 0; f < 8; ++f)
+#pragma unroll
+            for (int s = 0; s < SUB; ++s) {
                 const u32x4_t kf = *reinterpret_cast<const u32x4_t *>(lds + kat[f] + 8192 * s);
                 S[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf), Qf[f], S[s], 0, 0, 0);
             }
-        }
     };
-    auto weigh = [&](int tw) __attribute__((always_inline)) {
-        // register v of part s is token tw + 32 s + 8 (v / 4) + 4 hf + v % 4
+    // register v of part s is token tw + 32 s + 8 (v / 4) + 4 hf + v % 4: what this row does not see; then the logits that are kept
+    auto hide = [&](int tw, f32x16_t (&S)[SUB]) __attribute__((always_inline)) {
         if (tw + 32 * SUB > plain_end) {
 #pragma unroll
             for (int s = 0; s < SUB; ++s) {
@@ -386,14 +391,18 @@ __global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(Cach
                     if (tw + t + 4 * hf < t_end) to[t] = a.scale * S[s][v];
                 }
         }
-        float m_loc = S[0][0];
+    };
+    auto top_of = [&](const f32x16_t (&S)[SUB]) __attribute__((always_inline)) {
+        float m = S[0][0];
 #pragma unroll
         for (int s = 0; s < SUB; ++s)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) m_loc = fmaxf(m_loc, S[s][v]);
+            for (int v = 0; v < 16; ++v) m = fmaxf(m, S[s][v]);
         float lo, hi;
-        halves(m_loc, lo, hi);
-        m_loc = fmaxf(lo, hi);
+        halves(m, lo, hi);
+        return fmaxf(lo, hi);
+    };
+    auto raise = [&](float m_loc) __attribute__((always_inline)) {
         if (__ballot((m_loc - m_run) * c > 8.0f)) {
             const float m_new = fmaxf(m_run, m_loc), alpha = m_run == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m_run - m_new) * c);
             l_run *= alpha;
@@ -403,23 +412,27 @@ __global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(Cach
                 for (int v = 0; v < 16; ++v) O[db][v] *= alpha;
             m_run = m_new;
         }
-        const float less = m_run == -INFINITY ? 0.0f : -m_run * c;
-        float l_add = 0.0f;
-#pragma unroll
-        for (int s = 0; s < SUB; ++s)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                S[s][v] = __builtin_amdgcn_exp2f(fmaf(S[s][v], c, less));
-                l_add += S[s][v];
-            }
-        l_run += l_add;
     };
-    auto add_values = [&](const unsigned char *lds) __attribute__((always_inline)) {
+    auto weigh = [&](f32x16_t (&S)[SUB], bf16x8_t (&P)[2 * SUB]) __attribute__((always_inline)) {
+        const float less = m_run == -INFINITY ? 0.0f : -m_run * c;
 #pragma unroll
         for (int s = 0; s < SUB; ++s)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const bf16x8_t P = pack8(S[s], j);
+#pragma unroll
+                for (int v = 8 * j; v < 8 * j + 8; ++v) {
+                    S[s][v] = __builtin_amdgcn_exp2f(fmaf(S[s][v], c, less));
+                    if (OWN) l_run += S[s][v];  // (the weights that are given out are divided by this sum: in single precision)
+                }
+                P[2 * s + j] = pack8(S[s], j);
+                if (!OWN) l_run = add_pairs(P[2 * s + j], l_run);
+            }
+    };
+    auto add_values = [&](const unsigned char *lds, const bf16x8_t (&P)[2 * SUB]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int s = 0; s < SUB; ++s)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int db = 0; db < 4; ++db) {
                     // position e of lane (channel, hf): token 16 j + 8 (e / 4) + 4 hf + e % 4, as in P
@@ -427,9 +440,8 @@ __global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(Cach
                     const s16x4_t a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)from);
                     const s16x4_t a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(from + 2048));
                     O[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                        __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7)), P, O[db], 0, 0, 0);
+                        __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7)), P[2 * s + j], O[db], 0, 0, 0);
                 }
-            }
     };
     if constexpr (OWN) {
         // A wavefront keeps two tiles of its own and waits for nobody: the keys of the tile after the next are requested as soon as the
@@ -453,12 +465,16 @@ __global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(Cach
             else
                 XKV_WAIT_VMCNT(LOADS);
             asm volatile("" : : : "memory");
-            logits(lds);
+            f32x16_t S[SUB];
+            bf16x8_t P[2 * SUB];
+            logits(lds, S);
             if (then) {
                 wait_lds();
                 stage(t + 2 * TILE, buf, keys);
             }
-            weigh(t);
+            hide(t, S);
+            raise(top_of(S));
+            weigh(S, P);
             if (then)
                 XKV_WAIT_VMCNT(3 * LOADS);
             else if (next)
@@ -466,27 +482,112 @@ __global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(Cach
             else
                 XKV_WAIT_VMCNT(0);
             asm volatile("" : : : "memory");
-            add_values(lds);
+            add_values(lds, P);
             if (then) {
                 wait_lds();
                 stage(t + 2 * TILE, buf, values);
             }
         }
     } else {
+        // One tile ahead with the logits: the products of tile i + 1 with the keys run beside the exponentials of tile i, those of tile i
+        // with the values beside the maximum of tile i + 1.  Keys i + 1 and values i are there at the barrier, and nobody reads keys i
+        // and values i - 1 any more, whose places keys i + 2 and values i + 1 take.
         stage(t_begin + RPW * w, 0, keys);
         stage(t_begin + RPW * w, 0, values);
-        int buf = 0;
-        for (int t0 = t_begin; t0 < t_end; t0 += TILE, buf ^= 1) {
+        if (t_begin + TILE < t_end) stage(t_begin + TILE + RPW * w, 1, keys);
+        if (t_begin + TILE < t_end)
+            XKV_WAIT_VMCNT(2 * LOADS);
+        else
+            XKV_WAIT_VMCNT(LOADS);
+        __syncthreads();
+        f32x16_t S[SUB];
+        logits(lds_w, S);
+        hide(t_begin + 32 * SUB * tg, S);
+        float m_loc = top_of(S);
+        auto step = [&](int t0, auto which, f32x16_t (&S)[SUB], f32x16_t (&S1)[SUB]) __attribute__((always_inline)) {
+            constexpr int BUF = decltype(which)::value;
             XKV_WAIT_VMCNT(0);
-            __syncthreads();  // this tile is there, and nobody reads the other one any more
-            if (t0 + TILE < t_end) {
-                stage(t0 + TILE + RPW * w, buf ^ 1, keys);
-                stage(t0 + TILE + RPW * w, buf ^ 1, values);
+            __syncthreads();
+            stage_plain(t0 + 2 * TILE + RPW * w, BUF, keys);
+            stage_plain(t0 + TILE + RPW * w, BUF ^ 1, values);
+            raise(m_loc);
+            const unsigned char *kt = lds_w + (BUF ^ 1) * KTILE, *vt = lds_w + BUF * KTILE;
+            constexpr int STEPS = 8 * SUB, AHEAD = 3;
+            bf16x8_t P[2 * SUB];
+            // each product with the keys beside two exponentials
+            u32x4_t kf[STEPS];
+            auto read_key = [&](int i) __attribute__((always_inline)) {
+                kf[i] = *reinterpret_cast<const u32x4_t *>(kt + kat[i / SUB] + 8192 * (i % SUB));
+            };
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) read_key(i);
+            const float less = m_run == -INFINITY ? 0.0f : -m_run * c;
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) {
+                if (i + AHEAD < STEPS) read_key(i + AHEAD);
+                if (i < SUB) S1[i % SUB] = f32x16_t(0.0f);
+                S1[i % SUB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[i]), Qf[i / SUB], S1[i % SUB], 0, 0, 0);
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const int v = 2 * i + x;
+                    S[v / 16][v % 16] = __builtin_amdgcn_exp2f(fmaf(S[v / 16][v % 16], c, less));
+                }
+                if (i % 4 == 3) {
+                    P[i / 4] = pack8(S[i / 8], i / 4 % 2);
+                    l_run = add_pairs(P[i / 4], l_run);
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
-            const unsigned char *lds = lds_w + buf * STAGE;
-            logits(lds);
-            weigh(t0 + 32 * SUB * tg);
-            add_values(lds);
+            // each product with the values beside its share of the next maximum
+            s16x4_t vf[STEPS][2];
+            auto read_values = [&](int i) __attribute__((always_inline)) {
+                const unsigned char *from = vt + vat[i % 4] + 4096 * (i / 4);
+                vf[i][0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)from);
+                vf[i][1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(from + 2048));
+            };
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) read_values(i);
+            float m_next[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) {
+                if (i + AHEAD < STEPS) read_values(i + AHEAD);
+                O[i % 4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                    __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(vf[i][0], vf[i][1], 0, 1, 2, 3, 4, 5, 6, 7)), P[i / 4], O[i % 4], 0, 0, 0);
+                if (i >= STEPS / 2) {
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const int v = 4 * (i - STEPS / 2) + x;
+                        m_next[x >> 1] = fmaxf(m_next[x >> 1], S1[v / 16][v % 16]);
+                    }
+                    asm volatile("" : "+v"(m_next[0]), "+v"(m_next[1]));  // (here, not at the end)
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            float lo, hi;
+            halves(fmaxf(m_next[0], m_next[1]), lo, hi);
+            m_loc = fmaxf(lo, hi);
+        };
+        int buf = 0, t0 = t_begin;
+        for (; t0 + 4 * TILE <= plain_end; t0 += 2 * TILE) {  // the next three tiles are whole
+            f32x16_t S1[SUB];
+            step(t0, std::integral_constant<int, 0>{}, S, S1);
+            step(t0 + TILE, std::integral_constant<int, 1>{}, S1, S);
+        }
+        for (; t0 < t_end; t0 += TILE, buf ^= 1) {
+            XKV_WAIT_VMCNT(0);
+            __syncthreads();
+            if (t0 + 2 * TILE < t_end) stage(t0 + 2 * TILE + RPW * w, buf, keys);
+            if (t0 + TILE < t_end) stage(t0 + TILE + RPW * w, buf ^ 1, values);
+            raise(m_loc);
+            f32x16_t S1[SUB];
+            bf16x8_t P[2 * SUB];
+            logits(lds_w + (buf ^ 1) * KTILE, S1);  // (behind the last tile: of whatever is there, not used)
+            weigh(S, P);
+            if (t0 + TILE < t_end) hide(t0 + TILE + 32 * SUB * tg, S1);
+            add_values(lds_w + buf * KTILE, P);
+            m_loc = top_of(S1);
+#pragma unroll
+            for (int s = 0; s < SUB; ++s) S[s] = S1[s];
         }
     }
 
@@ -534,42 +635,64 @@ __global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(Cach
 }
 
 // ------------------------------------------------------------------------------------------
-// Merge: one workgroup per (query token, head).  Partials that no token went to were not written and are not read.
+// Merge.  A group of 2^lg lanes covers the columns of a row (query token, head), VEC a lane.  Where there are many rows, a group per row;
+// where there are few, all groups of a workgroup share a row's partials between them and are added up in LDS: latency is all there is to
+// it then.  Partials that no token went to were
+// not written and are not read.
 // ------------------------------------------------------------------------------------------
-template <typename T, CacheMode MODE>
-__global__ __launch_bounds__(256) void cache_merge_kernel(CacheArgs a)
+template <typename T, CacheMode MODE, int VEC>
+__global__ __launch_bounds__(256) void cache_merge_kernel(CacheArgs a, int lg, int share, int rows)
 {
-    __shared__ float sm_w[kMaxCacheParts], sm_o[4][256];
-    const int lane = lane_id(), w = wave_id(), d = a.d_h;
-    const int z = blockIdx.y, head = blockIdx.x;  // z: (sequence, query token)
+    typedef __attribute__((ext_vector_type(VEC))) float vec_t;
+    constexpr int BATCH = 4;
+    __shared__ vec_t sm[256];
+    __shared__ float sm_w[32][kMaxCacheParts];
+    const int width = 1 << lg, l = (int)threadIdx.x & (width - 1), grp = (int)threadIdx.x >> lg, groups = 256 >> lg;
+    const int col = ((int)blockIdx.y * width + l) * VEC;
+    const int item = share ? (int)blockIdx.x : (int)blockIdx.x * groups + grp, row = item < rows ? item : rows - 1;
+    const int z = row / a.H_q, head = row % a.H_q;  // z: (sequence, query token)
     int first, parts;
-    cache_parts(a, MODE, MODE == CacheMode::blocks ? z : z / a.N, first, parts);
-    const size_t row = part_row(a, MODE, first, z % a.N, head), stride = part_row(a, MODE, 1, 0, 0);  // of its first part, to the next one
-    const float *ml = a.part_ml + row * 2;
-    float M = -INFINITY;
-    for (int s = lane; s < parts; s += kWave) M = fmaxf(M, ml[2 * s * stride]);
-    M = wave_all(M, MaxOp());
-    float den = 0.0f;
-    for (int s = lane; s < parts; s += kWave) {
+    cache_parts(a, MODE, MODE == CacheMode::tree ? z / a.N : z, first, parts);
+    const size_t at = part_row(a, MODE, first, z % a.N, head), stride = part_row(a, MODE, 1, 0, 0);  // its first partial; to the next one
+    const float *ml = a.part_ml + at * 2;
+    float M = -INFINITY, den = 0.0f;
+    for (int s = l; s < parts; s += width) M = fmaxf(M, ml[2 * s * stride]);
+    for (int off = 1; off < width; off <<= 1) M = fmaxf(M, __shfl_xor(M, off, kWave));
+    for (int s = l; s < parts; s += width) {
         const float m = ml[2 * s * stride], wt = m == -INFINITY ? 0.0f : expf(m - M);
-        if (w == 0) sm_w[s] = wt;
+        sm_w[grp][s] = wt;
         den = fmaf(wt, ml[2 * s * stride + 1], den);
     }
-    den = wave_all(den, AddOp());
-    __syncthreads();
-    const float *po = a.part_o + row * d;
-    for (int j = lane; j < d; j += kWave) {
-        float acc = 0.0f;
-#pragma unroll 4
-        for (int s = w; s < parts; s += 4) acc = fmaf(sm_w[s], po[s * stride * d + j], acc);
-        sm_o[w][j] = acc;
+    for (int off = 1; off < width; off <<= 1) den += __shfl_xor(den, off, kWave);
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");  // (a group is part of a wavefront)
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    const float *po = a.part_o + at * a.d_h + (col < a.d_h ? col : 0);
+    const int step = share ? groups : 1;
+    vec_t acc = vec_t(0.0f);
+    for (int s1 = share ? grp : 0; s1 < parts; s1 += BATCH * step) {
+        vec_t v[BATCH];
+#pragma unroll
+        for (int u = 0; u < BATCH; ++u) {
+            const int s = s1 + u * step < parts ? s1 + u * step : parts - 1;
+            v[u] = *reinterpret_cast<const vec_t *>(po + (size_t)s * stride * a.d_h);
+        }
+#pragma unroll
+        for (int u = 0; u < BATCH; ++u) {
+            const int s = s1 + u * step;
+            acc += (s < parts ? sm_w[grp][s] : 0.0f) * v[u];
+        }
     }
-    __syncthreads();
-    const int j = threadIdx.x;
-    if (j < d) {
-        const float num = (sm_o[0][j] + sm_o[1][j]) + (sm_o[2][j] + sm_o[3][j]);
-        ((T *)a.out)[((size_t)z * a.H_q + head) * d + j] = from_f32<T>(den > 0.0f ? num / den : 0.0f);  // (a query that sees nothing: zeros)
+    if (share) {
+        sm[threadIdx.x] = acc;
+        __syncthreads();
+        if (grp > 0) return;
+        for (int k = 1; k < groups; ++k) acc += sm[(k << lg) + l];
     }
+    if (item >= rows || col >= a.d_h) return;
+    T *out = (T *)a.out + (size_t)row * a.d_h + col;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) out[e] = from_f32<T>(den > 0.0f ? acc[e] / den : 0.0f);  // (a query that sees nothing: zeros)
 }
 
 // ------------------------------------------------------------------------------------------
@@ -653,12 +776,17 @@ hipError_t launch_mode(const xkv_shape &s, const CacheArgs &a, hipStream_t st)
     hipError_t e = a.mfma && bits % 16 == 0 ? launch_mfma<MODE>(a, st)
                  : s.dtype == XKV_F32 ? launch_general<MODE, float>(gen, st) : launch_general<MODE, bf16_t>(gen, st);
     if (e != hipSuccess) return e;
-    const dim3 grid(a.H_q, a.batch * a.N);
-    if (s.dtype == XKV_F32)
-        hipLaunchKernelGGL((cache_merge_kernel<float, MODE>), grid, dim3(256), 0, st, a);
-    else
-        hipLaunchKernelGGL((cache_merge_kernel<bf16_t, MODE>), grid, dim3(256), 0, st, a);
-    return hipGetLastError();
+    const int vec = a.d_h % 4 == 0 ? 4 : 1, rows = a.batch * a.N * a.H_q;
+    int lg = 3;
+    while (lg < 6 && (vec << lg) < a.d_h) ++lg;
+    const int share = rows < 2048, groups = 256 >> lg;
+    const dim3 grid(share ? rows : (rows + groups - 1) / groups, (a.d_h + (vec << lg) - 1) / (vec << lg));
+    auto merge = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a, lg, share, rows);
+        return hipGetLastError();
+    };
+    if (s.dtype == XKV_F32) return vec == 4 ? merge(cache_merge_kernel<float, MODE, 4>) : merge(cache_merge_kernel<float, MODE, 1>);
+    return vec == 4 ? merge(cache_merge_kernel<bf16_t, MODE, 4>) : merge(cache_merge_kernel<bf16_t, MODE, 1>);
 }
 
 }  // namespace

@@ -45,5 +45,15 @@ __device__ __forceinline__ bf16x8_t pack8(const f32x16_t &c, int j)
     return __builtin_convertvector(x, bf16x8_t);
 }
 
+// sum + the eight weights as they enter the products (rounded): what divides the result is then the sum of what multiplied the values.
+__device__ __forceinline__ float add_pairs(const bf16x8_t &p, float sum)
+{
+    typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+    const bf16x2_t ones = {(__bf16)1.0f, (__bf16)1.0f};
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) sum = __builtin_amdgcn_fdot2_f32_bf16(bf16x2_t{p[e], p[e + 1]}, ones, sum, false);
+    return sum;
+}
+
 }  // namespace cache_tile
 }  // namespace xkv
