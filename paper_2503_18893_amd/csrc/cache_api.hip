@@ -52,13 +52,13 @@ xkv_status plan_cache_attend(const xkv_shape &s, CacheMode mode, int N, int c, C
         p.sel_shape = xkv_shape{1, s.H_kv, s.H_kv, 1, 1, 1, p.n_c, p.k_ch, (int32_t)(batch * N), XKV_F32, 1.0f};
         off = plan_selection(p, off);
     }
-    // The matrix-core kernel: as many rows per workgroup as there are, up to 128, and two workgroups (one, with up to 32 rows) to a
-    // compute unit.  The general one: 16 rows, rounds of 64 tokens, four workgroups.
+    // The matrix-core kernel: as many rows per workgroup as there are, up to 256 (128 where that leaves fewer of them empty), one workgroup
+    // to a compute unit (two of 128 rows).  The general one: 16 rows, rounds of 64 tokens, four workgroups.
     const int M = mode == CacheMode::blocks ? p.n_rep : N * p.n_rep;
     p.mfma = s.dtype == XKV_BF16 && s.d_h == 128;
-    p.rows = !p.mfma ? 16 : mode != CacheMode::tree || M <= 32 ? 32 : M <= 64 ? 64 : 128;
-    p.round = p.mfma && p.rows == 32 ? 128 : 64;
-    const int want = !p.mfma ? 1024 : p.rows == 32 ? 256 : 512;
+    p.rows = !p.mfma ? 16 : mode != CacheMode::tree || M <= 32 ? 32 : M <= 64 ? 64 : (ceil_div(M, 128) & 1) ? 128 : 256;
+    p.round = p.mfma && p.rows <= 64 ? 128 : 64;
+    const int want = !p.mfma ? 1024 : p.rows == 128 ? 512 : 256;
     const long long tiles = (long long)s.H_kv * ceil_div(M, p.rows);
     const int longest = ceil_div(most, p.round);  // parts that the longest sequence can have
     if (mode == CacheMode::blocks) {

@@ -205,25 +205,27 @@ __global__ __launch_bounds__(256) void cache_attend_general_kernel(CacheArgs a)
 // P^T is the second product's operand as it comes.  V^T is read from its tile by the transposing LDS read.
 // The maximum m is only raised when a row's logits outgrow it by a factor of 2^8: until then weights reach 2^8, sums stay exact to
 // single precision, and the accumulators need not be rescaled.
-// LDS: row t of a tile is 256 B; its 16-byte piece p of K sits at (p + t) % 16, its 32-byte piece u of V at (u + t) % 8, so that
-// neither the fragment reads (32 rows, one piece each) nor the transposing reads (8 rows, 64 B each) meet in a bank.
+// LDS: row t of a tile is 256 B; its 16-byte piece p of K sits at (p + t) % 16, its 32-byte piece u of V at (u + 2 t) % 8, so
+// that neither the fragment reads (16 rows at a time, one piece each) nor the transposing reads (4 rows at a time, two pieces each)
+// meet in a bank.
 // ------------------------------------------------------------------------------------------
 __device__ const u32x4_t kZeroRow[16] = {};  // stands for drafted tokens that nothing sees, and for places behind the last token
 
-template <CacheMode MODE, int WR, int WT, int SUB>
-__global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(CacheArgs a)
+template <CacheMode MODE, int WR, int WT, int SUB, int RT>
+__global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_attend_mfma_kernel(CacheArgs a)
 {
     constexpr bool OWN = WR == 1;  // tiles that only one wavefront reads
     constexpr int WAVES = WR * WT, TILE = 32 * SUB * WT, STAGE = 512 * TILE, RPW = TILE / WAVES, LOADS = RPW / 4, KTILE = OWN ? 8192 : 256 * TILE, VBASE = OWN ? KTILE : 2 * KTILE;
     static_assert(!OWN || SUB == 1, "a wavefront's tile is 32 tokens");
-    static_assert(RPW % 16 == 0 && 2 * STAGE >= WAVES * 16384, "rotations by i; room for the merge");
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE];
-    __shared__ float sm_m[WT][32 * WR], sm_l[WT][32 * WR];
+    static_assert(RPW % 8 == 0 && (WR > 4 || 2 * STAGE >= WAVES * 16384), "rotations by i; room for the merge");
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE >= WAVES * 16384 ? 2 * STAGE : WAVES * 16384];
+    __shared__ float sm_m[WT][32 * WR * RT], sm_l[WT][32 * WR * RT];
     __shared__ uint32_t sm_seen[32];
+    __shared__ __attribute__((aligned(16))) float sm_z[MODE == CacheMode::weights ? WAVES : 1][MODE == CacheMode::weights ? 16 : 1][36];  // logits of a tile
     __shared__ int sm_rows[MODE == CacheMode::blocks ? kPartBlocks + 2 : 1];  // blocks: first rows of this part's blocks
     const int lane = lane_id(), w = wave_id(), rg = w % WR, tg = w / WR, n32 = lane & 31, hf = lane >> 5, n_rep = a.H_q / a.H_kv;
     const int M = MODE == CacheMode::blocks ? n_rep : a.N * n_rep;
-    const CacheUnit u = cache_unit(a, MODE, (M + 32 * WR - 1) / (32 * WR));
+    const CacheUnit u = cache_unit(a, MODE, (M + 32 * WR * RT - 1) / (32 * WR * RT));
     if (!u.some) return;  // (the merge knows)
     const int tile = u.tile, g = u.g, n = u.n, t_begin = u.t_begin, t_end = u.t_end;
     const int seq = MODE == CacheMode::blocks ? u.seq / a.N : u.seq, first_token = MODE == CacheMode::blocks ? u.seq % a.N : 0;
@@ -234,12 +236,18 @@ __global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(Cach
     const bf16_t *Vd = (const bf16_t *)a.V_draft + ((size_t)seq * a.H_kv + g) * a.N * 128;
 
     // Q^T fragments: lane (row n32, hf), fragment f, position e: channel 16 f + 8 hf + e
-    const int m_row = (tile * WR + rg) * 32 + n32, m_in = m_row < M ? m_row : M - 1;
-    const int token = first_token + m_in / n_rep;
-    const size_t q_row = ((size_t)seq * a.N + token) * a.H_q + g * n_rep + m_in % n_rep;
-    bf16x8_t Qf[8];
+    int m_row[RT], token[RT];
+    bf16x8_t Qf[RT][8];
 #pragma unroll
-    for (int f = 0; f < 8; ++f) Qf[f] = __builtin_bit_cast(bf16x8_t, reinterpret_cast<const u32x4_t *>((const bf16_t *)a.q + q_row * 128)[2 * f + hf]);
+    for (int rt = 0; rt < RT; ++rt) {
+        m_row[rt] = ((tile * WR + rg) * RT + rt) * 32 + n32;
+        const int m_in = m_row[rt] < M ? m_row[rt] : M - 1;
+        token[rt] = first_token + m_in / n_rep;
+        const size_t q_row = ((size_t)seq * a.N + token[rt]) * a.H_q + g * n_rep + m_in % n_rep;
+#pragma unroll
+        for (int f = 0; f < 8; ++f)
+            Qf[rt][f] = __builtin_bit_cast(bf16x8_t, reinterpret_cast<const u32x4_t *>((const bf16_t *)a.q + q_row * 128)[2 * f + hf]);
+    }
 
     if (MODE == CacheMode::tree && t_end > n) {  // which drafted tokens any token sees
         if (threadIdx.x < 32) sm_seen[threadIdx.x] = a.tree ? 0u : 0xFFFFFFFFu;
@@ -275,11 +283,10 @@ __global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(Cach
     // Where this wavefront puts rows: its share of a tile that all read (WR > 1), or tiles of 32 rows of its own.
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem + (OWN ? 32768 * w : 256 * RPW * w);
     const int r4 = lane >> 4, x16 = lane & 15;
-    uint32_t koff[4], voff[2];
+    uint32_t koff[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) koff[i] = 256 * r4 + 16 * ((x16 - 4 * i - r4) & 15);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) voff[i] = 256 * r4 + 32 * (((x16 >> 1) - 4 * i - r4) & 7) + 16 * (x16 & 1);
+    for (int i = 0; i < 4; ++i) koff[i] = 256 * r4 + 16 * ((x16 - (OWN ? 0 : RPW * w) - 4 * i - r4) & 15);
+    const uint32_t voff = 256 * r4 + 32 * (((x16 >> 1) - 2 * r4) & 7) + 16 * (x16 & 1);
     const int plain_end = MODE == CacheMode::tree && n < t_end ? n : t_end;  // rows of the cache end here
     auto stage_plain = [&](int first, int buf, auto values) __attribute__((always_inline)) {  // RPW rows of the cache
         constexpr bool is_v = decltype(values)::value;
@@ -288,9 +295,9 @@ __global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(Cach
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             if (OWN)
-                copy16_to_lds_once(base + 1024 * i, is_v ? voff[i & 1] : koff[i & 3], at + 1024 * i);
+                copy16_to_lds_once(base + 1024 * i, is_v ? voff : koff[i & 3], at + 1024 * i);
             else
-                copy16_to_lds(base + 1024 * i, is_v ? voff[i & 1] : koff[i & 3], at + 1024 * i);
+                copy16_to_lds(base + 1024 * i, is_v ? voff : koff[i & 3], at + 1024 * i);
         }
     };
     auto stage = [&](int first, int buf, auto values) __attribute__((always_inline)) {  // RPW tokens from `first` on
@@ -313,7 +320,7 @@ __global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(Cach
             }
 #pragma unroll
             for (int i = 0; i < LOADS; ++i)
-                copy16_global_to_lds((const unsigned char *)(rows + (size_t)rows_of[i] * 128) + ((is_v ? voff[i & 1] : koff[i & 3]) - 256 * r4),
+                copy16_global_to_lds((const unsigned char *)(rows + (size_t)rows_of[i] * 128) + ((is_v ? voff : koff[i & 3]) - 256 * r4),
                                      at + 1024 * i);
             return;
         }
@@ -333,7 +340,7 @@ __global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(Cach
                 t = t < t_end ? t : t_end - 1;  // (its weight will be zero)
                 from = rows + (size_t)t * 128;
             }
-            copy16_global_to_lds((const unsigned char *)from + ((is_v ? voff[i & 1] : koff[i & 3]) - 256 * r4), at + 1024 * i);
+            copy16_global_to_lds((const unsigned char *)from + ((is_v ? voff : koff[i & 3]) - 256 * r4), at + 1024 * i);
         }
     };
     constexpr std::false_type keys{};
@@ -349,99 +356,124 @@ __global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(Cach
         const int rl = 4 * hf + ((lane & 15) >> 2);
 #pragma unroll
         for (int db = 0; db < 4; ++db)
-            vat[db] = VBASE + 256 * (32 * SUB * TG * tg + rl) + 32 * ((2 * db + ((lane >> 4) & 1) + rl) & 7) + 8 * (lane & 3);
+            vat[db] = VBASE + 256 * (32 * SUB * TG * tg + rl) + 32 * ((2 * db + ((lane >> 4) & 1) + 2 * rl) & 7) + 8 * (lane & 3);
     }
 
-    f32x16_t O[4];
+    // Row tile rt, part s of a tile of tokens: S[rt SUB + s]; its weights as operands: P[2 (rt SUB + s)] and the next one.
+    constexpr int PARTS = RT * SUB;
+    f32x16_t O[RT][4];
+    float m_run[RT], l_run[RT];
 #pragma unroll
-    for (int db = 0; db < 4; ++db) O[db] = f32x16_t(0.0f);
-    float m_run = -INFINITY, l_run = 0.0f;
+    for (int rt = 0; rt < RT; ++rt) {
+        m_run[rt] = -INFINITY;
+        l_run[rt] = 0.0f;
+#pragma unroll
+        for (int db = 0; db < 4; ++db) O[rt][db] = f32x16_t(0.0f);
+    }
     // logits of a tile of keys
-    auto logits = [&](const unsigned char *lds, f32x16_t (&S)[SUB]) __attribute__((always_inline)) {
+    auto logits = [&](const unsigned char *lds, f32x16_t (&S)[PARTS]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int s = 0; s < SUB; ++s) S[s] = f32x16_t(0.0f);
+        for (int s = 0; s < PARTS; ++s) S[s] = f32x16_t(0.0f);
 #pragma unroll
         for (int f = 0; f < 8; ++f)
 #pragma unroll
             for (int s = 0; s < SUB; ++s) {
                 const u32x4_t kf = *reinterpret_cast<const u32x4_t *>(lds + kat[f] + 8192 * s);
-                S[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf), Qf[f], S[s], 0, 0, 0);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+                    S[rt * SUB + s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf), Qf[rt][f], S[rt * SUB + s], 0, 0, 0);
             }
     };
     // register v of part s is token tw + 32 s + 8 (v / 4) + 4 hf + v % 4: what this row does not see; then the logits that are kept
-    auto hide = [&](int tw, f32x16_t (&S)[SUB]) __attribute__((always_inline)) {
+    auto hide = [&](int tw, f32x16_t (&S)[PARTS]) __attribute__((always_inline)) {
         if (tw + 32 * SUB > plain_end) {
 #pragma unroll
-            for (int s = 0; s < SUB; ++s) {
-                const int t = tw + 32 * s, left = t_end - t;
+            for (int p = 0; p < PARTS; ++p) {
+                const int t = tw + 32 * (p % SUB), left = t_end - t;
                 uint32_t sees = left >= 32 ? 0xFFFFFFFFu : left > 0 ? (1u << left) - 1u : 0u;
-                if (MODE == CacheMode::tree) sees &= draft_bits(a, seq, token, t - n);
+                if (MODE == CacheMode::tree) sees &= draft_bits(a, seq, token[p / SUB], t - n);
                 sees >>= 4 * hf;
 #pragma unroll
-                for (int v = 0; v < 16; ++v) S[s][v] = sees >> (8 * (v / 4) + v % 4) & 1u ? S[s][v] : -INFINITY;
+                for (int v = 0; v < 16; ++v) S[p][v] = sees >> (8 * (v / 4) + v % 4) & 1u ? S[p][v] : -INFINITY;
             }
         }
-        if (MODE == CacheMode::weights && m_row < M) {
-            float *to = a.logits + q_row * a.L + tw + 4 * hf;
+        if constexpr (MODE == CacheMode::weights) {  // through LDS: a head's 32 logits leave as one line
+            static_assert(PARTS == 1 && OWN, "one tile of up to 16 rows per wavefront");
+            if (n32 < n_rep) {
+#pragma unroll
+                for (int v = 0; v < 16; v += 4)
+                    *reinterpret_cast<f32x4_t *>(&sm_z[w][n32][2 * v + 4 * hf]) =
+                        f32x4_t{a.scale * S[0][v], a.scale * S[0][v + 1], a.scale * S[0][v + 2], a.scale * S[0][v + 3]};
+            }
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            float *to = a.logits + ((size_t)seq * a.H_q + g * n_rep) * a.L + tw + n32;
+            for (int h = hf; h < n_rep; h += 2)
+                if (tw + n32 < t_end) to[(size_t)h * a.L] = sm_z[w][h][n32];
+            __builtin_amdgcn_wave_barrier();
+        }
+    };
+    auto top_of = [&](const f32x16_t (&S)[PARTS], float (&m_loc)[RT]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            float m = S[rt * SUB][0], lo, hi;
 #pragma unroll
             for (int s = 0; s < SUB; ++s)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    const int t = 32 * s + 8 * (v / 4) + v % 4;
-                    if (tw + t + 4 * hf < t_end) to[t] = a.scale * S[s][v];
-                }
+                for (int v = 0; v < 16; ++v) m = fmaxf(m, S[rt * SUB + s][v]);
+            halves(m, lo, hi);
+            m_loc[rt] = fmaxf(lo, hi);
         }
     };
-    auto top_of = [&](const f32x16_t (&S)[SUB]) __attribute__((always_inline)) {
-        float m = S[0][0];
+    auto raise = [&](const float (&m_loc)[RT]) __attribute__((always_inline)) {
+        bool any = false;
 #pragma unroll
-        for (int s = 0; s < SUB; ++s)
+        for (int rt = 0; rt < RT; ++rt) any |= (m_loc[rt] - m_run[rt]) * c > 8.0f;
+        if (__ballot(any)) {
 #pragma unroll
-            for (int v = 0; v < 16; ++v) m = fmaxf(m, S[s][v]);
-        float lo, hi;
-        halves(m, lo, hi);
-        return fmaxf(lo, hi);
-    };
-    auto raise = [&](float m_loc) __attribute__((always_inline)) {
-        if (__ballot((m_loc - m_run) * c > 8.0f)) {
-            const float m_new = fmaxf(m_run, m_loc), alpha = m_run == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m_run - m_new) * c);
-            l_run *= alpha;
+            for (int rt = 0; rt < RT; ++rt) {
+                const float m_new = fmaxf(m_run[rt], m_loc[rt]), alpha = m_run[rt] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m_run[rt] - m_new) * c);
+                l_run[rt] *= alpha;
 #pragma unroll
-            for (int db = 0; db < 4; ++db)
+                for (int db = 0; db < 4; ++db)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) O[db][v] *= alpha;
-            m_run = m_new;
+                    for (int v = 0; v < 16; ++v) O[rt][db][v] *= alpha;
+                m_run[rt] = m_new;
+            }
         }
     };
-    auto weigh = [&](f32x16_t (&S)[SUB], bf16x8_t (&P)[2 * SUB]) __attribute__((always_inline)) {
-        const float less = m_run == -INFINITY ? 0.0f : -m_run * c;
+    auto weigh = [&](f32x16_t (&S)[PARTS], bf16x8_t (&P)[2 * PARTS]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int s = 0; s < SUB; ++s)
+        for (int p = 0; p < PARTS; ++p) {
+            const int rt = p / SUB;
+            const float less = m_run[rt] == -INFINITY ? 0.0f : -m_run[rt] * c;
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
 #pragma unroll
                 for (int v = 8 * j; v < 8 * j + 8; ++v) {
-                    S[s][v] = __builtin_amdgcn_exp2f(fmaf(S[s][v], c, less));
-                    if (OWN) l_run += S[s][v];  // (the weights that are given out are divided by this sum: in single precision)
+                    S[p][v] = __builtin_amdgcn_exp2f(fmaf(S[p][v], c, less));
+                    if (OWN) l_run[rt] += S[p][v];  // (the weights that are given out are divided by this sum: in single precision)
                 }
-                P[2 * s + j] = pack8(S[s], j);
-                if (!OWN) l_run = add_pairs(P[2 * s + j], l_run);
+                P[2 * p + j] = pack8(S[p], j);
+                if (!OWN) l_run[rt] = add_pairs(P[2 * p + j], l_run[rt]);
             }
+        }
     };
-    auto add_values = [&](const unsigned char *lds, const bf16x8_t (&P)[2 * SUB]) __attribute__((always_inline)) {
+    auto add_values = [&](const unsigned char *lds, const bf16x8_t (&P)[2 * PARTS]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int s = 0; s < SUB; ++s)
+        for (int sj = 0; sj < 2 * SUB; ++sj)
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+            for (int db = 0; db < 4; ++db) {
+                // position e of lane (channel, hf): token 16 sj + 8 (e / 4) + 4 hf + e % 4, as in P
+                const unsigned char *from = lds + vat[db] + 4096 * sj;
+                const s16x4_t a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)from);
+                const s16x4_t a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(from + 2048));
 #pragma unroll
-                for (int db = 0; db < 4; ++db) {
-                    // position e of lane (channel, hf): token 16 j + 8 (e / 4) + 4 hf + e % 4, as in P
-                    const unsigned char *from = lds + vat[db] + 8192 * s + 4096 * j;
-                    const s16x4_t a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)from);
-                    const s16x4_t a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(from + 2048));
-                    O[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                        __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7)), P[2 * s + j], O[db], 0, 0, 0);
-                }
+                for (int rt = 0; rt < RT; ++rt)
+                    O[rt][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                        __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7)), P[2 * SUB * rt + sj], O[rt][db], 0, 0, 0);
+            }
     };
     if constexpr (OWN) {
         // A wavefront keeps two tiles of its own and waits for nobody: the keys of the tile after the next are requested as soon as the
@@ -465,15 +497,17 @@ __global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(Cach
             else
                 XKV_WAIT_VMCNT(LOADS);
             asm volatile("" : : : "memory");
-            f32x16_t S[SUB];
-            bf16x8_t P[2 * SUB];
+            f32x16_t S[PARTS];
+            bf16x8_t P[2 * PARTS];
             logits(lds, S);
             if (then) {
                 wait_lds();
                 stage(t + 2 * TILE, buf, keys);
             }
             hide(t, S);
-            raise(top_of(S));
+            float m_loc[RT];
+            top_of(S, m_loc);
+            raise(m_loc);
             weigh(S, P);
             if (then)
                 XKV_WAIT_VMCNT(3 * LOADS);
@@ -500,76 +534,86 @@ __global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(Cach
         else
             XKV_WAIT_VMCNT(LOADS);
         __syncthreads();
-        f32x16_t S[SUB];
+        f32x16_t S[PARTS];
+        float m_loc[RT];
         logits(lds_w, S);
         hide(t_begin + 32 * SUB * tg, S);
-        float m_loc = top_of(S);
-        auto step = [&](int t0, auto which, f32x16_t (&S)[SUB], f32x16_t (&S1)[SUB]) __attribute__((always_inline)) {
-            constexpr int BUF = decltype(which)::value;
+        top_of(S, m_loc);
+        auto step = [&](int t0, auto which, f32x16_t (&S)[PARTS], f32x16_t (&S1)[PARTS]) __attribute__((always_inline)) {
+            constexpr int BUF = decltype(which)::value, READS = 8 * SUB, STEPS = READS * RT, AHEAD = 3;
             XKV_WAIT_VMCNT(0);
             __syncthreads();
             stage_plain(t0 + 2 * TILE + RPW * w, BUF, keys);
             stage_plain(t0 + TILE + RPW * w, BUF ^ 1, values);
             raise(m_loc);
             const unsigned char *kt = lds_w + (BUF ^ 1) * KTILE, *vt = lds_w + BUF * KTILE;
-            constexpr int STEPS = 8 * SUB, AHEAD = 3;
-            bf16x8_t P[2 * SUB];
+            bf16x8_t P[2 * PARTS];
             // each product with the keys beside two exponentials
-            u32x4_t kf[STEPS];
-            auto read_key = [&](int i) __attribute__((always_inline)) {
-                kf[i] = *reinterpret_cast<const u32x4_t *>(kt + kat[i / SUB] + 8192 * (i % SUB));
+            u32x4_t kf[READS];
+            auto read_key = [&](int k) __attribute__((always_inline)) {
+                kf[k] = *reinterpret_cast<const u32x4_t *>(kt + kat[k / SUB] + 8192 * (k % SUB));
             };
 #pragma unroll
-            for (int i = 0; i < AHEAD; ++i) read_key(i);
-            const float less = m_run == -INFINITY ? 0.0f : -m_run * c;
+            for (int k = 0; k < AHEAD; ++k) read_key(k);
+            float less[RT];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) less[rt] = m_run[rt] == -INFINITY ? 0.0f : -m_run[rt] * c;
 #pragma unroll
             for (int i = 0; i < STEPS; ++i) {
-                if (i + AHEAD < STEPS) read_key(i + AHEAD);
-                if (i < SUB) S1[i % SUB] = f32x16_t(0.0f);
-                S1[i % SUB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[i]), Qf[i / SUB], S1[i % SUB], 0, 0, 0);
+                const int k = i / RT, rt = i % RT, p = rt * SUB + k % SUB;
+                if (rt == 0 && k + AHEAD < READS) read_key(k + AHEAD);
+                if (k < SUB) S1[p] = f32x16_t(0.0f);
+                S1[p] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[k]), Qf[rt][k / SUB], S1[p], 0, 0, 0);
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
                     const int v = 2 * i + x;
-                    S[v / 16][v % 16] = __builtin_amdgcn_exp2f(fmaf(S[v / 16][v % 16], c, less));
+                    S[v / 16][v % 16] = __builtin_amdgcn_exp2f(fmaf(S[v / 16][v % 16], c, less[v / 16 / SUB]));
                 }
                 if (i % 4 == 3) {
                     P[i / 4] = pack8(S[i / 8], i / 4 % 2);
-                    l_run = add_pairs(P[i / 4], l_run);
+                    l_run[i / 8 / SUB] = add_pairs(P[i / 4], l_run[i / 8 / SUB]);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
             // each product with the values beside its share of the next maximum
-            s16x4_t vf[STEPS][2];
-            auto read_values = [&](int i) __attribute__((always_inline)) {
-                const unsigned char *from = vt + vat[i % 4] + 4096 * (i / 4);
-                vf[i][0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)from);
-                vf[i][1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(from + 2048));
+            s16x4_t vf[READS][2];
+            auto read_values = [&](int k) __attribute__((always_inline)) {
+                const unsigned char *from = vt + vat[k % 4] + 4096 * (k / 4);
+                vf[k][0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)from);
+                vf[k][1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(from + 2048));
             };
 #pragma unroll
-            for (int i = 0; i < AHEAD; ++i) read_values(i);
-            float m_next[2] = {-INFINITY, -INFINITY};
+            for (int k = 0; k < AHEAD; ++k) read_values(k);
+            float m_next[2 * RT];
+#pragma unroll
+            for (int i = 0; i < 2 * RT; ++i) m_next[i] = -INFINITY;
 #pragma unroll
             for (int i = 0; i < STEPS; ++i) {
-                if (i + AHEAD < STEPS) read_values(i + AHEAD);
-                O[i % 4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                    __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(vf[i][0], vf[i][1], 0, 1, 2, 3, 4, 5, 6, 7)), P[i / 4], O[i % 4], 0, 0, 0);
+                const int k = i / RT, rt = i % RT;
+                if (rt == 0 && k + AHEAD < READS) read_values(k + AHEAD);
+                O[rt][k % 4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                    __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(vf[k][0], vf[k][1], 0, 1, 2, 3, 4, 5, 6, 7)), P[2 * SUB * rt + k / 4],
+                    O[rt][k % 4], 0, 0, 0);
                 if (i >= STEPS / 2) {
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
-                        const int v = 4 * (i - STEPS / 2) + x;
-                        m_next[x >> 1] = fmaxf(m_next[x >> 1], S1[v / 16][v % 16]);
+                        const int v = 4 * (i - STEPS / 2) + x, m = 2 * (v / 16 / SUB) + (x >> 1);
+                        m_next[m] = fmaxf(m_next[m], S1[v / 16][v % 16]);
+                        if (x & 1) asm volatile("" : "+v"(m_next[m]));  // (here, not at the end)
                     }
-                    asm volatile("" : "+v"(m_next[0]), "+v"(m_next[1]));  // (here, not at the end)
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
-            float lo, hi;
-            halves(fmaxf(m_next[0], m_next[1]), lo, hi);
-            m_loc = fmaxf(lo, hi);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                float lo, hi;
+                halves(fmaxf(m_next[2 * rt], m_next[2 * rt + 1]), lo, hi);
+                m_loc[rt] = fmaxf(lo, hi);
+            }
         };
         int buf = 0, t0 = t_begin;
         for (; t0 + 4 * TILE <= plain_end; t0 += 2 * TILE) {  // the next three tiles are whole
-            f32x16_t S1[SUB];
+            f32x16_t S1[PARTS];
             step(t0, std::integral_constant<int, 0>{}, S, S1);
             step(t0 + TILE, std::integral_constant<int, 1>{}, S1, S);
         }
@@ -579,58 +623,65 @@ __global__ __launch_bounds__(64 * WR * WT, 2) void cache_attend_mfma_kernel(Cach
             if (t0 + 2 * TILE < t_end) stage(t0 + 2 * TILE + RPW * w, buf, keys);
             if (t0 + TILE < t_end) stage(t0 + TILE + RPW * w, buf ^ 1, values);
             raise(m_loc);
-            f32x16_t S1[SUB];
-            bf16x8_t P[2 * SUB];
+            f32x16_t S1[PARTS];
+            bf16x8_t P[2 * PARTS];
             logits(lds_w + (buf ^ 1) * KTILE, S1);  // (behind the last tile: of whatever is there, not used)
             weigh(S, P);
             if (t0 + TILE < t_end) hide(t0 + TILE + 32 * SUB * tg, S1);
             add_values(lds_w + buf * KTILE, P);
-            m_loc = top_of(S1);
+            top_of(S1, m_loc);
 #pragma unroll
-            for (int s = 0; s < SUB; ++s) S[s] = S1[s];
+            for (int s = 0; s < PARTS; ++s) S[s] = S1[s];
         }
     }
 
-    // merge the token groups through LDS, where rows come together as well: 16-byte piece p of row n32 sits at (p + n32) % 32
-    {
+    // merge the token groups through LDS, where rows come together as well, a row tile of every row group at a time: 16-byte piece p of
+    // row n32 sits at (p + n32) % 32
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
         float lo, hi;
-        halves(l_run, lo, hi);
+        halves(l_run[rt], lo, hi);
         if (hf == 0) {
-            sm_m[tg][32 * rg + n32] = m_run;
-            sm_l[tg][32 * rg + n32] = lo + hi;
+            sm_m[tg][32 * (rg * RT + rt) + n32] = m_run[rt];
+            sm_l[tg][32 * (rg * RT + rt) + n32] = lo + hi;
         }
     }
     __syncthreads();
-    float M_all = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < WT; ++i) M_all = fmaxf(M_all, sm_m[i][32 * rg + n32]);
-    const float f = m_run == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m_run - M_all) * c);
-    f32x4_t *ot = reinterpret_cast<f32x4_t *>(smem) + 1024 * w;
+    for (int rt = 0; rt < RT; ++rt) {
+        float M_all = -INFINITY;
 #pragma unroll
-    for (int db = 0; db < 4; ++db)
+        for (int i = 0; i < WT; ++i) M_all = fmaxf(M_all, sm_m[i][32 * (rg * RT + rt) + n32]);
+        const float f = m_run[rt] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m_run[rt] - M_all) * c);
+        f32x4_t *ot = reinterpret_cast<f32x4_t *>(smem) + 1024 * w;
 #pragma unroll
-        for (int v = 0; v < 16; v += 4) {
-            const f32x4_t x = {f * O[db][v], f * O[db][v + 1], f * O[db][v + 2], f * O[db][v + 3]};
-            ot[32 * n32 + ((8 * db + v / 2 + hf + n32) & 31)] = x;
+        for (int db = 0; db < 4; ++db)
+#pragma unroll
+            for (int v = 0; v < 16; v += 4)
+                ot[32 * n32 + ((8 * db + v / 2 + hf + n32) & 31)] =
+                    f32x4_t{f * O[rt][db][v], f * O[rt][db][v + 1], f * O[rt][db][v + 2], f * O[rt][db][v + 3]};
+        __syncthreads();
+        for (int item = threadIdx.x; item < WR * 1024; item += 64 * WAVES) {
+            const int row = item >> 5, p = item & 31, in_wg = 32 * ((row >> 5) * RT + rt) + (row & 31), m = tile * WR * RT * 32 + in_wg;
+            if (m >= M) continue;
+            f32x4_t x = f32x4_t(0.0f);
+#pragma unroll
+            for (int i = 0; i < WT; ++i)
+                x += reinterpret_cast<const f32x4_t *>(smem)[1024 * (i * WR + (row >> 5)) + 32 * (row & 31) + ((p + row) & 31)];
+            const size_t slot = part_row(a, MODE, u.part, m / n_rep, g * n_rep + m % n_rep);
+            *reinterpret_cast<f32x4_t *>(a.part_o + slot * 128 + 4 * p) = x;
+            if (p == 0) {
+                float top = -INFINITY, den = 0.0f;
+#pragma unroll
+                for (int i = 0; i < WT; ++i) top = fmaxf(top, sm_m[i][in_wg]);
+#pragma unroll
+                for (int i = 0; i < WT; ++i)
+                    den += sm_m[i][in_wg] == -INFINITY ? 0.0f : sm_l[i][in_wg] * __builtin_amdgcn_exp2f((sm_m[i][in_wg] - top) * c);
+                a.part_ml[2 * slot] = top * a.scale;
+                a.part_ml[2 * slot + 1] = den;
+            }
         }
-    __syncthreads();
-    for (int item = threadIdx.x; item < WR * 1024; item += 64 * WAVES) {
-        const int row = item >> 5, p = item & 31, m = tile * WR * 32 + row;
-        if (m >= M) continue;
-        f32x4_t x = f32x4_t(0.0f);
-#pragma unroll
-        for (int i = 0; i < WT; ++i) x += reinterpret_cast<const f32x4_t *>(smem)[1024 * (i * WR + (row >> 5)) + 32 * (row & 31) + ((p + row) & 31)];
-        const size_t slot = part_row(a, MODE, u.part, m / n_rep, g * n_rep + m % n_rep);
-        *reinterpret_cast<f32x4_t *>(a.part_o + slot * 128 + 4 * p) = x;
-        if (p == 0) {
-            float top = -INFINITY, den = 0.0f;
-#pragma unroll
-            for (int i = 0; i < WT; ++i) top = fmaxf(top, sm_m[i][row]);
-#pragma unroll
-            for (int i = 0; i < WT; ++i) den += sm_m[i][row] == -INFINITY ? 0.0f : sm_l[i][row] * __builtin_amdgcn_exp2f((sm_m[i][row] - top) * c);
-            a.part_ml[2 * slot] = top * a.scale;
-            a.part_ml[2 * slot + 1] = den;
-        }
+        if (rt + 1 < RT) __syncthreads();
     }
 }
 
@@ -758,12 +809,15 @@ hipError_t launch_mfma(const CacheArgs &a, hipStream_t st)
 {
     const int M = MODE == CacheMode::blocks ? a.H_q / a.H_kv : a.N * (a.H_q / a.H_kv);
     const dim3 grid = unit_grid(a, MODE, M);
-    if (MODE == CacheMode::tree && a.rows == 128)
-        hipLaunchKernelGGL((cache_attend_mfma_kernel<CacheMode::tree, 4, 1, 2>), grid, dim3(256), 0, st, a);
+    auto launch = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, st, a); };
+    if (MODE == CacheMode::tree && a.rows == 256)
+        launch(cache_attend_mfma_kernel<CacheMode::tree, 8, 1, 2, 1>, 512);
+    else if (MODE == CacheMode::tree && a.rows == 128)
+        launch(cache_attend_mfma_kernel<CacheMode::tree, 4, 1, 2, 1>, 256);
     else if (MODE == CacheMode::tree && a.rows == 64)
-        hipLaunchKernelGGL((cache_attend_mfma_kernel<CacheMode::tree, 2, 2, 1>), grid, dim3(256), 0, st, a);
+        launch(cache_attend_mfma_kernel<CacheMode::tree, 1, 4, 1, 2>, 256);
     else
-        hipLaunchKernelGGL((cache_attend_mfma_kernel<MODE, 1, 4, 1>), grid, dim3(256), 0, st, a);
+        launch(cache_attend_mfma_kernel<MODE, 1, 4, 1, 1>, 256);
     return hipGetLastError();
 }
 
