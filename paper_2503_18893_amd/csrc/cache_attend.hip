@@ -209,6 +209,7 @@ __global__ __launch_bounds__(256) void cache_attend_general_kernel(CacheArgs a)
 // that neither the fragment reads (16 rows at a time, one piece each) nor the transposing reads (4 rows at a time, two pieces each)
 // meet in a bank.
 // ------------------------------------------------------------------------------------------
+constexpr int kHeldLogits = 32;  // rows of 32 logits that a wavefront holds back
 __device__ const u32x4_t kZeroRow[16] = {};  // stands for drafted tokens that nothing sees, and for places behind the last token
 
 template <CacheMode MODE, int WR, int WT, int SUB, int RT>
@@ -221,7 +222,7 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_attend_mf
     __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE >= WAVES * 16384 ? 2 * STAGE : WAVES * 16384];
     __shared__ float sm_m[WT][32 * WR * RT], sm_l[WT][32 * WR * RT];
     __shared__ uint32_t sm_seen[32];
-    __shared__ __attribute__((aligned(16))) float sm_z[MODE == CacheMode::weights ? WAVES : 1][MODE == CacheMode::weights ? 16 : 1][36];  // logits of a tile
+    __shared__ __attribute__((aligned(16))) float sm_z[MODE == CacheMode::weights ? WAVES : 1][MODE == CacheMode::weights ? kHeldLogits : 1][36];  // logits of a few tiles
     __shared__ int sm_rows[MODE == CacheMode::blocks ? kPartBlocks + 2 : 1];  // blocks: first rows of this part's blocks
     const int lane = lane_id(), w = wave_id(), rg = w % WR, tg = w / WR, n32 = lane & 31, hf = lane >> 5, n_rep = a.H_q / a.H_kv;
     const int M = MODE == CacheMode::blocks ? n_rep : a.N * n_rep;
@@ -370,6 +371,8 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_attend_mf
 #pragma unroll
         for (int db = 0; db < 4; ++db) O[rt][db] = f32x16_t(0.0f);
     }
+    int held = 0;  // tiles whose logits wait, of `hold`
+    const int hold = n_rep <= kHeldLogits / 8 ? 8 : kHeldLogits / n_rep;
     // logits of a tile of keys
     auto logits = [&](const unsigned char *lds, f32x16_t (&S)[PARTS]) __attribute__((always_inline)) {
 #pragma unroll
@@ -397,21 +400,29 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_attend_mf
                 for (int v = 0; v < 16; ++v) S[p][v] = sees >> (8 * (v / 4) + v % 4) & 1u ? S[p][v] : -INFINITY;
             }
         }
-        if constexpr (MODE == CacheMode::weights) {  // through LDS: a head's 32 logits leave as one line
+        // The logits of a few tiles wait in LDS and leave together, a line of 32 per head and tile: small stores between the requests
+        // of a stream slow it down by more than their share of its bytes.
+        if constexpr (MODE == CacheMode::weights) {
             static_assert(PARTS == 1 && OWN, "one tile of up to 16 rows per wavefront");
             if (n32 < n_rep) {
 #pragma unroll
                 for (int v = 0; v < 16; v += 4)
-                    *reinterpret_cast<f32x4_t *>(&sm_z[w][n32][2 * v + 4 * hf]) =
+                    *reinterpret_cast<f32x4_t *>(&sm_z[w][held * n_rep + n32][2 * v + 4 * hf]) =
                         f32x4_t{a.scale * S[0][v], a.scale * S[0][v + 1], a.scale * S[0][v + 2], a.scale * S[0][v + 3]};
             }
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-            float *to = a.logits + ((size_t)seq * a.H_q + g * n_rep) * a.L + tw + n32;
-            for (int h = hf; h < n_rep; h += 2)
-                if (tw + n32 < t_end) to[(size_t)h * a.L] = sm_z[w][h][n32];
-            __builtin_amdgcn_wave_barrier();
+            if (++held == hold || tw + TILE >= t_end) {
+                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+                float *to = a.logits + ((size_t)seq * a.H_q + g * n_rep) * a.L + n32;
+                for (int i = 0; i < held; ++i) {
+                    const int t = tw - TILE * (held - 1 - i);
+                    for (int h = hf; h < n_rep; h += 2)
+                        if (t + n32 < t_end) to[(size_t)h * a.L + t] = sm_z[w][i * n_rep + h][n32];
+                }
+                __builtin_amdgcn_wave_barrier();
+                held = 0;
+            }
         }
     };
     auto top_of = [&](const f32x16_t (&S)[PARTS], float (&m_loc)[RT]) __attribute__((always_inline)) {
