@@ -21,7 +21,7 @@ struct CacheArgs {
     // Partials, [part][N][H_q] rows of d_h numbers and of (maximum, sum); the parts of all sequences stand one after the other.
     float *part_o, *part_ml;
     int32_t *table;                   // [batch + 1]: the first part of every sequence, and behind the last one
-    float *logits;                    // weights: [batch][H_q][L]
+    float *logits, *weights;          // weights: [batch][H_q][L], [batch][H_kv][L]
     void *out;
     int L, H_kv, H_q, d_h, batch, N, words, c, k_ch;
     int rows;    // rows (query token, head) per workgroup
@@ -227,8 +227,6 @@ xkv_status plan_cache_attend(const xkv_shape &s, CacheMode mode, int N, int c, C
 xkv_status plan_evict(const xkv_shape &s, CachePlan &p);
 
 hipError_t launch_cache_attend(CacheMode mode, const xkv_shape &s, const CacheArgs &a, hipStream_t st);
-// weights += the weights that belong to the logits that launch_cache_attend kept
-hipError_t launch_cache_weights(const CacheArgs &a, float *weights, hipStream_t st);
 hipError_t launch_block_scores(const xkv_shape &s, const CacheArgs &a, const void *landmarks, int n_c, float *scores, hipStream_t st);
 hipError_t launch_landmarks_update(const xkv_shape &s, const void *K, const int32_t *lengths, int N, int c, void *landmarks, hipStream_t st);
 

@@ -231,9 +231,8 @@ xkv_status xkv_dense_decode_weights(const xkv_shape *shape, const void *K, const
     if (shape->batch == 0) return XKV_OK;
     CacheArgs a = attend_args(*shape, p, K, V, lengths, q, 1, out, workspace);
     a.logits = at<float>(workspace, p.off_logits);
-    hipError_t e = launch_cache_attend(CacheMode::weights, *shape, a, (hipStream_t)hip_stream);
-    if (e == hipSuccess) e = launch_cache_weights(a, weights, (hipStream_t)hip_stream);
-    return hip_status(e);
+    a.weights = weights;
+    return hip_status(launch_cache_attend(CacheMode::weights, *shape, a, (hipStream_t)hip_stream));
 }
 
 xkv_status xkv_evict(const xkv_shape *shape, const void *K, const void *V, const float *weights, const int32_t *lengths, int32_t sink,

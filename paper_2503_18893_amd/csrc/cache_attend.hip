@@ -703,7 +703,7 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_attend_mf
 // not written and are not read.
 // ------------------------------------------------------------------------------------------
 template <typename T, CacheMode MODE, int VEC>
-__global__ __launch_bounds__(256) void cache_merge_kernel(CacheArgs a, int lg, int share, int rows)
+__device__ __forceinline__ void merge_block(const CacheArgs &a, int lg, int share, int rows)
 {
     typedef __attribute__((ext_vector_type(VEC))) float vec_t;
     constexpr int BATCH = 4;
@@ -761,11 +761,12 @@ __global__ __launch_bounds__(256) void cache_merge_kernel(CacheArgs a, int lg, i
 // weights[t] += sum over the query heads of a KV head of exp(z_t - max) / sum, from the kept logits.  The maximum and the sum
 // of a head are merged from the partials by every workgroup.
 // ------------------------------------------------------------------------------------------
-__global__ __launch_bounds__(256) void cache_weights_kernel(CacheArgs a, float *__restrict__ weights)
+__device__ __forceinline__ void weights_block(const CacheArgs &a, int block)
 {
     __shared__ float sm_m[16], sm_r[16];
-    const int lane = lane_id(), w = wave_id(), n_rep = a.H_q / a.H_kv, g = blockIdx.y, b = blockIdx.z;
-    const int n = cache_rows(a, b), t0 = blockIdx.x * 1024;
+    const int per_head = (a.L + 1023) / 1024, g = block / per_head % a.H_kv, b = block / per_head / a.H_kv;
+    const int lane = lane_id(), w = wave_id(), n_rep = a.H_q / a.H_kv;
+    const int n = cache_rows(a, b), t0 = block % per_head * 1024;
     if (t0 >= n) return;
     const size_t head = (size_t)b * a.H_q + g * n_rep, stride = a.H_q;
     int first, parts;
@@ -789,8 +790,18 @@ __global__ __launch_bounds__(256) void cache_weights_kernel(CacheArgs a, float *
         if (t >= n) break;
         float sum = 0.0f;
         for (int h = 0; h < n_rep; ++h) sum = fmaf(expf(a.logits[(head + h) * a.L + t] - sm_m[h]), sm_r[h], sum);
-        weights[((size_t)b * a.H_kv + g) * a.L + t] += sum;
+        a.weights[((size_t)b * a.H_kv + g) * a.L + t] += sum;
     }
+}
+
+// x: workgroups of the merge, then (weights) those of the weights.
+template <typename T, CacheMode MODE, int VEC>
+__global__ __launch_bounds__(256) void cache_merge_kernel(CacheArgs a, int lg, int share, int rows, int merges)
+{
+    if (MODE != CacheMode::weights || (int)blockIdx.x < merges)
+        merge_block<T, MODE, VEC>(a, lg, share, rows);
+    else if (blockIdx.y == 0)
+        weights_block(a, (int)blockIdx.x - merges);
 }
 
 dim3 unit_grid(const CacheArgs &a, CacheMode mode, int M)
@@ -845,9 +856,11 @@ hipError_t launch_mode(const xkv_shape &s, const CacheArgs &a, hipStream_t st)
     int lg = 3;
     while (lg < 6 && (vec << lg) < a.d_h) ++lg;
     const int share = rows < 2048, groups = 256 >> lg;
-    const dim3 grid(share ? rows : (rows + groups - 1) / groups, (a.d_h + (vec << lg) - 1) / (vec << lg));
+    const int merges = share ? rows : (rows + groups - 1) / groups;
+    const unsigned more = MODE == CacheMode::weights ? (unsigned)(a.batch * a.H_kv) * ((a.L + 1023) / 1024) : 0u;
+    const dim3 grid(merges + more, (a.d_h + (vec << lg) - 1) / (vec << lg));
     auto merge = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a, lg, share, rows);
+        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a, lg, share, rows, merges);
         return hipGetLastError();
     };
     if (s.dtype == XKV_F32) return vec == 4 ? merge(cache_merge_kernel<float, MODE, 4>) : merge(cache_merge_kernel<float, MODE, 1>);
@@ -860,12 +873,6 @@ hipError_t launch_cache_attend(CacheMode mode, const xkv_shape &s, const CacheAr
 {
     return mode == CacheMode::tree ? launch_mode<CacheMode::tree>(s, a, st)
          : mode == CacheMode::weights ? launch_mode<CacheMode::weights>(s, a, st) : launch_mode<CacheMode::blocks>(s, a, st);
-}
-
-hipError_t launch_cache_weights(const CacheArgs &a, float *weights, hipStream_t st)
-{
-    hipLaunchKernelGGL(cache_weights_kernel, dim3((a.L + 1023) / 1024, a.H_kv, a.batch), dim3(256), 0, st, a, weights);
-    return hipGetLastError();
 }
 
 }  // namespace xkv

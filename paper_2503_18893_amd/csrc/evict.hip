@@ -5,6 +5,8 @@
 namespace xkv {
 namespace {
 
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
+
 // What the selection goes by: the weight, +inf for rows that are kept anyway, and below every number for rows that are not in use.
 __global__ __launch_bounds__(256) void evict_keys_kernel(EvictArgs a)
 {
@@ -17,29 +19,62 @@ __global__ __launch_bounds__(256) void evict_keys_kernel(EvictArgs a)
     a.keys[at] = t >= n ? -INFINITY : (t < a.sink || t >= n - a.recent) ? INFINITY : a.weights[at];
 }
 
-// Rows to their new places.  A row's new place is never behind its old one, so that a workgroup which takes the rows in order and
-// reads a step's rows (and those of the next one, which lie behind everything it writes) before it writes any of them may work in
-// place; elsewhere steps are workgroups of their own.  z: keys or values, and slices of `width` pieces of the rows, which move
-// independently of each other and make four workgroups of a KV head whose 256-byte rows are moved in place.
+// Rows to new places elsewhere: a workgroup per step of rows, z: keys or values.  All of a thread's rows are requested at once; what
+// bounds it is the copy.
+constexpr int kMoveRows = 8;  // rows per thread and step
+template <typename P>
+__global__ __launch_bounds__(256) void evict_copy_kernel(EvictArgs a, int pieces, int log_threads)
+{
+    const int row = blockIdx.y, b = row / a.H_kv;
+    const int piece = (int)threadIdx.x & ((1 << log_threads) - 1), at_once = 256 >> log_threads, step = at_once * kMoveRows;
+    const int32_t *sel = a.sel + (size_t)row * a.k;
+    const bool of_v = blockIdx.z;
+    const int i0 = (int)blockIdx.x * step, r0 = (int)threadIdx.x >> log_threads;
+    int src[kMoveRows];
+#pragma unroll
+    for (int u = 0; u < kMoveRows; ++u) src[u] = sel[i0 + u * at_once + r0 < a.k ? i0 + u * at_once + r0 : a.k - 1];
+    const int n = a.n[b], m = n < a.k ? n : a.k;
+    if (i0 < m) {
+        const P *from = (const P *)(of_v ? a.V : a.K) + (size_t)row * a.L * pieces + (piece < pieces ? piece : 0);
+        P *to = (P *)(of_v ? a.V_out : a.K_out) + (size_t)row * a.L_out * pieces + piece;
+        P x[kMoveRows];
+#pragma unroll
+        for (int u = 0; u < kMoveRows; ++u) x[u] = __builtin_nontemporal_load(from + (size_t)src[u] * pieces);  // (any entry of sel is a row)
+#pragma unroll
+        for (int u = 0; u < kMoveRows; ++u) {
+            const int i = i0 + u * at_once + r0;
+            if (piece < pieces && i < m) __builtin_nontemporal_store(x[u], to + (size_t)i * pieces);
+        }
+    }
+    if (of_v) return;
+    for (int i = i0 + (int)threadIdx.x; i < i0 + step && i < a.k; i += 256) {
+        const int t = sel[i];
+        if (i < m) a.weights_out[(size_t)row * a.L_out + i] = a.weights[(size_t)row * a.L + t];
+        if (a.rows_out) a.rows_out[(size_t)row * a.k + i] = i < m ? t : -1;
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0 && row == b * a.H_kv && a.lengths_out) a.lengths_out[b] = m;
+}
+
+// Rows to new places in the same cache.  A row's new place is never behind its old one, so that a workgroup which takes the rows in
+// order and reads a step's rows (and those of the next one, which lie behind everything it writes) before it writes any of them may
+// work in place.  z: keys or values, and slices of `width` pieces of the rows, which move independently of each other and make four
+// workgroups of a KV head whose rows have 256 bytes.
 // A use of a loaded value: it is waited for here.
-__device__ __forceinline__ void arrived(uint4 &x) { asm volatile("" : "+v"(x.x), "+v"(x.y), "+v"(x.z), "+v"(x.w)); }
+__device__ __forceinline__ void arrived(u32x4_t &x) { asm volatile("" : "+v"(x)); }
 __device__ __forceinline__ void arrived(uint32_t &x) { asm volatile("" : "+v"(x)); }
 __device__ __forceinline__ void arrived(uint16_t &x) { asm volatile("" : "+v"(x)); }
 __device__ __forceinline__ void arrived(float &x) { asm volatile("" : "+v"(x)); }
 
-constexpr int kMoveRows = 8;  // rows per thread and step
 template <typename P>
 __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, int pieces, int width, int log_threads)
 {
     const int row = blockIdx.y, b = row / a.H_kv, n = a.n[b], m = n < a.k ? n : a.k;
     const bool of_v = blockIdx.z & 1;
-    const int piece = (int)(blockIdx.z >> 1) * width + ((int)threadIdx.x & ((1 << log_threads) - 1));
-    const bool mine = ((int)threadIdx.x & ((1 << log_threads) - 1)) < width && piece < pieces;
+    const int in_slice = (int)threadIdx.x & ((1 << log_threads) - 1), piece = (int)(blockIdx.z >> 1) * width + in_slice;
+    const bool mine = in_slice < width && piece < pieces;
     const int at_once = 256 >> log_threads, step = at_once * kMoveRows, r0 = (int)threadIdx.x >> log_threads;
     const int32_t *sel = a.sel + (size_t)row * a.k;
-    const P *from = (const P *)(of_v ? a.V : a.K) + (size_t)row * a.L * pieces + piece;
-    P *to = (P *)(of_v ? a.V_out : a.K_out) + (size_t)row * a.L_out * pieces + piece;
-    const bool in_place = (const void *)to == (const void *)from;
+    P *rows = (P *)(of_v ? a.V_out : a.K_out) + (size_t)row * a.L * pieces + piece;
     const bool head = blockIdx.z == 0;  // weights and row numbers are moved here
     P x[2][kMoveRows];
     int src[2][kMoveRows];  // -1: nothing to move
@@ -50,19 +85,19 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, int pieces
         for (int u = 0; u < kMoveRows; ++u) {
             const int i = i0 + u * at_once + r0;
             src[s][u] = mine && i < m ? sel[i] : -1;
-            if (in_place && src[s][u] == i) src[s][u] = -1;
+            if (src[s][u] == i) src[s][u] = -1;
         }
 #pragma unroll
         for (int u = 0; u < kMoveRows; ++u) {
             x[s][u] = P{};
-            if (src[s][u] >= 0) x[s][u] = from[(size_t)src[s][u] * pieces];
+            if (src[s][u] >= 0) x[s][u] = rows[(size_t)src[s][u] * pieces];
         }
         if (head) {
 #pragma unroll
             for (int u = 0; u < kMoveRows; ++u) {
                 const int r = 256 * u + (int)threadIdx.x, i = i0 + r;
                 wsrc[s][u] = r < step && i < m ? sel[i] : -1;
-                w[s][u] = wsrc[s][u] >= 0 ? a.weights[(size_t)row * a.L + wsrc[s][u]] : 0.0f;
+                w[s][u] = wsrc[s][u] >= 0 ? a.weights_out[(size_t)row * a.L + wsrc[s][u]] : 0.0f;
             }
         }
     };
@@ -77,30 +112,28 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, int pieces
         lds_barrier();
 #pragma unroll
         for (int u = 0; u < kMoveRows; ++u)
-            if (src[s][u] >= 0) to[(size_t)(i0 + u * at_once + r0) * pieces] = x[s][u];
+            if (src[s][u] >= 0) rows[(size_t)(i0 + u * at_once + r0) * pieces] = x[s][u];
         if (head) {
 #pragma unroll
             for (int u = 0; u < kMoveRows; ++u) {
                 const int r = 256 * u + (int)threadIdx.x, i = i0 + r;
                 if (r >= step || i >= a.k) continue;
-                if (wsrc[s][u] >= 0) a.weights_out[(size_t)row * a.L_out + i] = w[s][u];
+                if (wsrc[s][u] >= 0) a.weights_out[(size_t)row * a.L + i] = w[s][u];
                 if (a.rows_out) a.rows_out[(size_t)row * a.k + i] = wsrc[s][u];
             }
         }
     };
-    const int stride = (int)gridDim.x * step;
-    int i0 = (int)blockIdx.x * step;
-    if (i0 < a.k) read(i0, 0);
-    for (; i0 < a.k; i0 += 2 * stride) {
+    read(0, 0);
+    for (int i0 = 0; i0 < a.k; i0 += 2 * step) {
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            const int at = i0 + s * stride;
+            const int at = i0 + s * step;
             if (at >= a.k) break;
-            if (a.k - at > stride) read(at + stride, s ^ 1);
+            if (a.k - at > step) read(at + step, s ^ 1);
             write(at, s);
         }
     }
-    if (blockIdx.x == 0 && head && threadIdx.x == 0 && row == b * a.H_kv && a.lengths_out) a.lengths_out[b] = m;
+    if (head && threadIdx.x == 0 && row == b * a.H_kv && a.lengths_out) a.lengths_out[b] = m;
 }
 
 }  // namespace
@@ -114,19 +147,23 @@ hipError_t launch_evict(const xkv_shape &s, const CachePlan &p, const EvictArgs 
     if (e != hipSuccess) return e;
     const size_t row_bytes = (size_t)a.d_h * (s.dtype == XKV_F32 ? 4 : 2);
     const uintptr_t bits = (uintptr_t)a.K | (uintptr_t)a.V | (uintptr_t)a.K_out | (uintptr_t)a.V_out | row_bytes;
-    const bool in_place = a.K_out == a.K || a.V_out == a.V || a.weights_out == a.weights;
-    auto launch = [&](auto kernel, int piece) {
+    const bool in_place = a.K_out == a.K;
+    auto launch = [&](auto copy, auto move, int piece) {
         const int pieces = (int)(row_bytes / piece);
         // in place: slices of whole 128-byte lines, so that more than two workgroups work on a KV head
         const int width = in_place && row_bytes % 128 == 0 ? 128 / piece : pieces, slices = (pieces + width - 1) / width;
         int log_threads = 0;
         while ((1 << log_threads) < width) ++log_threads;
         const int step = (256 >> log_threads) * kMoveRows;
-        hipLaunchKernelGGL(kernel, dim3(in_place ? 1 : (a.k + step - 1) / step, rows, 2 * slices), dim3(256), 0, st, a, pieces, width, log_threads);
+        if (in_place)
+            hipLaunchKernelGGL(move, dim3(1, rows, 2 * slices), dim3(256), 0, st, a, pieces, width, log_threads);
+        else
+            hipLaunchKernelGGL(copy, dim3((a.k + step - 1) / step, rows, 2), dim3(256), 0, st, a, pieces, log_threads);
         return hipGetLastError();
     };
-    return bits % 16 == 0 ? launch(evict_move_kernel<uint4>, 16) : s.dtype == XKV_F32 ? launch(evict_move_kernel<uint32_t>, 4)
-                                                                                        : launch(evict_move_kernel<uint16_t>, 2);
+    return bits % 16 == 0 ? launch(evict_copy_kernel<u32x4_t>, evict_move_kernel<u32x4_t>, 16)
+         : s.dtype == XKV_F32 ? launch(evict_copy_kernel<uint32_t>, evict_move_kernel<uint32_t>, 4)
+                              : launch(evict_copy_kernel<uint16_t>, evict_move_kernel<uint16_t>, 2);
 }
 
 }  // namespace xkv
