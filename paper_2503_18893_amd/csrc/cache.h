@@ -219,7 +219,7 @@ struct CachePlan {
     bool mfma;
     xkv_shape sel_shape;  // the selection as a problem of launch_topk: rows of blocks, or rows of the cache
     Plan sel_plan;
-    size_t off_hist, off_state, off_keys, off_sel, off_n, off_logits, off_table, off_part_o, off_part_ml, total;
+    size_t off_hist, off_state, off_keys, off_reach, off_sel, off_n, off_logits, off_table, off_part_o, off_part_ml, total;
 };
 
 // The plan of one call.  N: query tokens of a sequence; c: rows of a block.
@@ -228,6 +228,10 @@ xkv_status plan_evict(const xkv_shape &s, CachePlan &p);
 
 hipError_t launch_cache_attend(CacheMode mode, const xkv_shape &s, const CacheArgs &a, hipStream_t st);
 hipError_t launch_block_scores(const xkv_shape &s, const CacheArgs &a, const void *landmarks, int n_c, float *scores, hipStream_t st);
+// The blocks of every query and KV head, for up to 16384 of them (block_select_ok); reach: room for [batch][N][H_kv][n_c / 16] numbers.
+bool block_select_ok(int n_c);
+hipError_t launch_block_select(const xkv_shape &s, const CacheArgs &a, const void *landmarks, int n_c, float *scores, float *reach, int32_t *blocks,
+                               hipStream_t st);
 hipError_t launch_landmarks_update(const xkv_shape &s, const void *K, const int32_t *lengths, int N, int c, void *landmarks, hipStream_t st);
 
 struct EvictArgs {

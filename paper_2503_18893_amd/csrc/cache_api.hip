@@ -50,7 +50,17 @@ xkv_status plan_cache_attend(const xkv_shape &s, CacheMode mode, int N, int c, C
         if ((long long)p.k_ch * c < most) most = (long long)p.k_ch * c;
         if ((long long)p.k_ch * c > 0x7FFFFFFFLL - 4096) return XKV_ERR_UNSUPPORTED;
         p.sel_shape = xkv_shape{1, s.H_kv, s.H_kv, 1, 1, 1, p.n_c, p.k_ch, (int32_t)(batch * N), XKV_F32, 1.0f};
-        off = plan_selection(p, off);
+        if (block_select_ok(p.n_c)) {
+            const size_t rows = (size_t)batch * N * s.H_kv;
+            p.off_keys = off;
+            off = align_up(off + rows * p.n_c * sizeof(float), 256);
+            p.off_reach = off;
+            off = align_up(off + rows * ceil_div(p.n_c, 16) * sizeof(float), 256);
+            p.off_sel = off;
+            off = align_up(off + rows * p.k_ch * sizeof(int32_t), 256);
+        } else {
+            off = plan_selection(p, off);
+        }
     }
     // The matrix-core kernel: as many rows per workgroup as there are, up to 256 (128 where that leaves fewer of them empty), one workgroup
     // to a compute unit (two of 128 rows).  The general one: 16 rows, rounds of 64 tokens, four workgroups.
@@ -201,10 +211,15 @@ xkv_status xkv_block_decode(const xkv_shape *shape, const void *K, const void *V
     float *scores = at<float>(workspace, p.off_keys);
     int32_t *sel = blocks_out ? blocks_out : at<int32_t>(workspace, p.off_sel);
     a.sel = sel;
-    hipError_t e = launch_block_scores(*shape, a, landmarks, p.n_c, scores, stream);
-    if (e == hipSuccess)
-        e = launch_topk(p.sel_shape, p.sel_plan, scores, sel, at<uint32_t>(workspace, p.off_hist), at<uint32_t>(workspace, p.off_state), false,
-                        stream);
+    hipError_t e;
+    if (block_select_ok(p.n_c)) {
+        e = launch_block_select(*shape, a, landmarks, p.n_c, scores, at<float>(workspace, p.off_reach), sel, stream);
+    } else {
+        e = launch_block_scores(*shape, a, landmarks, p.n_c, scores, stream);
+        if (e == hipSuccess)
+            e = launch_topk(p.sel_shape, p.sel_plan, scores, sel, at<uint32_t>(workspace, p.off_hist), at<uint32_t>(workspace, p.off_state), false,
+                            stream);
+    }
     if (e == hipSuccess) e = launch_cache_attend(CacheMode::blocks, *shape, a, stream);
     return hip_status(e);
 }

@@ -201,6 +201,23 @@ def test_blocks(name):
                 within(out[b, i, heads], o, bound, f"{name} {b} {i} {h}")
 
 
+@pytest.mark.parametrize("L,c,k", [(1500, 1, 300), (4000, 1, 64), (9000, 1, 1000), (17000, 1, 500), (3000, 2, 700)])
+@pytest.mark.parametrize("spread", [1.0, 2.0 ** -7, 2.0 ** -12, 0.0])
+def test_blocks_whose_scores_lie_close_together(L, c, k, spread):
+    """Means that differ by a few roundings, or not at all: the selection is that of the sums in double precision, rounded once."""
+    s = shape_of(1, 4, 128, L, 2, "bf16", k=k)
+    g, K, V = cache(s, [L, L], 14)
+    n_c, k_ch = -(-L // c), -(-k // c)
+    marks = (1.0 + spread * torch.randn((2, 1, n_c, 128), generator=g)).bfloat16()
+    marks[:, :, n_c // 2:n_c // 2 + 50] = marks[:, :, :50]  # and some twice
+    visible = [L, L - L // 3]
+    q = torch.randn((2, 1, 4, 128), generator=g).bfloat16()
+    out, blocks = torch.empty_like(q).cuda(), torch.empty((2, 1, 1, k_ch), dtype=torch.int32, device="cuda")
+    xb.xkv_block_decode(s, K.cuda(), V.cuda(), ints(visible), q.cuda(), 1, marks.cuda(), c, out, blocks, workspace(s, 1, c))
+    for b in range(2):
+        assert blocks.cpu()[b, 0, 0].tolist() == ref.choose_blocks(q[b, 0], marks[b, 0], visible[b], c, k_ch)
+
+
 def test_blocks_tie_towards_the_smaller_block():
     s = shape_of(1, 2, 128, 320, 1, "bf16", k=64)
     g, K, V = cache(s, [320], 9)
