@@ -85,16 +85,20 @@ struct MaxOp {
     __device__ __forceinline__ int operator()(int x, int y) const { return x > y ? x : y; }
 };
 
+struct UMaxOp {
+    __device__ __forceinline__ uint32_t operator()(uint32_t x, uint32_t y) const { return x > y ? x : y; }
+};
+
 __device__ __forceinline__ int ceil_div_dev(int a, int b) { return (int)(((unsigned)a + (unsigned)b - 1u) / (unsigned)b); }
 
-// Tokens per part.  All lanes of a wavefront call it together.
-__device__ __forceinline__ int cache_chunk(const CacheArgs &a, CacheMode mode)
+// Tokens per part.  All lanes of a wavefront call it together; t: tokens of sequence `lane` (of the first 64).
+__device__ __forceinline__ int cache_chunk(const CacheArgs &a, CacheMode mode, int t)
 {
     const int lane = lane_id();
     long long total = 0;  // (of 64 sequences: in whole 4096s and the rest)
     int most = 0;
     for (int b0 = 0; b0 < a.batch; b0 += kWave) {
-        const int t = b0 + lane < a.batch ? cache_tokens(a, mode, cache_rows(a, b0 + lane)) : 0;
+        if (b0 > 0) t = b0 + lane < a.batch ? cache_tokens(a, mode, cache_rows(a, b0 + lane)) : 0;
         total += ((long long)wave_all(t >> 12, AddOp()) << 12) + wave_all(t & 4095, AddOp());
         most = MaxOp()(most, wave_all(t, MaxOp()));
     }
@@ -107,7 +111,7 @@ __device__ __forceinline__ int cache_chunk(const CacheArgs &a, CacheMode mode)
     const int step = ceil_div_dev(hi - lo, kWave - 1), chunk = (lo + lane * step) * a.round;
     long long used = 0;
     for (int b0 = 0; b0 < a.batch; b0 += kWave) {
-        const int t = b0 + lane < a.batch ? cache_tokens(a, mode, cache_rows(a, b0 + lane)) : 0;
+        if (a.batch > kWave) t = b0 + lane < a.batch ? cache_tokens(a, mode, cache_rows(a, b0 + lane)) : 0;
         for (int i = 0; i < kWave && b0 + i < a.batch; ++i) used += ceil_div_dev(__builtin_amdgcn_readlane(t, i), chunk);
     }
     const uint64_t fits = __ballot(used <= a.parts);  // (the last candidate is at least hi)
@@ -157,10 +161,14 @@ __device__ __forceinline__ CacheUnit cache_unit(const CacheArgs &a, CacheMode mo
         }
         return u;
     }
-    const int chunk = __builtin_amdgcn_readfirstlane(cache_chunk(a, mode));
+    int n = lane < a.batch ? cache_rows(a, lane) : 0, t = lane < a.batch ? cache_tokens(a, mode, n) : 0;
+    const int chunk = __builtin_amdgcn_readfirstlane(cache_chunk(a, mode, t));
     int before = 0;
     for (int b0 = 0; b0 < a.batch; b0 += kWave) {
-        const int n = b0 + lane < a.batch ? cache_rows(a, b0 + lane) : 0, t = b0 + lane < a.batch ? cache_tokens(a, mode, n) : 0;
+        if (b0 > 0) {
+            n = b0 + lane < a.batch ? cache_rows(a, b0 + lane) : 0;
+            t = b0 + lane < a.batch ? cache_tokens(a, mode, n) : 0;
+        }
         const int mine = ceil_div_dev(t, chunk);
         int upto = mine;
 #pragma unroll
@@ -246,6 +254,7 @@ struct EvictArgs {
     int32_t *n;     // [batch] rows in use before
     int L, L_out, H_kv, d_h, k, sink, recent, batch;
 };
+bool evict_select_ok(int L);  // one launch selects; longer rows go through launch_topk
 hipError_t launch_evict(const xkv_shape &s, const CachePlan &p, const EvictArgs &a, uint32_t *hist, uint32_t *state, hipStream_t st);
 
 }  // namespace xkv

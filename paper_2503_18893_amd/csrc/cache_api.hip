@@ -104,7 +104,10 @@ xkv_status plan_evict(const xkv_shape &s, CachePlan &p)
 {
     std::memset(&p, 0, sizeof p);
     p.sel_shape = xkv_shape{1, s.H_kv, s.H_kv, 1, 1, 1, s.L, s.k, s.batch > 0 ? s.batch : 1, XKV_F32, 1.0f};
-    p.off_n = plan_selection(p, 0);
+    if (evict_select_ok(s.L))
+        p.off_n = align_up((size_t)p.sel_shape.batch * s.H_kv * s.k * sizeof(int32_t), 256);  // the rows, at 0
+    else
+        p.off_n = plan_selection(p, 0);
     p.total = align_up(p.off_n + (size_t)p.sel_shape.batch * sizeof(int32_t), 256);
     return XKV_OK;
 }

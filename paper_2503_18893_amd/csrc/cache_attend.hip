@@ -464,10 +464,11 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_attend_mf
 #pragma unroll
                 for (int v = 8 * j; v < 8 * j + 8; ++v) {
                     S[p][v] = __builtin_amdgcn_exp2f(fmaf(S[p][v], c, less));
-                    if (OWN) l_run[rt] += S[p][v];  // (the weights that are given out are divided by this sum: in single precision)
+                    // (weights that are given out are divided by this sum: unrounded)
+                    if (MODE == CacheMode::weights) l_run[rt] += S[p][v];
                 }
                 P[2 * p + j] = pack8(S[p], j);
-                if (!OWN) l_run[rt] = add_pairs(P[2 * p + j], l_run[rt]);
+                if (MODE != CacheMode::weights) l_run[rt] = add_pairs(P[2 * p + j], l_run[rt]);
             }
         }
     };
