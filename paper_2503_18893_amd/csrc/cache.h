@@ -6,6 +6,9 @@
 
 namespace xkv {
 
+constexpr int kMaxCacheParts = 256;  // parts of a sequence that the merge takes
+constexpr int kPartBlocks = 2048;    // blocks of a part (its first and its last one may be shared with its neighbours)
+
 // What a query attends to.  Its tokens are numbered 0 .. T - 1, T known on the device only:
 //   tree     the rows of the cache in use, then the drafted tokens; bits of `tree` say which of those it sees
 //   weights  the rows in use; logits are kept
@@ -44,7 +47,7 @@ __device__ __forceinline__ int cache_tokens(const CacheArgs &a, CacheMode mode, 
 {
     if (mode == CacheMode::tree) return n + a.N;
     if (mode == CacheMode::weights) return n;
-    const int blocks = (n + a.c - 1) / a.c, listed = blocks < a.k_ch ? blocks : a.k_ch;
+    const int blocks = (int)(((unsigned)n + (unsigned)a.c - 1u) / (unsigned)a.c), listed = blocks < a.k_ch ? blocks : a.k_ch;
     return listed > 0 ? (listed - 1) * a.c + n - (blocks - 1) * a.c : 0;
 }
 
@@ -107,7 +110,10 @@ __device__ __forceinline__ int cache_chunk(const CacheArgs &a, CacheMode mode, i
     const int top = whole / a.round;  // candidates, in rounds
     const long long enough = (total + (long long)(a.parts - a.batch) * a.round - 1) / ((long long)(a.parts - a.batch) * a.round);
     const long long least = (total + (long long)a.parts * a.round - 1) / ((long long)a.parts * a.round);
-    const int hi = enough < top ? (int)enough : top, lo = least < hi ? (int)least : hi;
+    const int most_parts = ceil_div_dev(top, kMaxCacheParts);  // (the others may be empty: one sequence may have all the parts)
+    int hi = enough < top ? (int)enough : top, lo = least < hi ? (int)least : hi;
+    lo = lo > most_parts ? lo : most_parts;
+    hi = hi > lo ? hi : lo;
     const int step = ceil_div_dev(hi - lo, kWave - 1), chunk = (lo + lane * step) * a.round;
     long long used = 0;
     for (int b0 = 0; b0 < a.batch; b0 += kWave) {
@@ -217,8 +223,6 @@ __device__ __forceinline__ size_t part_row(const CacheArgs &a, CacheMode mode, i
     return ((size_t)part * (mode == CacheMode::blocks ? 1 : a.N) + (mode == CacheMode::blocks ? 0 : token)) * a.H_q + head;
 }
 
-constexpr int kMaxCacheParts = 256;  // parts of a sequence that the merge takes
-constexpr int kPartBlocks = 2048;    // blocks of a part (its first and its last one may be shared with its neighbours)
 
 struct CachePlan {
     int n_rep, words, n_c, k_ch;

@@ -40,7 +40,7 @@ xkv_status plan_cache_attend(const xkv_shape &s, CacheMode mode, int N, int c, C
     p.scale = s.scale > 0.0f ? s.scale : 1.0f / std::sqrt((float)s.d_h);
     const long long batch = s.batch > 0 ? s.batch : 1;
     if (batch * N * s.H_kv > 65535LL) return XKV_ERR_UNSUPPORTED;  // rows of the selection and of the merge are y of a grid
-    if ((long long)s.L + N > 0x7FFFFFFFLL - 4096) return XKV_ERR_UNSUPPORTED;
+    if ((long long)s.L + N > (1LL << 30)) return XKV_ERR_UNSUPPORTED;  // (sums of two places in a sequence are ints)
     size_t off = 0;
     long long most = s.L + (mode == CacheMode::tree ? N : 0);  // tokens of a query
     if (mode == CacheMode::blocks) {
@@ -48,7 +48,7 @@ xkv_status plan_cache_attend(const xkv_shape &s, CacheMode mode, int N, int c, C
         p.n_c = ceil_div(s.L, c);
         p.k_ch = ceil_div(s.k, c) < p.n_c ? ceil_div(s.k, c) : p.n_c;
         if ((long long)p.k_ch * c < most) most = (long long)p.k_ch * c;
-        if ((long long)p.k_ch * c > 0x7FFFFFFFLL - 4096) return XKV_ERR_UNSUPPORTED;
+        if ((long long)p.k_ch * c > (1LL << 30)) return XKV_ERR_UNSUPPORTED;
         p.sel_shape = xkv_shape{1, s.H_kv, s.H_kv, 1, 1, 1, p.n_c, p.k_ch, (int32_t)(batch * N), XKV_F32, 1.0f};
         if (block_select_ok(p.n_c)) {
             const size_t rows = (size_t)batch * N * s.H_kv;

@@ -440,7 +440,7 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_attend_mf
     auto raise = [&](const float (&m_loc)[RT]) __attribute__((always_inline)) {
         bool any = false;
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) any |= (m_loc[rt] - m_run[rt]) * c > 8.0f;
+        for (int rt = 0; rt < RT; ++rt) any |= !((m_loc[rt] - m_run[rt]) * c <= 8.0f);
         if (__ballot(any)) {
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {

@@ -475,8 +475,9 @@ __global__ __launch_bounds__(256) void landmarks_update_kernel(const T *__restri
     const int lane = lane_id(), row = blockIdx.y;
     int n = lengths ? lengths[row / H_kv] : L;
     n = n < 0 ? 0 : n < L ? n : L;
-    const int j = (n > N ? n - N : 0) / c + blockIdx.x * 4 + wave_id(), t0 = j * c, t1 = t0 + c < n ? t0 + c : n;
+    const int j = (n > N ? n - N : 0) / c + blockIdx.x * 4 + wave_id();
     if (n == 0 || j > (n - 1) / c) return;
+    const int t0 = j * c, t1 = n - t0 > c ? t0 + c : n;
     const float inv = 1.0f / (float)(t1 - t0);
     for (int e = lane; e < d; e += kWave) {
         float sum = 0.0f;
@@ -546,7 +547,7 @@ hipError_t launch_block_scores(const xkv_shape &s, const CacheArgs &a, const voi
 
 hipError_t launch_landmarks_update(const xkv_shape &s, const void *K, const int32_t *lengths, int N, int c, void *landmarks, hipStream_t st)
 {
-    const int n_c = (s.L + c - 1) / c, most = (N + c - 1) / c + 1, blocks = most < n_c ? most : n_c;
+    const int n_c = (s.L - 1) / c + 1, most = (N - 1) / c + 2, blocks = most < n_c ? most : n_c;  // (N rows: one block more if they begin inside one)
     const dim3 grid((blocks + 3) / 4, s.batch * s.H_kv);
     if (s.dtype == XKV_F32)
         hipLaunchKernelGGL(landmarks_update_kernel<float>, grid, dim3(256), 0, st, (const float *)K, lengths, (float *)landmarks, s.L, s.d_h,

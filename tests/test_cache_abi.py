@@ -81,6 +81,8 @@ def test_counts_are_checked():
     assert tree(s, N=1025) == xb.XKV_ERR_UNSUPPORTED
     assert block(s, N=5000) == xb.XKV_ERR_UNSUPPORTED          # 2 * 5000 * 8 rows of the selection
     assert tree(shape(batch=100), N=100) == xb.XKV_ERR_UNSUPPORTED
+    long = shape(L=2 ** 30 + 1)
+    assert tree(long) == block(long) == weights(long) == xb.XKV_ERR_UNSUPPORTED
 
 
 def test_evictions_are_checked():

@@ -374,6 +374,98 @@ def test_evict_without_optional_results_and_lengths():
         assert torch.equal(Kc.cpu()[0, h, :77], K[0, h, keep]) and torch.equal(wc.cpu()[0, h, :77], w[0, h, keep])
 
 
+# ------------------------------------------------------------------------------------------------- shapes of a program
+@pytest.mark.parametrize("dtype,d,batch,H_kv", [("f32", 64, 100, 1), ("bf16", 128, 100, 1), ("bf16", 128, 300, 2)])
+def test_one_long_sequence_among_empty_ones(dtype, d, batch, H_kv):
+    """All parts that a launch has go to one sequence."""
+    L = 30000
+    s = shape_of(H_kv, 2, d, L, batch, dtype)
+    g = torch.Generator(device="cuda").manual_seed(15)
+    K, V = (torch.zeros((batch, H_kv, L, d), dtype=DT[dtype], device="cuda") for _ in "KV")
+    at = batch - 3
+    K[at], V[at] = (torch.randn((H_kv, L, d), generator=g, device="cuda") for _ in "KV")
+    lengths = [0] * batch
+    lengths[at] = L
+    q = torch.randn((batch, s.H_q, d), generator=g, device="cuda").to(DT[dtype])
+    out, w = torch.full_like(q, float("nan")), torch.zeros((batch, H_kv, L), device="cuda")
+    xb.xkv_dense_decode_weights(s, K, V, ints(lengths), q, out, w, workspace(s))
+    rest = torch.arange(batch) != at
+    assert (out.cpu()[rest] == 0).all() and (w.cpu()[rest] == 0).all()
+    for h in range(H_kv):
+        o, p, bound, rel = ref.attend(q.cpu()[at, 2 * h:2 * h + 2], K.cpu()[at, h], V.cpu()[at, h], torch.ones((2, L), dtype=torch.bool), scale_of(s))
+        within(out.cpu()[at, 2 * h:2 * h + 2], o, bound, "long")
+        assert ((w.cpu()[at, h].double() - p.sum(0)).abs() <= (2 * rel + 4 * 2.0 ** -24) * p.sum(0)).all()
+
+
+def test_pointers_that_are_not_aligned_take_the_general_kernels():
+    s = shape_of(1, 4, 128, 333, 1, "bf16", k=64)
+    g, K, V = cache(s, [333], 16)
+    q, Kd, Vd = (torch.randn(x, generator=g).bfloat16() for x in ((1, 9, 4, 128), (1, 1, 9, 128), (1, 1, 9, 128)))
+
+    def shifted(x):  # 8 bytes behind an aligned address
+        flat = torch.empty(x.numel() + 4, dtype=x.dtype, device="cuda")
+        flat[4:] = x.flatten().cuda()
+        return flat[4:].view(x.shape)
+
+    out, ws = torch.full_like(q, float("nan"), device="cuda"), workspace(s, 9, 16)
+    xb.xkv_tree_decode(s, shifted(K), shifted(V), None, shifted(q), shifted(Kd), shifted(Vd), None, 9, out, ws)
+    check_tree(s, [333], 9, K, V, q, Kd, Vd, torch.ones((1, 9, 9), dtype=torch.bool).tril(), out.cpu(), "shifted")
+    marks = means_of(K, [333], 16)
+    blocks = torch.empty((1, 9, 1, 4), dtype=torch.int32, device="cuda")
+    xb.xkv_block_decode(s, shifted(K), shifted(V), None, shifted(q), 9, shifted(marks), 16, out, blocks, ws)
+    for i in range(9):
+        want = ref.choose_blocks(q[0, i], marks[0, 0], 333, 16, 4)
+        assert blocks.cpu()[0, i, 0].tolist() == want
+        t = torch.tensor([j * 16 + x for j in want for x in range(16) if j * 16 + x < 333])
+        o, _, bound, _ = ref.attend(q[0, i], K[0, 0, t], V[0, 0, t], torch.ones((4, len(t)), dtype=torch.bool), scale_of(s))
+        within(out.cpu()[0, i], o, bound, "shifted blocks")
+    w = torch.rand((1, 1, 333), generator=g)
+    Ko, Vo, wo = shifted(torch.zeros((1, 1, 64, 128), dtype=torch.bfloat16)), shifted(torch.zeros((1, 1, 64, 128), dtype=torch.bfloat16)), torch.zeros((1, 1, 64), device="cuda")
+    xb.xkv_evict(s, shifted(K), shifted(V), w.cuda(), None, 1, 2, 64, Ko, Vo, wo, None, None, ws)
+    keep = ref.keep_rows(w[0, 0], 333, 64, 1, 2)
+    assert torch.equal(Ko.cpu()[0, 0], K[0, 0, keep]) and torch.equal(Vo.cpu()[0, 0], V[0, 0, keep])
+
+
+def test_a_cache_of_more_than_two_to_the_31_elements():
+    """Everything is at the end of it: the last sequence's last KV head is compared."""
+    batch, H_kv, L, d, N, c = 5, 4, 860000, 128, 5, 64
+    s = shape_of(H_kv, 2, d, L, batch, "bf16", k=640)
+    assert batch * H_kv * L * d > 2 ** 31
+    g = torch.Generator(device="cuda").manual_seed(17)
+    K, V = (torch.zeros((batch, H_kv, L, d), dtype=torch.bfloat16, device="cuda") for _ in "KV")
+    k, v = torch.randn((L, d), generator=g, device="cuda").bfloat16(), torch.randn((L, d), generator=g, device="cuda").bfloat16()
+    K[-1, -1], V[-1, -1] = k, v
+    lengths = ints([1, 0, 5, 64, L])
+    q = torch.randn((batch, N, s.H_q, d), generator=g, device="cuda").bfloat16()
+    Kd, Vd = (torch.randn((batch, H_kv, N, d), generator=g, device="cuda").bfloat16() for _ in "KV")
+    ws, out = workspace(s, N, c), torch.full_like(q, float("nan"))
+    xb.xkv_tree_decode(s, K, V, lengths, q, Kd, Vd, None, N, out, ws)
+    mask = torch.cat((torch.ones((N, L), dtype=torch.bool), torch.ones((N, N), dtype=torch.bool).tril()), 1).repeat_interleave(2, 0)
+    o, _, bound, _ = ref.attend(q[-1, :, 6:].reshape(-1, d).cpu(), torch.cat((k, Kd[-1, -1])).cpu(), torch.cat((v, Vd[-1, -1])).cpu(), mask, scale_of(s))
+    within(out[-1, :, 6:].reshape(-1, d).cpu(), o, bound, "tree")
+    w = torch.zeros((batch, H_kv, L), device="cuda")
+    q1, out1 = q[:, 0].contiguous(), torch.full((batch, s.H_q, d), float("nan"), dtype=torch.bfloat16, device="cuda")
+    xb.xkv_dense_decode_weights(s, K, V, lengths, q1, out1, w, ws)
+    o, p, bound, rel = ref.attend(q1[-1, 6:].cpu(), k.cpu(), v.cpu(), torch.ones((2, L), dtype=torch.bool), scale_of(s))
+    within(out1[-1, 6:].cpu(), o, bound, "weights")
+    assert ((w[-1, -1].cpu().double() - p.sum(0)).abs() <= (2 * rel + 4 * 2.0 ** -24) * p.sum(0)).all()
+    marks = torch.zeros((batch, H_kv, -(-L // c), d), dtype=torch.bfloat16, device="cuda")
+    xb.xkv_landmarks_update(s, K, lengths, L, c, marks)
+    blocks = torch.empty((batch, 1, H_kv, 10), dtype=torch.int32, device="cuda")
+    xb.xkv_block_decode(s, K, V, lengths, q1, 1, marks, c, out1, blocks, ws)
+    want = ref.choose_blocks(q1[-1, 6:].cpu(), marks[-1, -1].cpu(), L, c, 10)
+    assert blocks[-1, 0, -1].tolist() == want
+    t = torch.tensor([j * c + x for j in want for x in range(c) if j * c + x < L])
+    o, _, bound, _ = ref.attend(q1[-1, 6:].cpu(), k.cpu()[t], v.cpu()[t], torch.ones((2, len(t)), dtype=torch.bool), scale_of(s))
+    within(out1[-1, 6:].cpu(), o, bound, "blocks")
+    keep = ref.keep_rows(w[-1, -1].cpu(), L, 640, 4, 100)
+    rows = torch.empty((batch, H_kv, 640), dtype=torch.int32, device="cuda")
+    xb.xkv_evict(s, K, V, w, lengths, 4, 100, L, K, V, w, rows, None, ws)
+    assert rows[-1, -1].tolist() == keep
+    assert torch.equal(K[-1, -1, :640], k[torch.tensor(keep, device="cuda")]) and torch.equal(V[-1, -1, :640], v[torch.tensor(keep, device="cuda")])
+    assert torch.equal(K[-1, -1, 640:], k[640:])
+
+
 # ---------------------------------------------------------------------------------------------------------- together
 def serve(s, c, N, steps, state, stream=None):
     """Draft, verify, append, decode with weights, evict, refresh the block means, decode sparsely; all on device lengths."""
