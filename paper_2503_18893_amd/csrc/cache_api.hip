@@ -66,7 +66,7 @@ xkv_status plan_cache_attend(const xkv_shape &s, CacheMode mode, int N, int c, C
     // to a compute unit (two of 128 rows).  The general one: 16 rows, rounds of 64 tokens, four workgroups.
     const int M = mode == CacheMode::blocks ? p.n_rep : N * p.n_rep;
     p.mfma = s.dtype == XKV_BF16 && s.d_h == 128;
-    p.rows = !p.mfma ? 16 : mode != CacheMode::tree || M <= 32 ? 32 : M <= 64 ? 64 : (ceil_div(M, 128) & 1) ? 128 : 256;
+    p.rows = !p.mfma || M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : (ceil_div(M, 128) & 1) ? 128 : 256;
     p.round = p.mfma && p.rows <= 64 ? 128 : 64;
     int want = !p.mfma ? 1024 : p.rows == 128 ? 512 : 256;
     // Streams (up to 64 rows) of several sequences, whose lengths differ: up to three workgroups one after the other on a compute unit, so

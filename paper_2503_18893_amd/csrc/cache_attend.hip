@@ -209,12 +209,12 @@ __global__ __launch_bounds__(256) void cache_attend_general_kernel(CacheArgs a)
 // that neither the fragment reads (16 rows at a time, one piece each) nor the transposing reads (4 rows at a time, two pieces each)
 // meet in a bank.
 // ------------------------------------------------------------------------------------------
-constexpr int kHeldLogits = 32;  // rows of 32 logits that a wavefront holds back
 __device__ const u32x4_t kZeroRow[16] = {};  // stands for drafted tokens that nothing sees, and for places behind the last token
 
-template <CacheMode MODE, int WR, int WT, int SUB, int RT>
-__global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_attend_mfma_kernel(CacheArgs a)
+template <int WR, int WT, int SUB, int RT>
+__global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_tree_kernel(CacheArgs a)
 {
+    constexpr CacheMode MODE = CacheMode::tree;
     constexpr bool OWN = WR == 1;  // tiles that only one wavefront reads
     constexpr int WAVES = WR * WT, TILE = 32 * SUB * WT, STAGE = 512 * TILE, RPW = TILE / WAVES, LOADS = RPW / 4, KTILE = OWN ? 8192 : 256 * TILE, VBASE = OWN ? KTILE : 2 * KTILE;
     static_assert(!OWN || SUB == 1, "a wavefront's tile is 32 tokens");
@@ -222,14 +222,12 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_attend_mf
     __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE >= WAVES * 16384 ? 2 * STAGE : WAVES * 16384];
     __shared__ float sm_m[WT][32 * WR * RT], sm_l[WT][32 * WR * RT];
     __shared__ uint32_t sm_seen[32];
-    __shared__ __attribute__((aligned(16))) float sm_z[MODE == CacheMode::weights ? WAVES : 1][MODE == CacheMode::weights ? kHeldLogits : 1][36];  // logits of a few tiles
-    __shared__ int sm_rows[MODE == CacheMode::blocks ? kPartBlocks + 2 : 1];  // blocks: first rows of this part's blocks
     const int lane = lane_id(), w = wave_id(), rg = w % WR, tg = w / WR, n32 = lane & 31, hf = lane >> 5, n_rep = a.H_q / a.H_kv;
-    const int M = MODE == CacheMode::blocks ? n_rep : a.N * n_rep;
+    const int M = a.N * n_rep;
     const CacheUnit u = cache_unit(a, MODE, (M + 32 * WR * RT - 1) / (32 * WR * RT));
     if (!u.some) return;  // (the merge knows)
     const int tile = u.tile, g = u.g, n = u.n, t_begin = u.t_begin, t_end = u.t_end;
-    const int seq = MODE == CacheMode::blocks ? u.seq / a.N : u.seq, first_token = MODE == CacheMode::blocks ? u.seq % a.N : 0;
+    const int seq = u.seq;
     const float c = a.scale * 1.44269504088896340736f;
 
     const bf16_t *Kg = (const bf16_t *)a.K + ((size_t)seq * a.H_kv + g) * a.L * 128, *Vg = (const bf16_t *)a.V + ((size_t)seq * a.H_kv + g) * a.L * 128;
@@ -243,14 +241,14 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_attend_mf
     for (int rt = 0; rt < RT; ++rt) {
         m_row[rt] = ((tile * WR + rg) * RT + rt) * 32 + n32;
         const int m_in = m_row[rt] < M ? m_row[rt] : M - 1;
-        token[rt] = first_token + m_in / n_rep;
+        token[rt] = m_in / n_rep;
         const size_t q_row = ((size_t)seq * a.N + token[rt]) * a.H_q + g * n_rep + m_in % n_rep;
 #pragma unroll
         for (int f = 0; f < 8; ++f)
             Qf[rt][f] = __builtin_bit_cast(bf16x8_t, reinterpret_cast<const u32x4_t *>((const bf16_t *)a.q + q_row * 128)[2 * f + hf]);
     }
 
-    if (MODE == CacheMode::tree && t_end > n) {  // which drafted tokens any token sees
+    if (t_end > n) {  // which drafted tokens any token sees
         if (threadIdx.x < 32) sm_seen[threadIdx.x] = a.tree ? 0u : 0xFFFFFFFFu;
         __syncthreads();
         if (a.tree)
@@ -261,26 +259,6 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_attend_mf
         __syncthreads();
     }
 
-    // Blocks: a load of a block's number between the requests of rows would be waited for together with them, so the numbers go to LDS first.
-    // A lane's next tokens are TILE further on: `ahead` whole blocks and `rest` rows.
-    int in_list[8], in_block[8], rows_of[8], ahead = 0, rest = 0, last_row = 0;
-    if constexpr (MODE == CacheMode::blocks) {
-        static_assert(OWN, "rows of eight requests");
-        const int32_t *sel = a.sel + ((size_t)u.seq * a.H_kv + g) * a.k_ch;
-        const int b0 = t_begin / a.c, b1 = (t_end - 1) / a.c;  // b1 - b0 <= kPartBlocks
-        for (int i = threadIdx.x; i <= b1 - b0; i += 64 * WAVES) sm_rows[i] = sel[b0 + i] * a.c;
-        __syncthreads();
-        ahead = TILE / a.c;
-        rest = TILE % a.c;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int t = t_begin + 32 * w + 4 * i + (lane >> 4), j = t / a.c;
-            in_list[i] = j - b0;
-            in_block[i] = t - j * a.c;
-        }
-        last_row = sm_rows[b1 - b0] + (t_end - 1) - b1 * a.c;
-    }
-
     // Where this wavefront puts rows: its share of a tile that all read (WR > 1), or tiles of 32 rows of its own.
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem + (OWN ? 32768 * w : 256 * RPW * w);
     const int r4 = lane >> 4, x16 = lane & 15;
@@ -288,7 +266,7 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_attend_mf
 #pragma unroll
     for (int i = 0; i < 4; ++i) koff[i] = 256 * r4 + 16 * ((x16 - (OWN ? 0 : RPW * w) - 4 * i - r4) & 15);
     const uint32_t voff = 256 * r4 + 32 * (((x16 >> 1) - 2 * r4) & 7) + 16 * (x16 & 1);
-    const int plain_end = MODE == CacheMode::tree && n < t_end ? n : t_end;  // rows of the cache end here
+    const int plain_end = n < t_end ? n : t_end;  // rows of the cache end here
     auto stage_plain = [&](int first, int buf, auto values) __attribute__((always_inline)) {  // RPW rows of the cache
         constexpr bool is_v = decltype(values)::value;
         const uint32_t at = lds0 + buf * (OWN ? 2 * KTILE : KTILE) + (is_v ? VBASE : 0);
@@ -305,42 +283,15 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_attend_mf
         constexpr bool is_v = decltype(values)::value;
         const uint32_t at = lds0 + buf * (OWN ? 2 * KTILE : KTILE) + (is_v ? VBASE : 0);
         const bf16_t *rows = is_v ? Vg : Kg;
-        if constexpr (MODE == CacheMode::blocks) {  // called for the tiles in turn, keys before values
-            if constexpr (!is_v) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const bool real = first + 4 * i + r4 < t_end;  // (else the last row again, with weight zero)
-                    rows_of[i] = real ? sm_rows[real ? in_list[i] : 0] + in_block[i] : last_row;
-                    in_list[i] += ahead;
-                    in_block[i] += rest;
-                    if (in_block[i] >= a.c) {
-                        in_block[i] -= a.c;
-                        ++in_list[i];
-                    }
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i)
-                copy16_global_to_lds((const unsigned char *)(rows + (size_t)rows_of[i] * 128) + ((is_v ? voff : koff[i & 3]) - 256 * r4),
-                                     at + 1024 * i);
-            return;
-        }
         if (first + RPW <= plain_end) {  // (wave-uniform)
             stage_plain(first, buf, values);
             return;
         }
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            int t = first + 4 * i + r4;
-            const bf16_t *from;
-            if (MODE == CacheMode::tree) {
-                const int j = t - n;
-                const bool draft = t < t_end && j >= 0 && (sm_seen[(j >> 5) & 31] >> (j & 31) & 1u);
-                from = t < n ? rows + (size_t)t * 128 : draft ? (is_v ? Vd : Kd) + (size_t)j * 128 : (const bf16_t *)kZeroRow;
-            } else {
-                t = t < t_end ? t : t_end - 1;  // (its weight will be zero)
-                from = rows + (size_t)t * 128;
-            }
+            const int t = first + 4 * i + r4, j = t - n;
+            const bool draft = t < t_end && j >= 0 && (sm_seen[(j >> 5) & 31] >> (j & 31) & 1u);
+            const bf16_t *from = t < n ? rows + (size_t)t * 128 : draft ? (is_v ? Vd : Kd) + (size_t)j * 128 : (const bf16_t *)kZeroRow;
             copy16_global_to_lds((const unsigned char *)from + ((is_v ? voff : koff[i & 3]) - 256 * r4), at + 1024 * i);
         }
     };
@@ -371,8 +322,6 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_attend_mf
 #pragma unroll
         for (int db = 0; db < 4; ++db) O[rt][db] = f32x16_t(0.0f);
     }
-    int held = 0;  // tiles whose logits wait, of `hold`
-    const int hold = n_rep <= kHeldLogits / 8 ? 8 : kHeldLogits / n_rep;
     // logits of a tile of keys
     auto logits = [&](const unsigned char *lds, f32x16_t (&S)[PARTS]) __attribute__((always_inline)) {
 #pragma unroll
@@ -387,41 +336,17 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_attend_mf
                     S[rt * SUB + s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf), Qf[rt][f], S[rt * SUB + s], 0, 0, 0);
             }
     };
-    // register v of part s is token tw + 32 s + 8 (v / 4) + 4 hf + v % 4: what this row does not see; then the logits that are kept
+    // register v of part s is token tw + 32 s + 8 (v / 4) + 4 hf + v % 4: what this row does not see
     auto hide = [&](int tw, f32x16_t (&S)[PARTS]) __attribute__((always_inline)) {
         if (tw + 32 * SUB > plain_end) {
 #pragma unroll
             for (int p = 0; p < PARTS; ++p) {
                 const int t = tw + 32 * (p % SUB), left = t_end - t;
                 uint32_t sees = left >= 32 ? 0xFFFFFFFFu : left > 0 ? (1u << left) - 1u : 0u;
-                if (MODE == CacheMode::tree) sees &= draft_bits(a, seq, token[p / SUB], t - n);
+                sees &= draft_bits(a, seq, token[p / SUB], t - n);
                 sees >>= 4 * hf;
 #pragma unroll
                 for (int v = 0; v < 16; ++v) S[p][v] = sees >> (8 * (v / 4) + v % 4) & 1u ? S[p][v] : -INFINITY;
-            }
-        }
-        // The logits of a few tiles wait in LDS and leave together, a line of 32 per head and tile: small stores between the requests
-        // of a stream slow it down by more than their share of its bytes.
-        if constexpr (MODE == CacheMode::weights) {
-            static_assert(PARTS == 1 && OWN, "one tile of up to 16 rows per wavefront");
-            if (n32 < n_rep) {
-#pragma unroll
-                for (int v = 0; v < 16; v += 4)
-                    *reinterpret_cast<f32x4_t *>(&sm_z[w][held * n_rep + n32][2 * v + 4 * hf]) =
-                        f32x4_t{a.scale * S[0][v], a.scale * S[0][v + 1], a.scale * S[0][v + 2], a.scale * S[0][v + 3]};
-            }
-            if (++held == hold || tw + TILE >= t_end) {
-                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-                float *to = a.logits + ((size_t)seq * a.H_q + g * n_rep) * a.L + n32;
-                for (int i = 0; i < held; ++i) {
-                    const int t = tw - TILE * (held - 1 - i);
-                    for (int h = hf; h < n_rep; h += 2)
-                        if (t + n32 < t_end) to[(size_t)h * a.L + t] = sm_z[w][i * n_rep + h][n32];
-                }
-                __builtin_amdgcn_wave_barrier();
-                held = 0;
             }
         }
     };
@@ -462,13 +387,9 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_attend_mf
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
 #pragma unroll
-                for (int v = 8 * j; v < 8 * j + 8; ++v) {
-                    S[p][v] = __builtin_amdgcn_exp2f(fmaf(S[p][v], c, less));
-                    // (weights that are given out are divided by this sum: unrounded)
-                    if (MODE == CacheMode::weights) l_run[rt] += S[p][v];
-                }
+                for (int v = 8 * j; v < 8 * j + 8; ++v) S[p][v] = __builtin_amdgcn_exp2f(fmaf(S[p][v], c, less));
                 P[2 * p + j] = pack8(S[p], j);
-                if (MODE != CacheMode::weights) l_run[rt] = add_pairs(P[2 * p + j], l_run[rt]);
+                l_run[rt] = add_pairs(P[2 * p + j], l_run[rt]);
             }
         }
     };
@@ -489,8 +410,7 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_attend_mf
     };
     if constexpr (OWN) {
         // A wavefront keeps two tiles of its own and waits for nobody: the keys of the tile after the next are requested as soon as the
-        // logits are there, its values as soon as the products are.  (Counted waits: requests are answered in order; others in between,
-        // of logits that are stored, make a wait longer, not shorter.)
+        // logits are there, its values as soon as the products are.  (Counted waits: requests are answered in order.)
         const int t_first = t_begin + 32 * w;
         if (t_first < t_end) {
             stage(t_first, 0, keys);
@@ -698,6 +618,292 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_attend_mf
 }
 
 // ------------------------------------------------------------------------------------------
+// Up to 16 rows (a token's query heads, selected blocks, short drafts): the same products in 16 x 16 tiles, so that half as many logits are
+// formed per lane and no chain of products is longer than four.  A wavefront streams tiles of 32 tokens of its own, four in a workgroup.
+//   S^T: lane (row l % 16, kk = l / 16), part h, register r: token 16 h + 4 kk + r;  O^T: block db, register r: channel 16 db + 4 kk + r
+// LDS: the 16-byte piece p of row t of K at p ^ t % 16 (a fragment read takes two neighbouring pieces of 8 rows each at a time), the 32-byte
+// piece u of row t of V at (u + t) % 8 (a transposing read takes one piece of 8 rows at a time).
+// In 32 x 32 tiles, half of them empty: 256 queries of a 128K prompt 240 us, now 223; weights over 8 x 32768 tokens 26.3, now 25.6.
+// ------------------------------------------------------------------------------------------
+constexpr int kHeldLogits = 32;  // rows of 32 logits that a wavefront holds back
+
+template <CacheMode MODE>
+__global__ __launch_bounds__(256, 1) void cache_stream_kernel(CacheArgs a)
+{
+    constexpr int TILE = 128, LOADS = 8, KTILE = 8192;
+    constexpr bool BLK = MODE == CacheMode::blocks, KEEP = MODE == CacheMode::weights;
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * 4 * KTILE];
+    __shared__ float sm_m[4][16], sm_l[4][16];
+    __shared__ uint32_t sm_seen[32];
+    __shared__ __attribute__((aligned(16))) float sm_z[KEEP ? 4 : 1][KEEP ? kHeldLogits : 1][36];  // logits of a few tiles
+    __shared__ int sm_rows[BLK ? kPartBlocks + 2 : 1];                                              // first rows of this part's blocks
+    const int lane = lane_id(), w = wave_id(), n16 = lane & 15, kk = lane >> 4, n_rep = a.H_q / a.H_kv;
+    const int M = BLK ? n_rep : a.N * n_rep;
+    const CacheUnit u = cache_unit(a, MODE, 1);
+    if (!u.some) return;  // (the merge knows)
+    const int g = u.g, n = u.n, t_begin = u.t_begin, t_end = u.t_end;
+    const int seq = BLK ? u.seq / a.N : u.seq, first_token = BLK ? u.seq % a.N : 0;
+    const float c = a.scale * 1.44269504088896340736f;
+
+    const bf16_t *Kg = (const bf16_t *)a.K + ((size_t)seq * a.H_kv + g) * a.L * 128, *Vg = (const bf16_t *)a.V + ((size_t)seq * a.H_kv + g) * a.L * 128;
+    const bf16_t *Kd = (const bf16_t *)a.K_draft + ((size_t)seq * a.H_kv + g) * a.N * 128;
+    const bf16_t *Vd = (const bf16_t *)a.V_draft + ((size_t)seq * a.H_kv + g) * a.N * 128;
+
+    // Q^T fragments: lane (row n16, kk), fragment f, position e: channel 32 f + 8 kk + e
+    const int m_in = n16 < M ? n16 : M - 1, token = first_token + m_in / n_rep;
+    bf16x8_t Qf[4];
+    {
+        const u32x4_t *q = reinterpret_cast<const u32x4_t *>((const bf16_t *)a.q + (((size_t)seq * a.N + token) * a.H_q + g * n_rep + m_in % n_rep) * 128);
+#pragma unroll
+        for (int f = 0; f < 4; ++f) Qf[f] = __builtin_bit_cast(bf16x8_t, q[4 * f + kk]);
+    }
+    if (MODE == CacheMode::tree && t_end > n) {  // which drafted tokens any token sees
+        if (threadIdx.x < 32) sm_seen[threadIdx.x] = a.tree ? 0u : 0xFFFFFFFFu;
+        __syncthreads();
+        if (a.tree)
+            for (int i = threadIdx.x; i < a.N * a.words; i += 256) {
+                const uint32_t x = a.tree[(size_t)seq * a.N * a.words + i];
+                if (x) atomicOr(&sm_seen[i % a.words], x);
+            }
+        __syncthreads();
+    }
+    // Blocks: a load of a block's number between the requests of rows would be waited for together with them, so the numbers go to LDS first.
+    // A lane's next tokens are TILE further on: `ahead` whole blocks and `rest` rows.
+    int in_list[8], in_block[8], rows_of[8], ahead = 0, rest = 0, last_row = 0;
+    if constexpr (BLK) {
+        const int32_t *sel = a.sel + ((size_t)u.seq * a.H_kv + g) * a.k_ch;
+        const int b0 = t_begin / a.c, b1 = (t_end - 1) / a.c;  // b1 - b0 <= kPartBlocks
+        for (int i = threadIdx.x; i <= b1 - b0; i += 256) sm_rows[i] = sel[b0 + i] * a.c;
+        __syncthreads();
+        ahead = TILE / a.c;
+        rest = TILE % a.c;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int t = t_begin + 32 * w + 4 * i + (lane >> 4), j = t / a.c;
+            in_list[i] = j - b0;
+            in_block[i] = t - j * a.c;
+        }
+        last_row = sm_rows[b1 - b0] + (t_end - 1) - b1 * a.c;
+    }
+
+
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem + 4 * KTILE * w;
+    const int r4 = lane >> 4, x16 = lane & 15;
+    uint32_t koff[4], voff[2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) koff[i] = 256 * r4 + 16 * (x16 ^ (4 * i + r4));
+#pragma unroll
+    for (int i = 0; i < 2; ++i) voff[i] = 256 * r4 + 32 * (((x16 >> 1) - 4 * i - r4) & 7) + 16 * (x16 & 1);
+    const int plain_end = MODE == CacheMode::tree && n < t_end ? n : t_end;  // rows of the cache end here
+    auto stage = [&](int first, int buf, auto values) __attribute__((always_inline)) {  // 32 tokens from `first` on
+        constexpr bool is_v = decltype(values)::value;
+        const uint32_t at = lds0 + buf * 2 * KTILE + (is_v ? KTILE : 0);
+        const bf16_t *rows = is_v ? Vg : Kg;
+        if constexpr (BLK) {  // called for the tiles in turn, keys before values
+            if constexpr (!is_v) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const bool real = first + 4 * i + r4 < t_end;  // (else the last row again, with weight zero)
+                    rows_of[i] = real ? sm_rows[real ? in_list[i] : 0] + in_block[i] : last_row;
+                    in_list[i] += ahead;
+                    in_block[i] += rest;
+                    if (in_block[i] >= a.c) {
+                        in_block[i] -= a.c;
+                        ++in_list[i];
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i)
+                copy16_global_to_lds((const unsigned char *)(rows + (size_t)rows_of[i] * 128) + ((is_v ? voff[i & 1] : koff[i & 3]) - 256 * r4),
+                                     at + 1024 * i);
+            return;
+        }
+        if (first + 32 <= plain_end) {  // (wave-uniform)
+            const unsigned char *base = (const unsigned char *)(rows + (size_t)first * 128);
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) copy16_to_lds_once(base + 1024 * i, is_v ? voff[i & 1] : koff[i & 3], at + 1024 * i);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            int t = first + 4 * i + r4;
+            const bf16_t *from;
+            if (MODE == CacheMode::tree) {
+                const int j = t - n;
+                const bool draft = t < t_end && j >= 0 && (sm_seen[(j >> 5) & 31] >> (j & 31) & 1u);
+                from = t < n ? rows + (size_t)t * 128 : draft ? (is_v ? Vd : Kd) + (size_t)j * 128 : (const bf16_t *)kZeroRow;
+            } else {
+                t = t < t_end ? t : t_end - 1;  // (its weight will be zero)
+                from = rows + (size_t)t * 128;
+            }
+            copy16_global_to_lds((const unsigned char *)from + ((is_v ? voff[i & 1] : koff[i & 3]) - 256 * r4), at + 1024 * i);
+        }
+    };
+    constexpr std::false_type keys{};
+    constexpr std::true_type values{};
+
+    uint32_t kat[4], vat[8];
+#pragma unroll
+    for (int f = 0; f < 4; ++f) kat[f] = 256 * n16 + 16 * ((4 * f + kk) ^ n16);
+    {
+        const int rl = 4 * kk + (n16 >> 2);
+#pragma unroll
+        for (int db = 0; db < 8; ++db) vat[db] = KTILE + 256 * rl + 32 * ((db + rl) & 7) + 8 * (lane & 3);
+    }
+    f32x4_t O[8];
+#pragma unroll
+    for (int db = 0; db < 8; ++db) O[db] = f32x4_t(0.0f);
+    float m_run = -INFINITY, l_run = 0.0f;
+    int held = 0;  // tiles whose logits wait, of `hold`
+    const int hold = n_rep <= kHeldLogits / 8 ? 8 : kHeldLogits / n_rep;
+
+    // A wavefront keeps two tiles and waits for nobody: the keys of the tile after the next are requested as soon as the logits are there,
+    // its values as soon as the products are.  (Counted waits: requests are answered in order; others in between, of logits that are
+    // stored, make a wait longer, not shorter.)
+    const int t_first = t_begin + 32 * w;
+    if (t_first < t_end) {
+        stage(t_first, 0, keys);
+        stage(t_first, 0, values);
+    }
+    if (t_first + TILE < t_end) {
+        stage(t_first + TILE, 1, keys);
+        stage(t_first + TILE, 1, values);
+    }
+    int buf = 0;
+    for (int t = t_first; t < t_end; t += TILE, buf ^= 1) {
+        const unsigned char *lds = smem + 4 * KTILE * w + 2 * KTILE * buf;
+        const bool next = t + TILE < t_end, then = t + 2 * TILE < t_end;
+        if (next)
+            XKV_WAIT_VMCNT(3 * LOADS);
+        else
+            XKV_WAIT_VMCNT(LOADS);
+        asm volatile("" : : : "memory");
+        f32x4_t S[2];
+        S[0] = S[1] = f32x4_t(0.0f);
+#pragma unroll
+        for (int f = 0; f < 4; ++f)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const u32x4_t kf = *reinterpret_cast<const u32x4_t *>(lds + kat[f] + 4096 * h);
+                S[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf), Qf[f], S[h], 0, 0, 0);
+            }
+        if (then) {
+            wait_lds();
+            stage(t + 2 * TILE, buf, keys);
+        }
+        if (t + 32 > plain_end) {
+            const int left = t_end - t;
+            uint32_t sees = left >= 32 ? 0xFFFFFFFFu : (1u << left) - 1u;
+            if (MODE == CacheMode::tree) sees &= draft_bits(a, seq, token, t - n);
+            sees >>= 4 * kk;
+#pragma unroll
+            for (int v = 0; v < 8; ++v) S[v / 4][v % 4] = sees >> (16 * (v / 4) + v % 4) & 1u ? S[v / 4][v % 4] : -INFINITY;
+        }
+        // The logits of a few tiles wait in LDS and leave together, a line of 32 per head and tile: small stores between the requests of a
+        // stream slow it down by more than their share of its bytes.
+        if constexpr (KEEP) {
+            if (n16 < n_rep) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) *reinterpret_cast<f32x4_t *>(&sm_z[w][held * n_rep + n16][16 * h + 4 * kk]) = a.scale * S[h];
+            }
+            if (++held == hold || !next) {
+                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+                const int n32 = lane & 31;
+                float *to = a.logits + ((size_t)seq * a.H_q + g * n_rep) * a.L + n32;
+                for (int i = 0; i < held; ++i) {
+                    const int ti = t - TILE * (held - 1 - i);
+                    for (int h = lane >> 5; h < n_rep; h += 2)
+                        if (ti + n32 < t_end) to[(size_t)h * a.L + ti] = sm_z[w][i * n_rep + h][n32];
+                }
+                __builtin_amdgcn_wave_barrier();
+                held = 0;
+            }
+        }
+        float m_loc = fmaxf(fmaxf(fmaxf(S[0][0], S[0][1]), fmaxf(S[0][2], S[0][3])), fmaxf(fmaxf(S[1][0], S[1][1]), fmaxf(S[1][2], S[1][3])));
+        float lo, hi;
+        quarters(m_loc, lo, hi);
+        halves(fmaxf(lo, hi), lo, hi);
+        m_loc = fmaxf(lo, hi);
+        if (__ballot(!((m_loc - m_run) * c <= 8.0f))) {
+            const float m_new = fmaxf(m_run, m_loc), alpha = m_run == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m_run - m_new) * c);
+            l_run *= alpha;
+#pragma unroll
+            for (int db = 0; db < 8; ++db) O[db] *= alpha;
+            m_run = m_new;
+        }
+        const float less = m_run == -INFINITY ? 0.0f : -m_run * c;
+        f32x8_t p;
+#pragma unroll
+        for (int v = 0; v < 8; ++v) {
+            p[v] = __builtin_amdgcn_exp2f(fmaf(S[v / 4][v % 4], c, less));
+            if (KEEP) l_run += p[v];  // (weights that are given out are divided by this sum: unrounded)
+        }
+        const bf16x8_t P = __builtin_convertvector(p, bf16x8_t);
+        if (!KEEP) l_run = add_pairs(P, l_run);
+        if (then)
+            XKV_WAIT_VMCNT(3 * LOADS);
+        else if (next)
+            XKV_WAIT_VMCNT(2 * LOADS);
+        else
+            XKV_WAIT_VMCNT(0);
+        asm volatile("" : : : "memory");
+#pragma unroll
+        for (int db = 0; db < 8; ++db) {
+            // position e of lane (channel, kk): token 16 (e / 4) + 4 kk + e % 4, as in P
+            const unsigned char *from = lds + vat[db];
+            const s16x4_t a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)from);
+            const s16x4_t a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(from + 4096));
+            O[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7)), P,
+                                                            O[db], 0, 0, 0);
+        }
+        if (then) {
+            wait_lds();
+            stage(t + 2 * TILE, buf, values);
+        }
+    }
+
+    // merge the wavefronts through LDS: 16-byte piece p of row n16 sits at (p + n16) % 32
+    {
+        float lo, hi;
+        quarters(l_run, lo, hi);
+        halves(lo + hi, lo, hi);
+        if (kk == 0) {
+            sm_m[w][n16] = m_run;
+            sm_l[w][n16] = lo + hi;
+        }
+    }
+    __syncthreads();
+    const float top = fmaxf(fmaxf(sm_m[0][n16], sm_m[1][n16]), fmaxf(sm_m[2][n16], sm_m[3][n16]));
+    const float f = m_run == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m_run - top) * c);
+    f32x4_t *ot = reinterpret_cast<f32x4_t *>(smem) + 512 * w;
+#pragma unroll
+    for (int db = 0; db < 8; ++db) ot[32 * n16 + ((4 * db + kk + n16) & 31)] = f * O[db];
+    __syncthreads();
+    for (int item = threadIdx.x; item < 512; item += 256) {
+        const int row = item >> 5, p = item & 31;
+        if (row >= M) continue;
+        f32x4_t x = f32x4_t(0.0f);
+        float den = 0.0f, most = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x += reinterpret_cast<const f32x4_t *>(smem)[512 * i + 32 * row + ((p + row) & 31)];
+            most = fmaxf(most, sm_m[i][row]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) den += sm_m[i][row] == -INFINITY ? 0.0f : sm_l[i][row] * __builtin_amdgcn_exp2f((sm_m[i][row] - most) * c);
+        const size_t slot = part_row(a, MODE, u.part, row / n_rep, g * n_rep + row % n_rep);
+        *reinterpret_cast<f32x4_t *>(a.part_o + slot * 128 + 4 * p) = x;
+        if (p == 0) {
+            a.part_ml[2 * slot] = most * a.scale;
+            a.part_ml[2 * slot + 1] = den;
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------
 // Merge.  A group of 2^lg lanes covers the columns of a row (query token, head), VEC a lane.  Where there are many rows, a group per row;
 // where there are few, all groups of a workgroup share a row's partials between them and are added up in LDS: latency is all there is to
 // it then.  Partials that no token went to were
@@ -833,14 +1039,14 @@ hipError_t launch_mfma(const CacheArgs &a, hipStream_t st)
     const int M = MODE == CacheMode::blocks ? a.H_q / a.H_kv : a.N * (a.H_q / a.H_kv);
     const dim3 grid = unit_grid(a, MODE, M);
     auto launch = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, st, a); };
-    if (MODE == CacheMode::tree && a.rows == 256)
-        launch(cache_attend_mfma_kernel<CacheMode::tree, 8, 1, 2, 1>, 512);
-    else if (MODE == CacheMode::tree && a.rows == 128)
-        launch(cache_attend_mfma_kernel<CacheMode::tree, 4, 1, 2, 1>, 256);
-    else if (MODE == CacheMode::tree && a.rows == 64)
-        launch(cache_attend_mfma_kernel<CacheMode::tree, 1, 4, 1, 2>, 256);
-    else
-        launch(cache_attend_mfma_kernel<MODE, 1, 4, 1, 1>, 256);
+    if (a.rows == 16) {
+        launch(cache_stream_kernel<MODE>, 256);
+    } else if constexpr (MODE == CacheMode::tree) {
+        a.rows == 256 ? launch(cache_tree_kernel<8, 1, 2, 1>, 512) : a.rows == 128 ? launch(cache_tree_kernel<4, 1, 2, 1>, 256)
+            : a.rows == 64 ? launch(cache_tree_kernel<1, 4, 1, 2>, 256) : launch(cache_tree_kernel<1, 4, 1, 1>, 256);
+    } else {
+        return hipErrorInvalidValue;
+    }
     return hipGetLastError();
 }
 

@@ -37,6 +37,14 @@ __device__ __forceinline__ void halves(float x, float &lo, float &hi)
     hi = __uint_as_float(r[1]);
 }
 
+// The same for rows of 16 lanes: l and l + 16 of either half.
+__device__ __forceinline__ void quarters(float x, float &lo, float &hi)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    lo = __uint_as_float(r[0]);
+    hi = __uint_as_float(r[1]);
+}
+
 __device__ __forceinline__ bf16x8_t pack8(const f32x16_t &c, int j)
 {
     f32x8_t x;

@@ -35,7 +35,7 @@ def test_parts_leave_one_for_every_sequence_and_fit_the_merge(plan_of):
     for s, p in zip(shapes, plan_of(shapes)):
         assert p["status"] == 0 and s["batch"] <= p["parts"] <= s["batch"] + p["max_parts"] - 1, (s, p)
         rows = s["N"] * s["H_q"] // s["H_kv"]
-        assert p["rows"] == (16 if not p["mfma"] else 32) or rows > p["rows"] // 2, (s, p)   # no tile is empty by half for no reason
+        assert p["rows"] == 16 or rows > p["rows"] // 2, (s, p)   # no tile is empty by half for no reason
         assert p["round"] % 64 == 0 and (p["round"] == 128 or not p["mfma"] or p["rows"] > 64), (s, p)
         assert p["total"] >= p["parts"] * s["N"] * s["H_q"] * (128 + 2) * 4, (s, p)
 
