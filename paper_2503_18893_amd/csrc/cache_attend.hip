@@ -38,8 +38,7 @@ __device__ __forceinline__ uint32_t draft_bits(const CacheArgs &a, int seq, int 
 // ------------------------------------------------------------------------------------------
 // General path, any type, width and alignment.  A round takes 64 tokens, whose keys and values go to LDS in single precision (the
 // next round's are requested before this one is computed).  For the logits a lane multiplies one of the keys with the four queries
-// of its wavefront, four channels a time; for the sums lanes run over the channels, and the weights come from the lanes that
-// hold them.  With few rows its time is that of one round, latencies: 8 drafted tokens of 4 heads after 512 tokens, fp32.
+// of its wavefront, four channels a time; for the sums lanes run over the channels, and the weights go through LDS.  With few rows its time is that of one round, latencies: 8 drafted tokens of 4 heads after 512 tokens, fp32.
 // ------------------------------------------------------------------------------------------
 __host__ __device__ inline int general_pitch(int d) { return ((d + 3) / 4 | 1) * 4; }  // floats; an odd number of 16-byte pieces
 
@@ -55,7 +54,7 @@ __global__ __launch_bounds__(256) void cache_attend_general_kernel(CacheArgs a)
     const int tile = u.tile, g = u.g, n = u.n, t_begin = u.t_begin, t_end = u.t_end;
     // blocks: one query token; else all query tokens of a sequence
     const int seq = MODE == CacheMode::blocks ? u.seq / a.N : u.seq, first_token = MODE == CacheMode::blocks ? u.seq % a.N : 0;
-    float *kt = smem_f, *vt = kt + kGenTokens * pitch, *qs = vt + kGenTokens * pitch;
+    float *kt = smem_f, *vt = kt + kGenTokens * pitch, *qs = vt + kGenTokens * pitch, *ps = qs + kGenRows * d4;
 
     const T *Kg = (const T *)a.K + ((size_t)seq * a.H_kv + g) * a.L * d, *Vg = (const T *)a.V + ((size_t)seq * a.H_kv + g) * a.L * d;
     const T *Kd = (const T *)a.K_draft + ((size_t)seq * a.H_kv + g) * a.N * d, *Vd = (const T *)a.V_draft + ((size_t)seq * a.H_kv + g) * a.N * d;
@@ -106,6 +105,11 @@ __global__ __launch_bounds__(256) void cache_attend_general_kernel(CacheArgs a)
     for (int t0 = t_begin; t0 < t_end; t0 += kGenTokens) {
         const int t = t0 + lane < t_end ? t0 + lane : t_end - 1;
         const bool real = t0 + lane < t_end;
+        uint32_t bits[4] = {1u, 1u, 1u, 1u};  // tree: whether the rows see this lane's token (requested here, used after the logits)
+        if (MODE == CacheMode::tree && t0 + kGenTokens > n) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) bits[r] = draft_bits(a, seq, token[r], t - n);
+        }
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < PER_WAVE; ++i)
@@ -120,6 +124,7 @@ __global__ __launch_bounds__(256) void cache_attend_general_kernel(CacheArgs a)
         __syncthreads();
         if (t0 + kGenTokens < t_end) request(row_of(t0 + kGenTokens));
         float p[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
         for (int j = 0; j < d4; j += 4) {
             const float4 x = *reinterpret_cast<const float4 *>(kt + lane * pitch + j);
 #pragma unroll
@@ -135,14 +140,10 @@ __global__ __launch_bounds__(256) void cache_attend_general_kernel(CacheArgs a)
             if (MODE == CacheMode::weights && real && m0 + r < M) a.logits[row_id[r] * a.L + t] = z[r];
             if (!real) z[r] = -INFINITY;
         }
-        if (MODE == CacheMode::tree && t0 + kGenTokens > n) {
-            uint32_t bits[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) bits[r] = draft_bits(a, seq, token[r], t - n);
+        if (MODE == CacheMode::tree) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) z[r] = bits[r] & 1u ? z[r] : -INFINITY;
         }
-        int used = 0;
 #pragma unroll
         for (int r = 0; r < 4; ++r) top[r] = wave_all(z[r], MaxOp());
 #pragma unroll
@@ -150,34 +151,42 @@ __global__ __launch_bounds__(256) void cache_attend_general_kernel(CacheArgs a)
             const float m_new = fmaxf(mx[r], top[r]);
             const float alpha = m_new == -INFINITY ? 1.0f : expf(mx[r] - m_new);
             p[r] = z[r] == -INFINITY ? 0.0f : expf(z[r] - m_new);
-            used |= z[r] != -INFINITY;
             den[r] = den[r] * alpha + wave_all(p[r], AddOp());
             mx[r] = m_new;
 #pragma unroll
             for (int jj = 0; jj < JP; ++jj) o[r][jj] *= alpha;
         }
+        // the four weights of a token to every lane
+        *reinterpret_cast<float4 *>(ps + 4 * (64 * w + lane)) = float4{p[0], p[1], p[2], p[3]};
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         const int count = t_end - t0 < kGenTokens ? t_end - t0 : kGenTokens;
-        for (int i0 = 0; i0 < count; i0 += 8) {  // (lanes from `count` on hold the last token again, with weight zero)
+        for (int i0 = 0; i0 < count; i0 += 8) {  // (places from `count` on hold the last token again, with weight zero)
             float v[8][JP];
+            float4 y[8];
 #pragma unroll
             for (int x = 0; x < 8; ++x) {
-                // a drafted token that none of these rows sees may be padding with anything in it
-                const bool use = __builtin_amdgcn_readlane(used, i0 + x) != 0;
+                y[x] = *reinterpret_cast<const float4 *>(ps + 4 * (64 * w + i0 + x));
 #pragma unroll
                 for (int jj = 0; jj < JP; ++jj) {
                     const int j = lane + jj * kWave;
-                    const float y = vt[(i0 + x) * pitch + (j < d ? j : 0)];
-                    v[x][jj] = use ? y : 0.0f;
+                    v[x][jj] = vt[(i0 + x) * pitch + (j < d ? j : 0)];
                 }
             }
 #pragma unroll
-            for (int x = 0; x < 8; ++x)
+            for (int x = 0; x < 8; ++x) {
+                // a drafted token that none of these rows sees may be padding with anything in it
+                const bool use = MODE != CacheMode::tree || y[x].x + y[x].y + y[x].z + y[x].w > 0.0f;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float pw = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(p[r]), i0 + x));
-#pragma unroll
-                    for (int jj = 0; jj < JP; ++jj) o[r][jj] = fmaf(pw, v[x][jj], o[r][jj]);
+                for (int jj = 0; jj < JP; ++jj) {
+                    const float vv = use ? v[x][jj] : 0.0f;
+                    o[0][jj] = fmaf(y[x].x, vv, o[0][jj]);
+                    o[1][jj] = fmaf(y[x].y, vv, o[1][jj]);
+                    o[2][jj] = fmaf(y[x].z, vv, o[2][jj]);
+                    o[3][jj] = fmaf(y[x].w, vv, o[3][jj]);
                 }
+            }
         }
     }
 #pragma unroll
@@ -640,7 +649,12 @@ __global__ __launch_bounds__(256, 1) void cache_stream_kernel(CacheArgs a)
     const int lane = lane_id(), w = wave_id(), n16 = lane & 15, kk = lane >> 4, n_rep = a.H_q / a.H_kv;
     const int M = BLK ? n_rep : a.N * n_rep;
     const CacheUnit u = cache_unit(a, MODE, 1);
-    if (!u.some) return;  // (the merge knows)
+    const bool direct = BLK && a.parts == 1;  // a query's only part: the result instead of a partial
+    if (!u.some) {  // (the merge knows)
+        if (direct)
+            for (int i = threadIdx.x; i < n_rep * 128; i += 256) ((bf16_t *)a.out)[((size_t)u.seq * a.H_q + u.g * n_rep) * 128 + i] = 0;
+        return;
+    }
     const int g = u.g, n = u.n, t_begin = u.t_begin, t_end = u.t_end;
     const int seq = BLK ? u.seq / a.N : u.seq, first_token = BLK ? u.seq % a.N : 0;
     const float c = a.scale * 1.44269504088896340736f;
@@ -894,6 +908,12 @@ __global__ __launch_bounds__(256, 1) void cache_stream_kernel(CacheArgs a)
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) den += sm_m[i][row] == -INFINITY ? 0.0f : sm_l[i][row] * __builtin_amdgcn_exp2f((sm_m[i][row] - most) * c);
+        if (direct) {
+            bf16_t *out = (bf16_t *)a.out + ((size_t)u.seq * a.H_q + g * n_rep + row) * 128 + 4 * p;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) out[e] = f32_to_bf16(x[e] / den);
+            continue;
+        }
         const size_t slot = part_row(a, MODE, u.part, row / n_rep, g * n_rep + row % n_rep);
         *reinterpret_cast<f32x4_t *>(a.part_o + slot * 128 + 4 * p) = x;
         if (p == 0) {
@@ -1021,9 +1041,9 @@ hipError_t launch_general(const CacheArgs &a, hipStream_t st)
 {
     const int M = MODE == CacheMode::blocks ? a.H_q / a.H_kv : a.N * (a.H_q / a.H_kv);
     const dim3 grid = unit_grid(a, MODE, M);
-    const size_t lds = (2 * (size_t)kGenTokens * general_pitch(a.d_h) + (size_t)kGenRows * ((a.d_h + 3) / 4 * 4)) * sizeof(float);
+    const size_t lds = (2 * (size_t)kGenTokens * general_pitch(a.d_h) + (size_t)kGenRows * ((a.d_h + 3) / 4 * 4) + 4 * 4 * kGenTokens) * sizeof(float);
     auto launch = [&](auto kernel, DynamicLdsOnce &attr) {
-        const hipError_t e = attr.ensure((const void *)kernel, 160 * 1024);  // (at most 146 KiB, at 256 channels)
+        const hipError_t e = attr.ensure((const void *)kernel, 160 * 1024);  // (at most 150 KiB, at 256 channels)
         if (e != hipSuccess) return e;
         hipLaunchKernelGGL(kernel, grid, dim3(256), lds, st, a);
         return hipGetLastError();
@@ -1056,9 +1076,10 @@ hipError_t launch_mode(const xkv_shape &s, const CacheArgs &a, hipStream_t st)
     const uintptr_t bits = (uintptr_t)a.K | (uintptr_t)a.V | (uintptr_t)a.q | (uintptr_t)a.K_draft | (uintptr_t)a.V_draft;
     CacheArgs gen = a;
     gen.rows = kGenRows;  // (its rounds divide those of the plan)
-    hipError_t e = a.mfma && bits % 16 == 0 ? launch_mfma<MODE>(a, st)
+    const bool matrix = a.mfma && bits % 16 == 0;
+    hipError_t e = matrix ? launch_mfma<MODE>(a, st)
                  : s.dtype == XKV_F32 ? launch_general<MODE, float>(gen, st) : launch_general<MODE, bf16_t>(gen, st);
-    if (e != hipSuccess) return e;
+    if (e != hipSuccess || (MODE == CacheMode::blocks && a.parts == 1 && matrix)) return e;
     const int vec = a.d_h % 4 == 0 ? 4 : 1, rows = a.batch * a.N * a.H_q;
     int lg = 3;
     while (lg < 6 && (vec << lg) < a.d_h) ++lg;

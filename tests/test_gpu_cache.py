@@ -153,6 +153,7 @@ BLOCKS = {
     "bf16_everything": ("bf16", 2, 4, 128, 700, 1, 32, 700, [[700], [333]]),
     "bf16_only_its_own": ("bf16", 2, 4, 128, 700, 1, 64, 64, [[700], [641], [640]]),
     "bf16_prompt": ("bf16", 2, 4, 128, 600, 40, 16, 128, [list(range(561, 601)), list(range(0, 40))]),
+    "bf16_prompt_in_one_part": ("bf16", 2, 4, 128, 300, 150, 16, 64, [list(range(0, 150)), list(range(151, 301))]),
     "bf16_large_blocks": ("bf16", 1, 4, 128, 6000, 1, 500, 2000, [[6000], [5555]]),
     "bf16_one_head": ("bf16", 3, 1, 128, 2000, 3, 64, 640, [[2000, 1990, 64]]),
 }
