@@ -481,6 +481,7 @@ __global__ __launch_bounds__(256) void landmarks_update_kernel(const T *__restri
     const float inv = 1.0f / (float)(t1 - t0);
     for (int e = lane; e < d; e += kWave) {
         float sum = 0.0f;
+#pragma unroll 8
         for (int t = t0; t < t1; ++t) sum += to_f32(K[((size_t)row * L + t) * d + e]);
         landmarks[((size_t)row * n_c + j) * d + e] = from_f32<T>(sum * inv);
     }

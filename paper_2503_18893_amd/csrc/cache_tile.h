@@ -26,8 +26,8 @@ __device__ __forceinline__ void copy16_to_lds_once(const void *base, uint32_t of
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" : : "s"(lds_base), "v"(off), "s"(base) : "memory", "m0");
 }
 
-// s_waitcnt for LDS reads alone (see XKV_WAIT_VMCNT): what they read may be overwritten after it.
-__device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(0xF | (7 << 4) | (3 << 14)); }
+// Waits for LDS reads alone: what they read may be overwritten after it (and none of them is moved behind it).
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
 
 // Both halves of a wavefront see the other's value as well: max or sum of lanes l and l + 32, in both.
 __device__ __forceinline__ void halves(float x, float &lo, float &hi)

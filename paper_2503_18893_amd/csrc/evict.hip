@@ -224,18 +224,23 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, int pieces
     int src[2][kMoveRows];  // -1: nothing to move
     float w[2][kMoveRows];  // of rows i0 + 256 u + threadIdx.x of a step
     int wsrc[2][kMoveRows];
+    int later[kMoveRows];  // entries of sel for the step that is read next
+    auto look_up = [&](int i0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < kMoveRows; ++u) later[u] = sel[i0 + u * at_once + r0 < a.k ? i0 + u * at_once + r0 : a.k - 1];
+    };
     auto read = [&](int i0, int s) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < kMoveRows; ++u) {
             const int i = i0 + u * at_once + r0;
-            src[s][u] = mine && i < m ? sel[i] : -1;
-            if (src[s][u] == i) src[s][u] = -1;
+            src[s][u] = mine && i < m && later[u] != i ? later[u] : -1;
         }
 #pragma unroll
         for (int u = 0; u < kMoveRows; ++u) {
             x[s][u] = P{};
             if (src[s][u] >= 0) x[s][u] = rows[(size_t)src[s][u] * pieces];
         }
+        look_up(i0 + step);
         if (head) {
 #pragma unroll
             for (int u = 0; u < kMoveRows; ++u) {
@@ -267,6 +272,7 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, int pieces
             }
         }
     };
+    look_up(0);
     read(0, 0);
     for (int i0 = 0; i0 < a.k; i0 += 2 * step) {
 #pragma unroll
