@@ -7,7 +7,8 @@ namespace {
 
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
 
-// What the selection of longer rows (launch_topk) goes by: the weight, +inf for rows that are kept anyway, and below every number for rows that are not in use.
+// What the selection of longer rows (launch_topk) goes by, numbers whose order keys are: the largest key for rows that are kept anyway, the
+// smallest one for rows that are not in use (behind those in use, whose places are smaller), and the weight's own between the two.
 __global__ __launch_bounds__(256) void evict_keys_kernel(EvictArgs a)
 {
     const int t = blockIdx.x * 256 + threadIdx.x, row = blockIdx.y, b = row / a.H_kv;
@@ -16,7 +17,11 @@ __global__ __launch_bounds__(256) void evict_keys_kernel(EvictArgs a)
     if (t == 0 && row == b * a.H_kv) a.n[b] = n;
     if (t >= a.L) return;
     const size_t at = (size_t)row * a.L + t;
-    a.keys[at] = t >= n ? -INFINITY : (t < a.sink || t >= n - a.recent) ? INFINITY : a.weights[at];
+    const float x = a.weights[at];
+    const uint32_t key = order_key(x);
+    const bool kept = t < a.sink || t >= n - a.recent;
+    const float first = __uint_as_float(0x7FFFFFFFu), before = __uint_as_float(0x7FFFFFFEu), last = __uint_as_float(0xFFFFFFFEu);  // keys 2^32 - 1, 2^32 - 2, 1
+    a.keys[at] = t >= n ? last : kept ? first : key == 0xFFFFFFFFu ? before : key < 1u ? last : x;
 }
 
 // The rows that stay, for caches of up to 1024 KPT rows: one workgroup per (sequence, KV head), the order keys of the weights in

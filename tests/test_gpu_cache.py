@@ -375,6 +375,31 @@ def test_evict_without_optional_results_and_lengths():
         assert torch.equal(Kc.cpu()[0, h, :77], K[0, h, keep]) and torch.equal(wc.cpu()[0, h, :77], w[0, h, keep])
 
 
+@pytest.mark.parametrize("L,lengths", [(5000, [5000, 3000]), (20000, [20000, 700]), (40000, [40000, 1000, 900])])
+def test_evict_weights_that_are_no_numbers(L, lengths):
+    """Infinities and NaN of both signs are ordered by their bits like the rest, below the rows that stay anyway.  (The two NaN at either
+    end of that order count as one: only one of each end is here.)"""
+    k, sink, recent = 1000, 5, 300
+    s = shape_of(2, 1, 16, L, len(lengths), "f32", k=k)
+    g, K, V = cache(s, lengths, 61)
+    w = torch.rand((s.batch, 2, L), generator=g)
+    odd = torch.tensor([0x7F800000, 0x7FC00000, 0x7FFFFFFF, 0x7F800001, -0x800000, -0x400000, -1, -3], dtype=torch.int32).view(torch.float32)
+    for b, n in enumerate(lengths):
+        for h in range(2):
+            at = torch.randperm(n, generator=g)[: n // 2 if h else 40]
+            w[b, h, at] = odd[torch.randint(0, 8, (len(at),), generator=g)]
+    w[0, 1, :lengths[0]] = odd[torch.randint(4, 8, (lengths[0],), generator=g)]  # nothing but negative ones
+    rows = torch.full((s.batch, 2, k), -9, dtype=torch.int32, device="cuda")
+    dst = [torch.zeros((s.batch, 2, k, 16), device="cuda") for _ in "KV"] + [torch.zeros((s.batch, 2, k), device="cuda")]
+    xb.xkv_evict(s, K.cuda(), V.cuda(), w.cuda(), ints(lengths), sink, recent, k, *dst, rows, None, workspace(s))
+    torch.cuda.synchronize()
+    for b, n in enumerate(lengths):
+        for h in range(2):
+            keep = ref.keep_rows(w[b, h], n, k, sink, recent)
+            assert rows[b, h].tolist() == keep + [-1] * (k - len(keep)), (b, h)
+            assert torch.equal(dst[0].cpu()[b, h, :len(keep)], K[b, h, keep])
+
+
 # ------------------------------------------------------------------------------------------------- shapes of a program
 @pytest.mark.parametrize("dtype,d,batch,H_kv", [("f32", 64, 100, 1), ("bf16", 128, 100, 1), ("bf16", 128, 300, 2)])
 def test_one_long_sequence_among_empty_ones(dtype, d, batch, H_kv):
