@@ -4,9 +4,12 @@
 namespace xkv {
 namespace {
 
-// S[j] = max over the query heads of a KV head of <q_h, mean_j>; +inf for the block that ends with the query's last visible row,
-// -inf for those behind it.  The sums decide which block is read, so they are taken in double precision and rounded once to
-// single: then the order of addition does not show in the selection.  A wavefront per block, lanes over the channels.
+// The score of the block that ends with the query's last visible row: the number with the largest order key, above +inf.
+#define XKV_OWN_BLOCK __uint_as_float(0x7FFFFFFFu)
+
+// S[j] = max over the query heads of a KV head of <q_h, mean_j>; XKV_OWN_BLOCK for the query's own, -inf for those behind it.  The sums
+// decide which block is read, so they are taken in double precision and rounded once to single: then the order of addition does not
+// show in the selection.  A wavefront per block, lanes over the channels.
 template <typename T>
 __global__ __launch_bounds__(256) void block_scores_kernel(CacheArgs a, const T *__restrict__ landmarks, float *__restrict__ scores,
                                                            int n_c)
@@ -15,7 +18,7 @@ __global__ __launch_bounds__(256) void block_scores_kernel(CacheArgs a, const T 
     const int v = cache_rows(a, z), last = v > 0 ? (v - 1) / a.c : -1;
     const T *q = (const T *)a.q + ((size_t)z * a.H_q + g * n_rep) * d;
     for (int j = blockIdx.x * 4 + w; j < n_c; j += gridDim.x * 4) {
-        float best = j == last ? INFINITY : -INFINITY;
+        float best = j == last ? XKV_OWN_BLOCK : -INFINITY;
         if (j < last) {
             const T *m = landmarks + (((size_t)b * a.H_kv + g) * n_c + j) * d;
             for (int h = 0; h < n_rep; ++h) {
@@ -89,7 +92,7 @@ __global__ __launch_bounds__(256) void block_scores_mfma_kernel(CacheArgs a, con
             const int j = j0 + i16, z = b * a.N + t0 + i, v = cache_rows(a, z), last = v > 0 ? (v - 1) / a.c : -1;
             float best = -INFINITY;
             for (int h = 0; h < n_rep; ++h) best = fmaxf(best, sm[w][i16][i * n_rep + h]);
-            best = j < last ? best : j == last ? INFINITY : -INFINITY;
+            best = j < last ? best : j == last ? XKV_OWN_BLOCK : -INFINITY;
             if (j < n_c) scores[((size_t)z * a.H_kv + g) * n_c + j] = best;
         }
     }

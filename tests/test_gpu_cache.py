@@ -219,6 +219,26 @@ def test_blocks_whose_scores_lie_close_together(L, c, k, spread):
         assert blocks.cpu()[b, 0, 0].tolist() == ref.choose_blocks(q[b, 0], marks[b, 0], visible[b], c, k_ch)
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64), ("f32", 20)])
+@pytest.mark.parametrize("L", [3000, 17000])
+def test_blocks_whose_scores_overflow(dtype, d, L):
+    """Scores that are infinite in single precision rank like any other; the query's own block is read all the same."""
+    k = 50
+    s = shape_of(1, 2, d, L, 2, dtype, k=k)
+    g, K, V = cache(s, [L, L], 71)
+    marks = torch.randn((2, 1, L, d), generator=g)
+    marks[:, :, ::5] *= 1e20
+    marks[1, :, 7] = float("nan")  # a mean that is no number counts below all others
+    q = torch.randn((2, 2, d), generator=g) * 1e20
+    q, marks = q.to(DT[dtype]), marks.to(DT[dtype])
+    out, blocks = torch.empty((2, 2, d), dtype=DT[dtype], device="cuda"), torch.empty((2, 1, 1, k), dtype=torch.int32, device="cuda")
+    xb.xkv_block_decode(s, K.cuda(), V.cuda(), None, q.cuda(), 1, marks.cuda(), 1, out, blocks, workspace(s, 1, 1))
+    torch.cuda.synchronize()
+    marks[1, :, 7] = 0.0  # (among hundreds of positive scores neither this nor a NaN is chosen)
+    for b in range(2):
+        assert blocks.cpu()[b, 0, 0].tolist() == ref.choose_blocks(q[b], marks[b, 0], L, 1, k), b
+
+
 def test_blocks_tie_towards_the_smaller_block():
     s = shape_of(1, 2, 128, 320, 1, "bf16", k=64)
     g, K, V = cache(s, [320], 9)
