@@ -416,8 +416,8 @@ XKV_API xkv_status xkv_sr_decode_absorbed_q4(const xkv_shape *shape, int32_t lay
  * workspace: xkv_cache_workspace_bytes(shape, N, c) bytes, 256-byte aligned, for any of these calls with this shape, N query tokens
  *   and blocks of c rows (c = 0: no xkv_block_decode).
  * XKV_ERR_INVALID_ARG for N < 1, c < 1 (xkv_block_decode, xkv_landmarks_update), sink or recent < 0, sink + recent > k, L_out < k, or only
- * part of an eviction in place; XKV_ERR_UNSUPPORTED where batch * N * H_kv > 65535, L + N or the rows of a query's blocks exceed 2^30,
- * a query has more than 491520 blocks, or for more drafted tokens than above.
+ * part of an eviction in place; XKV_ERR_UNSUPPORTED where batch * N * H_kv > 65535, L + N (xkv_landmarks_update, xkv_evict: L) or the rows
+ * of a query's blocks exceed 2^30, a query has more than 491520 blocks, or for more drafted tokens than above.
  */
 XKV_API xkv_status xkv_cache_workspace_bytes(const xkv_shape *shape, int32_t N, int32_t c, size_t *bytes);
 XKV_API xkv_status xkv_tree_decode(const xkv_shape *shape, const void *K, const void *V, const int32_t *lengths, const void *q,

@@ -12,7 +12,8 @@ static inline int clampi(int x, int lo, int hi) { return x < lo ? lo : (x > hi ?
 template <typename T> static inline T *at(void *ws, size_t off) { return reinterpret_cast<T *>((char *)ws + off); }
 static inline xkv_status hip_status(hipError_t e) { return e == hipSuccess ? XKV_OK : XKV_ERR_HIP; }
 
-constexpr int kMaxDraft = 1024;  // drafted tokens of a sequence
+constexpr int kMaxDraft = 1024;        // drafted tokens of a sequence
+constexpr int kMaxPlaces = 1 << 30;    // rows and drafted tokens of a sequence: sums of two places are ints
 
 // Scratch of launch_topk for p.sel_shape, and room for what it selects from and for the ids.
 static size_t plan_selection(CachePlan &p, size_t off)
@@ -40,7 +41,7 @@ xkv_status plan_cache_attend(const xkv_shape &s, CacheMode mode, int N, int c, C
     p.scale = s.scale > 0.0f ? s.scale : 1.0f / std::sqrt((float)s.d_h);
     const long long batch = s.batch > 0 ? s.batch : 1;
     if (batch * N * s.H_kv > 65535LL) return XKV_ERR_UNSUPPORTED;  // rows of the selection and of the merge are y of a grid
-    if ((long long)s.L + N > (1LL << 30)) return XKV_ERR_UNSUPPORTED;  // (sums of two places in a sequence are ints)
+    if ((long long)s.L + N > kMaxPlaces) return XKV_ERR_UNSUPPORTED;
     size_t off = 0;
     long long most = s.L + (mode == CacheMode::tree ? N : 0);  // tokens of a query
     if (mode == CacheMode::blocks) {
@@ -48,7 +49,7 @@ xkv_status plan_cache_attend(const xkv_shape &s, CacheMode mode, int N, int c, C
         p.n_c = ceil_div(s.L, c);
         p.k_ch = ceil_div(s.k, c) < p.n_c ? ceil_div(s.k, c) : p.n_c;
         if ((long long)p.k_ch * c < most) most = (long long)p.k_ch * c;
-        if ((long long)p.k_ch * c > (1LL << 30)) return XKV_ERR_UNSUPPORTED;
+        if ((long long)p.k_ch * c > kMaxPlaces) return XKV_ERR_UNSUPPORTED;
         p.sel_shape = xkv_shape{1, s.H_kv, s.H_kv, 1, 1, 1, p.n_c, p.k_ch, (int32_t)(batch * N), XKV_F32, 1.0f};
         if (block_select_ok(p.n_c)) {
             const size_t rows = (size_t)batch * N * s.H_kv;
@@ -63,7 +64,9 @@ xkv_status plan_cache_attend(const xkv_shape &s, CacheMode mode, int N, int c, C
         }
     }
     // The matrix-core kernel: as many rows per workgroup as there are, up to 256 (128 where that leaves fewer of them empty), one workgroup
-    // to a compute unit (two of 128 rows).  The general one: 16 rows, rounds of 64 tokens, four workgroups.
+    // to a compute unit (two of 128 rows).  The general one: 16 rows, rounds of 64 tokens, four workgroups.  384 rows by 128 / by 256, us:
+    // one sequence of 32768 tokens 81 / 85, four of 65536 513 / 570, two of 9457 67 / 57, two of 1000 36 / 33; 640 rows, 32768 tokens 134 /
+    // 172; just over 256 rows it makes no difference at 32768 tokens (260 rows 73 / 74), and 280 rows of four sequences 231 / 266.
     const int M = mode == CacheMode::blocks ? p.n_rep : N * p.n_rep;
     p.mfma = s.dtype == XKV_BF16 && s.d_h == 128;
     p.rows = !p.mfma || M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : (ceil_div(M, 128) & 1) ? 128 : 256;
@@ -103,6 +106,7 @@ xkv_status plan_cache_attend(const xkv_shape &s, CacheMode mode, int N, int c, C
 xkv_status plan_evict(const xkv_shape &s, CachePlan &p)
 {
     std::memset(&p, 0, sizeof p);
+    if (s.L > kMaxPlaces) return XKV_ERR_UNSUPPORTED;
     p.sel_shape = xkv_shape{1, s.H_kv, s.H_kv, 1, 1, 1, s.L, s.k, s.batch > 0 ? s.batch : 1, XKV_F32, 1.0f};
     if (evict_select_ok(s.L))
         p.off_n = align_up((size_t)p.sel_shape.batch * s.H_kv * s.k * sizeof(int32_t), 256);  // the rows, at 0
@@ -233,6 +237,7 @@ xkv_status xkv_landmarks_update(const xkv_shape *shape, const void *K, const int
     xkv_status st = validate(shape);
     if (st != XKV_OK) return st;
     if (N < 1 || c < 1 || !K || !landmarks) return XKV_ERR_INVALID_ARG;
+    if (shape->L > kMaxPlaces) return XKV_ERR_UNSUPPORTED;
     if (shape->batch == 0) return XKV_OK;
     return hip_status(launch_landmarks_update(*shape, K, lengths, N, c, landmarks, (hipStream_t)hip_stream));
 }

@@ -85,6 +85,12 @@ def test_counts_are_checked():
     assert tree(long) == block(long) == weights(long) == xb.XKV_ERR_UNSUPPORTED
 
 
+def test_caches_that_are_too_long_are_refused():
+    for call in (tree, block, weights, evict, update):
+        assert call(shape(L=2 ** 30 + 1)) == xb.XKV_ERR_UNSUPPORTED, call.__name__
+        assert call(shape(L=2 ** 31 - 1)) == xb.XKV_ERR_UNSUPPORTED, call.__name__
+
+
 def test_evictions_are_checked():
     s = shape()
     assert evict(s, sink=-1) == evict(s, recent=-1) == xb.XKV_ERR_INVALID_ARG
