@@ -95,34 +95,42 @@ struct UMaxOp {
 __device__ __forceinline__ int ceil_div_dev(int a, int b) { return (int)(((unsigned)a + (unsigned)b - 1u) / (unsigned)b); }
 
 // Tokens per part.  All lanes of a wavefront call it together; t: tokens of sequence `lane` (of the first 64).
+// In rounds: r_i of sequence i, at most 2^24, R altogether.  Parts of m rounds number sum ceil(r_i / m), between R / m and R / m + batch,
+// so m is at least R / parts, and R / (parts - batch) is enough.  A lane counts for one m between the two.  Divisions are
+// products with a reciprocal, a factor of 1 + 2^-20 upwards: never too few, and exact up to 2^20 rounds of a sequence ((r + m - 1) / m
+// is a multiple of 1 / m).
 __device__ __forceinline__ int cache_chunk(const CacheArgs &a, CacheMode mode, int t)
 {
-    const int lane = lane_id();
-    long long total = 0;  // (of 64 sequences: in whole 4096s and the rest)
-    int most = 0;
+    const int lane = lane_id(), shift = __builtin_ctz(a.round);  // (a power of two)
+    constexpr float UP = 1.0f + 0x1p-20f;
+    int r = 0, top = 1;
+    long long R = 0;
     for (int b0 = 0; b0 < a.batch; b0 += kWave) {
         if (b0 > 0) t = b0 + lane < a.batch ? cache_tokens(a, mode, cache_rows(a, b0 + lane)) : 0;
-        total += ((long long)wave_all(t >> 12, AddOp()) << 12) + wave_all(t & 4095, AddOp());
-        most = MaxOp()(most, wave_all(t, MaxOp()));
+        r = (t + a.round - 1) >> shift;
+        R += wave_all(r, AddOp());
+        top = MaxOp()(top, wave_all(r, MaxOp()));
     }
-    const int whole = ceil_div_dev(most > 0 ? most : 1, a.round) * a.round;  // (a part per sequence is always allowed)
-    if (a.parts <= a.batch || total == 0) return whole;
-    const int top = whole / a.round;  // candidates, in rounds
-    const long long enough = (total + (long long)(a.parts - a.batch) * a.round - 1) / ((long long)(a.parts - a.batch) * a.round);
-    const long long least = (total + (long long)a.parts * a.round - 1) / ((long long)a.parts * a.round);
+    if (a.parts <= a.batch || R == 0) return top << shift;  // (a part per sequence is always allowed)
+    const float enough = (float)R * __builtin_amdgcn_rcpf((float)(a.parts - a.batch)) * UP + 1.0f;
+    const float least = (float)R * __builtin_amdgcn_rcpf((float)a.parts) * (1.0f - 0x1p-20f);
     const int most_parts = ceil_div_dev(top, kMaxCacheParts);  // (the others may be empty: one sequence may have all the parts)
-    int hi = enough < top ? (int)enough : top, lo = least < hi ? (int)least : hi;
+    int hi = enough < (float)top ? (int)enough : top, lo = least < (float)hi ? (int)least : hi;
     lo = lo > most_parts ? lo : most_parts;
     hi = hi > lo ? hi : lo;
-    const int step = ceil_div_dev(hi - lo, kWave - 1), chunk = (lo + lane * step) * a.round;
-    long long used = 0;
+    const int step = ceil_div_dev(hi - lo, kWave - 1), m = lo + lane * step;
+    const float inv = __builtin_amdgcn_rcpf((float)m) * UP;
+    float used = 0.0f;
     for (int b0 = 0; b0 < a.batch; b0 += kWave) {
-        if (a.batch > kWave) t = b0 + lane < a.batch ? cache_tokens(a, mode, cache_rows(a, b0 + lane)) : 0;
-        for (int i = 0; i < kWave && b0 + i < a.batch; ++i) used += ceil_div_dev(__builtin_amdgcn_readlane(t, i), chunk);
+        if (a.batch > kWave) {
+            t = b0 + lane < a.batch ? cache_tokens(a, mode, cache_rows(a, b0 + lane)) : 0;
+            r = (t + a.round - 1) >> shift;
+        }
+        for (int i = 0; i < kWave && b0 + i < a.batch; ++i) used += floorf((float)(__builtin_amdgcn_readlane(r, i) + m - 1) * inv);
     }
-    const uint64_t fits = __ballot(used <= a.parts);  // (the last candidate is at least hi)
-    const int best = (lo + (fits ? __builtin_ctzll(fits) : kWave - 1) * step) * a.round;
-    return best > 0 && best < whole ? best : whole;
+    const uint64_t fits = __ballot(used <= (float)a.parts);  // (the last candidate is at least hi)
+    const int best = lo + (fits ? __builtin_ctzll(fits) : kWave - 1) * step;
+    return (best > 0 && best < top ? best : top) << shift;
 }
 
 __device__ __forceinline__ CacheUnit cache_unit(const CacheArgs &a, CacheMode mode, int tiles)
