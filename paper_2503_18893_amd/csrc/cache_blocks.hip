@@ -532,8 +532,13 @@ hipError_t launch_block_select(const xkv_shape &s, const CacheArgs &a, const voi
         hipLaunchKernelGGL(kernel, dim3(a.batch * a.N * a.H_kv), dim3(threads), 0, st, a, (const bf16_t *)landmarks, scores, estimate ? reach : nullptr, blocks, n_c);
         return hipGetLastError();
     };
-    return n_c <= 1024 ? select(block_select_kernel<256, 4>, 256) : n_c <= 2048 ? select(block_select_kernel<256, 8>, 256)
-         : n_c <= 4096 ? select(block_select_kernel<256, 16>, 256) : select(block_select_kernel<1024, 16>, 1024);
+    // Eight wavefronts where a workgroup has a compute unit to itself and more than 1024 blocks.  A whole call with four / eight, us: 8 queries
+    // and KV heads, 2048 blocks 22.4 / 21.5, 128 of them 77.6 / 76.3, 1024 of them 263 / 268; 16 with 4000 blocks 25.9 / 24.2; 8 with 1000 the same.
+    const bool few = a.batch * a.N * a.H_kv <= 256;
+    return n_c <= 1024 ? select(block_select_kernel<256, 4>, 256)
+         : n_c <= 2048 ? (few ? select(block_select_kernel<512, 4>, 512) : select(block_select_kernel<256, 8>, 256))
+         : n_c <= 4096 ? (few ? select(block_select_kernel<512, 8>, 512) : select(block_select_kernel<256, 16>, 256))
+                       : select(block_select_kernel<1024, 16>, 1024);
 }
 
 hipError_t launch_block_scores(const xkv_shape &s, const CacheArgs &a, const void *landmarks, int n_c, float *scores, hipStream_t st)

@@ -219,6 +219,26 @@ def test_blocks_whose_scores_lie_close_together(L, c, k, spread):
         assert blocks.cpu()[b, 0, 0].tolist() == ref.choose_blocks(q[b, 0], marks[b, 0], visible[b], c, k_ch)
 
 
+@pytest.mark.parametrize("L,N", [(1100, 3), (2049, 2), (1100, 150), (2049, 140)])
+def test_blocks_with_few_and_many_queries(L, N):
+    """More than 1024 and 2048 blocks, for fewer and more queries than compute units."""
+    s = shape_of(2, 2, 128, L, 1, "bf16", k=40)
+    g, K, V = cache(s, [L], 81)
+    marks, q = torch.randn((1, 2, L, 128), generator=g).bfloat16(), torch.randn((1, N, 4, 128), generator=g).bfloat16()
+    visible = torch.randint(1, L + 1, (1, N), generator=g, dtype=torch.int32)
+    visible[0, 0] = L
+    out, blocks = torch.empty_like(q, device="cuda"), torch.empty((1, N, 2, 40), dtype=torch.int32, device="cuda")
+    xb.xkv_block_decode(s, K.cuda(), V.cuda(), visible.cuda(), q.cuda(), N, marks.cuda(), 1, out, blocks, workspace(s, N, 1))
+    torch.cuda.synchronize()
+    for i in range(N):
+        n = visible[0, i].item()
+        for h in range(2):
+            want = ref.choose_blocks(q[0, i, 2 * h:2 * h + 2], marks[0, h], n, 1, 40)
+            assert blocks.cpu()[0, i, h].tolist() == want + list(range(n, n + 40 - len(want))), (i, h)
+            o, _, bound, _ = ref.attend(q[0, i, 2 * h:2 * h + 2], K[0, h, want], V[0, h, want], torch.ones((2, len(want)), dtype=torch.bool), scale_of(s))
+            within(out.cpu()[0, i, 2 * h:2 * h + 2], o, bound, f"{i} {h}")
+
+
 @pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64), ("f32", 20)])
 @pytest.mark.parametrize("L", [3000, 17000])
 def test_blocks_whose_scores_overflow(dtype, d, L):
