@@ -38,7 +38,8 @@ __device__ __forceinline__ uint32_t draft_bits(const CacheArgs &a, int seq, int 
 // ------------------------------------------------------------------------------------------
 // General path, any type, width and alignment.  A round takes 64 tokens, whose keys and values go to LDS in single precision (the
 // next round's are requested before this one is computed).  For the logits a lane multiplies one of the keys with the four queries
-// of its wavefront, four channels a time; for the sums lanes run over the channels, and the weights go through LDS.  With few rows its time is that of one round, latencies: 8 drafted tokens of 4 heads after 512 tokens, fp32.
+// of its wavefront, four channels a time; for the sums lanes run over the channels, and the weights go through LDS.  With few rows its time
+// is that of one round, latencies: 8 drafted tokens of 4 heads after 512 tokens, fp32, 9.7 us.
 // ------------------------------------------------------------------------------------------
 __host__ __device__ inline int general_pitch(int d) { return ((d + 3) / 4 | 1) * 4; }  // floats; an odd number of 16-byte pieces
 
@@ -214,6 +215,9 @@ __global__ __launch_bounds__(256) void cache_attend_general_kernel(CacheArgs a)
 // P^T is the second product's operand as it comes.  V^T is read from its tile by the transposing LDS read.
 // The maximum m is only raised when a row's logits outgrow it by a factor of 2^8: until then weights reach 2^8, sums stay exact to
 // single precision, and the accumulators need not be rescaled.
+// Weights are rounded to bf16 once, as operands of the second product (P in fp32 would take products of a quarter of the rate): that moves
+// a result by at most 2^-8 sum p |v|, at random in sign, beside its own rounding; the error against 64 bits is 0.0023 of the
+// results' root mean square, 0.0017 with the output's rounding alone.  Logits, statistics and sums are fp32.
 // LDS: row t of a tile is 256 B; its 16-byte piece p of K sits at (p + t) % 16, its 32-byte piece u of V at (u + 2 t) % 8, so
 // that neither the fragment reads (16 rows at a time, one piece each) nor the transposing reads (4 rows at a time, two pieces each)
 // meet in a bank.
