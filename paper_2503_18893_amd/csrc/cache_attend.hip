@@ -215,7 +215,7 @@ __global__ __launch_bounds__(256) void cache_attend_general_kernel(CacheArgs a)
 // P^T is the second product's operand as it comes.  V^T is read from its tile by the transposing LDS read.
 // The maximum m is only raised when a row's logits outgrow it by a factor of 2^8: until then weights reach 2^8, sums stay exact to
 // single precision, and the accumulators need not be rescaled.
-// Weights are rounded to bf16 once, as operands of the second product (P in fp32 would take products of a quarter of the rate): that moves
+// Weights are rounded to bf16 once, as operands of the second product (in fp32 the matrix cores multiply at a sixteenth of the rate): that moves
 // a result by at most 2^-8 sum p |v|, at random in sign, beside its own rounding; the error against 64 bits is 0.0023 of the
 // results' root mean square, 0.0017 with the output's rounding alone.  Logits, statistics and sums are fp32.
 // LDS: row t of a tile is 256 B; its 16-byte piece p of K sits at (p + t) % 16, its 32-byte piece u of V at (u + 2 t) % 8, so
