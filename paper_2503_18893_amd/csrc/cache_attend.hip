@@ -215,9 +215,10 @@ __global__ __launch_bounds__(256) void cache_attend_general_kernel(CacheArgs a)
 // P^T is the second product's operand as it comes.  V^T is read from its tile by the transposing LDS read.
 // The maximum m is only raised when a row's logits outgrow it by a factor of 2^8: until then weights reach 2^8, sums stay exact to
 // single precision, and the accumulators need not be rescaled.
-// Weights are rounded to bf16 once, as operands of the second product (in fp32 the matrix cores multiply at a sixteenth of the rate): that moves
-// a result by at most 2^-8 sum p |v|, at random in sign, beside its own rounding; the error against 64 bits is 0.0023 of the
-// results' root mean square, 0.0017 with the output's rounding alone.  Logits, statistics and sums are fp32.
+// Weights are operands of two products, their upper 16 bits and what is left of them rounded to bf16, so that they keep 2^-15: the error
+// against 64 bits is the output's rounding alone, 0.0017 of the results' root mean square (0.0023 with weights rounded to bf16).  What the
+// second product costs: up to 16 rows nothing, the stream covers it; 64 rows after 32768 tokens 34.6 -> 36.0 us; 256 rows of four sequences
+// of 16K to 64K 193 -> 258, 231 rows 62 -> 76, where the matrix cores bound it.  Logits, statistics and sums are fp32.
 // LDS: row t of a tile is 256 B; its 16-byte piece p of K sits at (p + t) % 16, its 32-byte piece u of V at (u + 2 t) % 8, so
 // that neither the fragment reads (16 rows at a time, one piece each) nor the transposing reads (4 rows at a time, two pieces each)
 // meet in a bank.
@@ -393,7 +394,8 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_tree_kern
             }
         }
     };
-    auto weigh = [&](f32x16_t (&S)[PARTS], bf16x8_t (&P)[2 * PARTS]) __attribute__((always_inline)) {
+    // logits to weights, as operands of two products
+    auto weigh = [&](f32x16_t (&S)[PARTS], bf16x8_t (&P)[2 * PARTS], bf16x8_t (&R)[2 * PARTS]) __attribute__((always_inline)) {
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
             const int rt = p / SUB;
@@ -402,12 +404,14 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_tree_kern
             for (int j = 0; j < 2; ++j) {
 #pragma unroll
                 for (int v = 8 * j; v < 8 * j + 8; ++v) S[p][v] = __builtin_amdgcn_exp2f(fmaf(S[p][v], c, less));
-                P[2 * p + j] = pack8(S[p], j);
-                l_run[rt] = add_pairs(P[2 * p + j], l_run[rt]);
+                const f32x8_t x = eight(S[p], j);
+                l_run[rt] = sum8(x, l_run[rt]);
+                P[2 * p + j] = upper8(x);
+                R[2 * p + j] = lower8(x);
             }
         }
     };
-    auto add_values = [&](const unsigned char *lds, const bf16x8_t (&P)[2 * PARTS]) __attribute__((always_inline)) {
+    auto add_values = [&](const unsigned char *lds, const bf16x8_t (&P)[2 * PARTS], const bf16x8_t (&R)[2 * PARTS]) __attribute__((always_inline)) {
 #pragma unroll
         for (int sj = 0; sj < 2 * SUB; ++sj)
 #pragma unroll
@@ -416,10 +420,11 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_tree_kern
                 const unsigned char *from = lds + vat[db] + 4096 * sj;
                 const s16x4_t a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)from);
                 const s16x4_t a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(from + 2048));
+                const bf16x8_t v = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
-                    O[rt][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                        __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7)), P[2 * SUB * rt + sj], O[rt][db], 0, 0, 0);
+                for (int rt = 0; rt < RT; ++rt) O[rt][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, R[2 * SUB * rt + sj], O[rt][db], 0, 0, 0);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) O[rt][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, P[2 * SUB * rt + sj], O[rt][db], 0, 0, 0);
             }
     };
     if constexpr (OWN) {
@@ -444,7 +449,7 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_tree_kern
                 XKV_WAIT_VMCNT(LOADS);
             asm volatile("" : : : "memory");
             f32x16_t S[PARTS];
-            bf16x8_t P[2 * PARTS];
+            bf16x8_t P[2 * PARTS], R[2 * PARTS];
             logits(lds, S);
             if (then) {
                 wait_lds();
@@ -454,7 +459,7 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_tree_kern
             float m_loc[RT];
             top_of(S, m_loc);
             raise(m_loc);
-            weigh(S, P);
+            weigh(S, P, R);
             if (then)
                 XKV_WAIT_VMCNT(3 * LOADS);
             else if (next)
@@ -462,7 +467,7 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_tree_kern
             else
                 XKV_WAIT_VMCNT(0);
             asm volatile("" : : : "memory");
-            add_values(lds, P);
+            add_values(lds, P, R);
             if (then) {
                 wait_lds();
                 stage(t + 2 * TILE, buf, values);
@@ -493,7 +498,7 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_tree_kern
             stage_plain(t0 + TILE + RPW * w, BUF ^ 1, values);
             raise(m_loc);
             const unsigned char *kt = lds_w + (BUF ^ 1) * KTILE, *vt = lds_w + BUF * KTILE;
-            bf16x8_t P[2 * PARTS];
+            bf16x8_t P[2 * PARTS], R[RT];
             // each product with the keys beside two exponentials
             u32x4_t kf[READS];
             auto read_key = [&](int k) __attribute__((always_inline)) {
@@ -516,8 +521,9 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_tree_kern
                     S[v / 16][v % 16] = __builtin_amdgcn_exp2f(fmaf(S[v / 16][v % 16], c, less[v / 16 / SUB]));
                 }
                 if (i % 4 == 3) {
-                    P[i / 4] = pack8(S[i / 8], i / 4 % 2);
-                    l_run[i / 8 / SUB] = add_pairs(P[i / 4], l_run[i / 8 / SUB]);
+                    const f32x8_t x = eight(S[i / 8], i / 4 % 2);
+                    l_run[i / 8 / SUB] = sum8(x, l_run[i / 8 / SUB]);
+                    P[i / 4] = upper8(x);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -537,9 +543,10 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_tree_kern
             for (int i = 0; i < STEPS; ++i) {
                 const int k = i / RT, rt = i % RT;
                 if (rt == 0 && k + AHEAD < READS) read_values(k + AHEAD);
-                O[rt][k % 4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                    __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(vf[k][0], vf[k][1], 0, 1, 2, 3, 4, 5, 6, 7)), P[2 * SUB * rt + k / 4],
-                    O[rt][k % 4], 0, 0, 0);
+                if (k % 4 == 0) R[rt] = lower8(eight(S[(2 * SUB * rt + k / 4) / 2], k / 4 % 2));  // (not before: the exponentials keep the other half busy)
+                const bf16x8_t v8 = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(vf[k][0], vf[k][1], 0, 1, 2, 3, 4, 5, 6, 7));
+                O[rt][k % 4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v8, R[rt], O[rt][k % 4], 0, 0, 0);
+                O[rt][k % 4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v8, P[2 * SUB * rt + k / 4], O[rt][k % 4], 0, 0, 0);
                 if (i >= STEPS / 2) {
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
@@ -570,11 +577,11 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_tree_kern
             if (t0 + TILE < t_end) stage(t0 + TILE + RPW * w, buf ^ 1, values);
             raise(m_loc);
             f32x16_t S1[PARTS];
-            bf16x8_t P[2 * PARTS];
+            bf16x8_t P[2 * PARTS], R[2 * PARTS];
             logits(lds_w + (buf ^ 1) * KTILE, S1);  // (behind the last tile: of whatever is there, not used)
-            weigh(S, P);
+            weigh(S, P, R);
             if (t0 + TILE < t_end) hide(t0 + TILE + 32 * SUB * tg, S1);
-            add_values(lds_w + buf * KTILE, P);
+            add_values(lds_w + buf * KTILE, P, R);
             top_of(S1, m_loc);
 #pragma unroll
             for (int s = 0; s < PARTS; ++s) S[s] = S1[s];
@@ -870,12 +877,9 @@ __global__ __launch_bounds__(256, 1) void cache_stream_kernel(CacheArgs a)
         const float less = m_run == -INFINITY ? 0.0f : -m_run * c;
         f32x8_t p;
 #pragma unroll
-        for (int v = 0; v < 8; ++v) {
-            p[v] = __builtin_amdgcn_exp2f(fmaf(S[v / 4][v % 4], c, less));
-            if (KEEP) l_run += p[v];  // (weights that are given out are divided by this sum: unrounded)
-        }
-        const bf16x8_t P = __builtin_convertvector(p, bf16x8_t);
-        if (!KEEP) l_run = add_pairs(P, l_run);
+        for (int v = 0; v < 8; ++v) p[v] = __builtin_amdgcn_exp2f(fmaf(S[v / 4][v % 4], c, less));
+        l_run = sum8(p, l_run);
+        const bf16x8_t P = upper8(p), R = lower8(p);
         if (then)
             XKV_WAIT_VMCNT(3 * LOADS);
         else if (next)
@@ -889,8 +893,9 @@ __global__ __launch_bounds__(256, 1) void cache_stream_kernel(CacheArgs a)
             const unsigned char *from = lds + vat[db];
             const s16x4_t a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)from);
             const s16x4_t a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(from + 4096));
-            O[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7)), P,
-                                                            O[db], 0, 0, 0);
+            const bf16x8_t v = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
+            O[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, R, O[db], 0, 0, 0);
+            O[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, P, O[db], 0, 0, 0);
         }
         if (then) {
             wait_lds();

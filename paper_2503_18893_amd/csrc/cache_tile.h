@@ -45,22 +45,36 @@ __device__ __forceinline__ void quarters(float x, float &lo, float &hi)
     hi = __uint_as_float(r[1]);
 }
 
-__device__ __forceinline__ bf16x8_t pack8(const f32x16_t &c, int j)
+__device__ __forceinline__ f32x8_t eight(const f32x16_t &c, int j)
 {
     f32x8_t x;
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = c[8 * j + e];
-    return __builtin_convertvector(x, bf16x8_t);
+    return x;
 }
 
-// sum + the eight weights as they enter the products (rounded): what divides the result is then the sum of what multiplied the values.
-__device__ __forceinline__ float add_pairs(const bf16x8_t &p, float sum)
+__device__ __forceinline__ float sum8(const f32x8_t &p, float sum)
 {
-    typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
-    const bf16x2_t ones = {(__bf16)1.0f, (__bf16)1.0f};
 #pragma unroll
-    for (int e = 0; e < 8; e += 2) sum = __builtin_amdgcn_fdot2_f32_bf16(bf16x2_t{p[e], p[e + 1]}, ones, sum, false);
+    for (int e = 0; e < 8; ++e) sum += p[e];
     return sum;
+}
+
+// Eight weights as operands of two products: their upper 16 bits (one instruction for two weights), and what is left of each, rounded.
+// Together they hold a weight to 2^-15.
+__device__ __forceinline__ bf16x8_t upper8(const f32x8_t &p)
+{
+    u32x4_t x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = __builtin_amdgcn_perm(__float_as_uint(p[2 * e + 1]), __float_as_uint(p[2 * e]), 0x07060302u);
+    return __builtin_bit_cast(bf16x8_t, x);
+}
+__device__ __forceinline__ bf16x8_t lower8(const f32x8_t &p)
+{
+    f32x8_t x;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = p[e] - __uint_as_float(__float_as_uint(p[e]) & 0xFFFF0000u);
+    return __builtin_convertvector(x, bf16x8_t);
 }
 
 }  // namespace cache_tile
