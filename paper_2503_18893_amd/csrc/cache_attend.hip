@@ -623,7 +623,7 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_tree_kern
 #pragma unroll
         for (int i = 0; i < WT; ++i) {
             const float mi = sm_m[i][threadIdx.x];
-            den += mi == -INFINITY ? 0.0f : sm_l[i][threadIdx.x] * __builtin_amdgcn_exp2f((mi - top) * c);
+            den += sm_l[i][threadIdx.x] * (mi == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((mi - top) * c));  // (without a maximum: 0, or NaN)
         }
         const size_t slot = part_row(a, MODE, u.part, m / n_rep, g * n_rep + m % n_rep);
         sm_slot[threadIdx.x] = m < M ? (uint32_t)slot : 0xFFFFFFFFu;
@@ -931,7 +931,7 @@ __global__ __launch_bounds__(256, 1) void cache_stream_kernel(CacheArgs a)
             most = fmaxf(most, sm_m[i][row]);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) den += sm_m[i][row] == -INFINITY ? 0.0f : sm_l[i][row] * __builtin_amdgcn_exp2f((sm_m[i][row] - most) * c);
+        for (int i = 0; i < 4; ++i) den += sm_l[i][row] * (sm_m[i][row] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((sm_m[i][row] - most) * c));
         if (direct) {
             bf16_t *out = (bf16_t *)a.out + ((size_t)u.seq * a.H_q + g * n_rep + row) * 128 + 4 * p;
 #pragma unroll
@@ -945,6 +945,17 @@ __global__ __launch_bounds__(256, 1) void cache_stream_kernel(CacheArgs a)
             a.part_ml[2 * slot + 1] = den;
         }
     }
+}
+
+// Whether query z (sequence, query token) sees no token at all: its result is zeros.
+__device__ __forceinline__ bool sees_nothing(const CacheArgs &a, CacheMode mode, int z)
+{
+    if (cache_rows(a, mode == CacheMode::tree ? z / a.N : z) > 0) return false;
+    if (mode != CacheMode::tree) return true;
+    if (!a.tree) return false;  // (it sees itself)
+    uint32_t any = 0;
+    for (int k = 0; k < a.words; ++k) any |= a.tree[(size_t)z * a.words + k] & (32 * k + 32 <= a.N ? 0xFFFFFFFFu : (1u << (a.N & 31)) - 1u);
+    return any == 0;
 }
 
 // ------------------------------------------------------------------------------------------
@@ -1004,8 +1015,9 @@ __device__ __forceinline__ void merge_block(const CacheArgs &a, int lg, int shar
     }
     if (item >= rows || col >= a.d_h) return;
     T *out = (T *)a.out + (size_t)row * a.d_h + col;
+    const bool none = den == 0.0f && sees_nothing(a, MODE, z);  // (a sum of zero otherwise: logits of -inf alone, 0 / 0)
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) out[e] = from_f32<T>(den > 0.0f ? acc[e] / den : 0.0f);  // (a query that sees nothing: zeros)
+    for (int e = 0; e < VEC; ++e) out[e] = from_f32<T>(none ? 0.0f : acc[e] / den);
 }
 
 // ------------------------------------------------------------------------------------------
