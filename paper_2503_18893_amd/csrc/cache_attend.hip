@@ -106,8 +106,9 @@ __global__ __launch_bounds__(256) void cache_attend_general_kernel(CacheArgs a)
     for (int t0 = t_begin; t0 < t_end; t0 += kGenTokens) {
         const int t = t0 + lane < t_end ? t0 + lane : t_end - 1;
         const bool real = t0 + lane < t_end;
-        uint32_t bits[4] = {1u, 1u, 1u, 1u};  // tree: whether the rows see this lane's token (requested here, used after the logits)
-        if (MODE == CacheMode::tree && t0 + kGenTokens > n) {
+        const bool mixed = MODE == CacheMode::tree && t0 + kGenTokens > n;  // rows see different tokens of this round
+        uint32_t bits[4] = {1u, 1u, 1u, 1u};                                  // whether the rows see this lane's token (requested here, used after the logits)
+        if (mixed) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) bits[r] = draft_bits(a, seq, token[r], t - n);
         }
@@ -119,7 +120,7 @@ __global__ __launch_bounds__(256) void cache_attend_general_kernel(CacheArgs a)
                 const int j = lane + jj * kWave;
                 if (j < d4) {
                     kt[(4 * i + w) * pitch + j] = j < d ? to_f32(kr[i][jj]) : 0.0f;
-                    vt[(4 * i + w) * pitch + j] = to_f32(vr[i][jj]);
+                    vt[(4 * i + w) * pitch + j] = t0 + 4 * i + w < t_end ? to_f32(vr[i][jj]) : 0.0f;
                 }
             }
         __syncthreads();
@@ -157,38 +158,45 @@ __global__ __launch_bounds__(256) void cache_attend_general_kernel(CacheArgs a)
 #pragma unroll
             for (int jj = 0; jj < JP; ++jj) o[r][jj] *= alpha;
         }
+        if (mixed) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) p[r] = bits[r] & 1u ? p[r] : -0.0f;  // (weights are not negative: hidden from this row)
+        }
         // the four weights of a token to every lane
         *reinterpret_cast<float4 *>(ps + 4 * (64 * w + lane)) = float4{p[0], p[1], p[2], p[3]};
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         const int count = t_end - t0 < kGenTokens ? t_end - t0 : kGenTokens;
-        for (int i0 = 0; i0 < count; i0 += 8) {  // (places from `count` on hold the last token again, with weight zero)
-            float v[8][JP];
-            float4 y[8];
+        auto add_values = [&](auto take) __attribute__((always_inline)) {
+            for (int i0 = 0; i0 < count; i0 += 8) {  // (places from `count` on hold zeros)
+                float v[8][JP];
+                float4 y[8];
 #pragma unroll
-            for (int x = 0; x < 8; ++x) {
-                y[x] = *reinterpret_cast<const float4 *>(ps + 4 * (64 * w + i0 + x));
+                for (int x = 0; x < 8; ++x) {
+                    y[x] = *reinterpret_cast<const float4 *>(ps + 4 * (64 * w + i0 + x));
 #pragma unroll
-                for (int jj = 0; jj < JP; ++jj) {
-                    const int j = lane + jj * kWave;
-                    v[x][jj] = vt[(i0 + x) * pitch + (j < d ? j : 0)];
+                    for (int jj = 0; jj < JP; ++jj) {
+                        const int j = lane + jj * kWave;
+                        v[x][jj] = vt[(i0 + x) * pitch + (j < d ? j : 0)];
+                    }
                 }
-            }
 #pragma unroll
-            for (int x = 0; x < 8; ++x) {
-                // a drafted token that none of these rows sees may be padding with anything in it
-                const bool use = MODE != CacheMode::tree || y[x].x + y[x].y + y[x].z + y[x].w > 0.0f;
+                for (int x = 0; x < 8; ++x)
 #pragma unroll
-                for (int jj = 0; jj < JP; ++jj) {
-                    const float vv = use ? v[x][jj] : 0.0f;
-                    o[0][jj] = fmaf(y[x].x, vv, o[0][jj]);
-                    o[1][jj] = fmaf(y[x].y, vv, o[1][jj]);
-                    o[2][jj] = fmaf(y[x].z, vv, o[2][jj]);
-                    o[3][jj] = fmaf(y[x].w, vv, o[3][jj]);
-                }
+                    for (int jj = 0; jj < JP; ++jj) {
+                        o[0][jj] = fmaf(y[x].x, take(y[x].x, v[x][jj]), o[0][jj]);
+                        o[1][jj] = fmaf(y[x].y, take(y[x].y, v[x][jj]), o[1][jj]);
+                        o[2][jj] = fmaf(y[x].z, take(y[x].z, v[x][jj]), o[2][jj]);
+                        o[3][jj] = fmaf(y[x].w, take(y[x].w, v[x][jj]), o[3][jj]);
+                    }
             }
-        }
+        };
+        // what a row does not see is not multiplied by zero: it may be padding with anything in it, or other rows' infinities
+        if (mixed)
+            add_values([](float weight, float value) { return __float_as_uint(weight) == 0x80000000u ? 0.0f : value; });
+        else
+            add_values([](float, float value) { return value; });
     }
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
@@ -1004,7 +1012,7 @@ __device__ __forceinline__ void merge_block(const CacheArgs &a, int lg, int shar
 #pragma unroll
         for (int u = 0; u < BATCH; ++u) {
             const int s = s1 + u * step;
-            acc += (s < parts ? sm_w[grp][s] : 0.0f) * v[u];
+            acc += (s < parts ? sm_w[grp][s] : 0.0f) * (s < parts ? v[u] : vec_t(0.0f));
         }
     }
     if (share) {

@@ -191,3 +191,49 @@ def test_blocks(name, batch, how):
                     continue
                 want, _, bound, _ = attend(q[b, i, heads], K[b, h, t], V[b, h, t], torch.ones((n_rep, len(t)), dtype=torch.bool), scale_of(s))
                 same(out[b, i, heads], want, bound, f"{how} {b} {i} {h}")
+
+
+GENERAL = ("f32", "bf16_96")
+
+
+@pytest.mark.parametrize("name", GENERAL)
+def test_a_nan_query_leaves_other_rows_alone(name):
+    s, N, lengths, x, sees = tree_inputs(name, 904)
+    x[0][0, N - 1, 1, 3] = NAN
+    x[0][1, 0, s.H_q - 1] = NAN
+    check_tree(s, N, lengths, x, sees, "NaN query")
+
+
+def spoil_draft(x, sees, how):
+    """Drafted tokens that some tokens see and others do not."""
+    N = sees.shape[-1]
+    Kd, Vd = x[3], x[4]
+    j = N // 2
+    for t in (j, N - 1):
+        sees[:, :, t] = False
+        sees[:, t, t] = True  # only itself
+    if how == "nan":
+        Kd[:, :, j], Vd[:, :, j] = NAN, NAN
+        Vd[1, 0, N - 1] = NAN
+    elif how == "inf_values":
+        Vd[:, :, j] = INF
+        Vd[0, 1, N - 1] = -INF
+    elif how == "inf_in_places":
+        Vd[0, :, j, 5], Vd[0, :, j, -1] = -INF, INF
+        Vd[1, :, N - 1, 0] = NAN
+    else:  # +inf and -inf in one place, seen together by some rows and alone by others
+        Vd[:, :, 0, 7], Vd[:, :, j, 7], Vd[:, :, N - 1, 7] = INF, -INF, INF
+        sees[:, N // 3:, j] = True
+        sees[:, N // 2:, N - 1] = True
+
+
+DRAFTS = ("nan", "inf_values", "inf_in_places", "inf_and_minus_inf")
+
+
+@pytest.mark.parametrize("empty", (False, True))
+@pytest.mark.parametrize("how", DRAFTS)
+@pytest.mark.parametrize("name", GENERAL)
+def test_what_a_drafted_token_holds_reaches_only_those_who_see_it(name, how, empty):
+    s, N, lengths, x, sees = tree_inputs(name, 905)
+    spoil_draft(x, sees, how)
+    check_tree(s, N, [0, 33] if empty else lengths, x, sees, how)
