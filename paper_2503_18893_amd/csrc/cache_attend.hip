@@ -233,6 +233,52 @@ __global__ __launch_bounds__(256) void cache_attend_general_kernel(CacheArgs a)
 // ------------------------------------------------------------------------------------------
 __device__ const u32x4_t kZeroRow[16] = {};  // stands for drafted tokens that nothing sees, and for places behind the last token
 
+// Rows see different drafted tokens, but a product with the values takes all of them, with weight zero where they are hidden: infinities and
+// NaN must not be among them.  A wavefront that has received rows of values of drafted tokens sets such values to zero where they lie in LDS
+// and notes the tokens; when rows leave, they are added to those that see them.  (Without any it is a look at the last tiles.)
+//   clear_odd: 4 LOADS rows at `at` (this lane's 16 bytes of the first four), those from `skip` on -> a bit for each row that had some
+template <int LOADS> __device__ __forceinline__ uint32_t clear_odd(unsigned char *at, int skip)
+{
+    uint32_t rows = 0;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        u32x4_t x = *reinterpret_cast<const u32x4_t *>(at + 1024 * i);
+        bool odd = false;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool lo = (x[e] & 0x7F80u) == 0x7F80u, hi = (x[e] & 0x7F800000u) == 0x7F800000u;
+            x[e] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
+            odd |= lo || hi;
+        }
+        odd &= 4 * i + (lane_id() >> 4) >= skip;
+        const uint64_t m = __ballot(odd);
+        if (m == 0) continue;
+        if (odd) *reinterpret_cast<u32x4_t *>(at + 1024 * i) = x;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) rows |= (m >> (16 * r) & 0xFFFFu) ? 1u << (4 * i + r) : 0u;
+    }
+    return rows;
+}
+// bit i of rows: drafted token j + i (j may be negative, such bits are not set), in all wavefronts' notes
+__device__ __forceinline__ void note_odd(uint32_t *notes, uint32_t rows, int j)
+{
+    if (rows == 0 || lane_id() != 0) return;
+    const uint64_t bits = j < 0 ? rows >> -j : (uint64_t)rows << (j & 31);
+    const int k = j < 0 ? 0 : j >> 5;
+    if ((uint32_t)bits) atomicOr(&notes[k], (uint32_t)bits);
+    if (bits >> 32) atomicOr(&notes[k + 1], (uint32_t)(bits >> 32));
+}
+__device__ __forceinline__ f32x4_t add_odd(const CacheArgs &a, const uint32_t *notes, const bf16_t *values, int seq, int token, int channel, f32x4_t x)
+{
+    for (int k = 0; k < a.words; ++k)
+        for (uint32_t bits = notes[k] & draft_word(a, seq, token, k); bits; bits &= bits - 1) {
+            const bf16_t *v = values + (size_t)(32 * k + __builtin_ctz(bits)) * 128 + channel;
+            for (int e = 0; e < 4; ++e)
+                if ((v[e] & 0x7F80) == 0x7F80) x[e] += bf16_to_f32(v[e]);
+        }
+    return x;
+}
+
 template <int WR, int WT, int SUB, int RT>
 __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_tree_kernel(CacheArgs a)
 {
@@ -244,7 +290,7 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_tree_kern
     constexpr int MERGE = WAVES * RT * 16384;
     __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE >= MERGE ? 2 * STAGE : MERGE];
     __shared__ float sm_m[WT][32 * WR * RT], sm_l[WT][32 * WR * RT];
-    __shared__ uint32_t sm_seen[32], sm_slot[32 * WR * RT];
+    __shared__ uint32_t sm_seen[32], sm_odd[32], sm_slot[32 * WR * RT];
     const int lane = lane_id(), w = wave_id(), rg = w % WR, tg = w / WR, n32 = lane & 31, hf = lane >> 5, n_rep = a.H_q / a.H_kv;
     const int M = a.N * n_rep;
     const CacheUnit u = cache_unit(a, MODE, (M + 32 * WR * RT - 1) / (32 * WR * RT));
@@ -272,7 +318,7 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_tree_kern
     }
 
     if (t_end > n) {  // which drafted tokens any token sees
-        if (threadIdx.x < 32) sm_seen[threadIdx.x] = a.tree ? 0u : 0xFFFFFFFFu;
+        if (threadIdx.x < 32) sm_seen[threadIdx.x] = a.tree ? 0u : 0xFFFFFFFFu, sm_odd[threadIdx.x] = 0u;
         __syncthreads();
         if (a.tree)
             for (int i = threadIdx.x; i < a.N * a.words; i += 64 * WAVES) {
@@ -475,6 +521,7 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_tree_kern
             else
                 XKV_WAIT_VMCNT(0);
             asm volatile("" : : : "memory");
+            if (t_end > n && t + 32 > n) note_odd(sm_odd, clear_odd<LOADS>(smem + 32768 * w + 16384 * buf + VBASE + 16 * lane, n - t), t - n);
             add_values(lds, P, R);
             if (then) {
                 wait_lds();
@@ -580,6 +627,11 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_tree_kern
         }
         for (; t0 < t_end; t0 += TILE, buf ^= 1) {
             XKV_WAIT_VMCNT(0);
+            if (t_end > n && t0 + TILE > n) {
+                asm volatile("" : : : "memory");
+                const int first = t0 + RPW * w;
+                note_odd(sm_odd, clear_odd<LOADS>(smem + 256 * RPW * w + buf * KTILE + VBASE + 16 * lane, n - first), first - n);
+            }
             __syncthreads();
             if (t0 + 2 * TILE < t_end) stage(t0 + 2 * TILE + RPW * w, buf, keys);
             if (t0 + TILE < t_end) stage(t0 + TILE + RPW * w, buf ^ 1, values);
@@ -642,6 +694,7 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_tree_kern
     }
     __syncthreads();
     const int p = threadIdx.x & 31, r0 = threadIdx.x >> 5;
+    const bool odd = t_end > n && __ballot(sm_odd[n32] != 0u);
 #pragma unroll
     for (int s0 = 0; s0 < ROWS / AT_ONCE; s0 += BATCH) {
         f32x4_t x[BATCH];
@@ -653,6 +706,11 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_tree_kern
             x[s] = f32x4_t(0.0f);
 #pragma unroll
             for (int i = 0; i < WT; ++i) x[s] += reinterpret_cast<const f32x4_t *>(smem)[1024 * i * WR * RT + 32 * row + ((p + row) & 31)];
+        }
+        if (odd) {
+#pragma unroll
+            for (int s = 0; s < BATCH; ++s)
+                if (slot[s] != 0xFFFFFFFFu) x[s] = add_odd(a, sm_odd, Vd, seq, (tile * ROWS + r0 + (s0 + s) * AT_ONCE) / n_rep, 4 * p, x[s]);
         }
 #pragma unroll
         for (int s = 0; s < BATCH; ++s)
@@ -677,7 +735,7 @@ __global__ __launch_bounds__(256, 1) void cache_stream_kernel(CacheArgs a)
     constexpr bool BLK = MODE == CacheMode::blocks, KEEP = MODE == CacheMode::weights;
     __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * 4 * KTILE];
     __shared__ float sm_m[4][16], sm_l[4][16];
-    __shared__ uint32_t sm_seen[32];
+    __shared__ uint32_t sm_seen[32], sm_odd[32];
     __shared__ __attribute__((aligned(16))) float sm_z[KEEP ? 4 : 1][KEEP ? kHeldLogits : 1][36];  // logits of a few tiles
     __shared__ int sm_rows[BLK ? kPartBlocks + 2 : 1];                                              // first rows of this part's blocks
     const int lane = lane_id(), w = wave_id(), n16 = lane & 15, kk = lane >> 4, n_rep = a.H_q / a.H_kv;
@@ -706,7 +764,7 @@ __global__ __launch_bounds__(256, 1) void cache_stream_kernel(CacheArgs a)
         for (int f = 0; f < 4; ++f) Qf[f] = __builtin_bit_cast(bf16x8_t, q[4 * f + kk]);
     }
     if (MODE == CacheMode::tree && t_end > n) {  // which drafted tokens any token sees
-        if (threadIdx.x < 32) sm_seen[threadIdx.x] = a.tree ? 0u : 0xFFFFFFFFu;
+        if (threadIdx.x < 32) sm_seen[threadIdx.x] = a.tree ? 0u : 0xFFFFFFFFu, sm_odd[threadIdx.x] = 0u;
         __syncthreads();
         if (a.tree)
             for (int i = threadIdx.x; i < a.N * a.words; i += 256) {
@@ -717,7 +775,7 @@ __global__ __launch_bounds__(256, 1) void cache_stream_kernel(CacheArgs a)
     }
     // Blocks: a load of a block's number between the requests of rows would be waited for together with them, so the numbers go to LDS first.
     // A lane's next tokens are TILE further on: `ahead` whole blocks and `rest` rows.
-    int in_list[8], in_block[8], rows_of[8], ahead = 0, rest = 0, last_row = 0;
+    int in_list[8], in_block[8], rows_of[8], ahead = 0, rest = 0;
     if constexpr (BLK) {
         const int32_t *sel = a.sel + ((size_t)u.seq * a.H_kv + g) * a.k_ch;
         const int b0 = t_begin / a.c, b1 = (t_end - 1) / a.c;  // b1 - b0 <= kPartBlocks
@@ -731,7 +789,6 @@ __global__ __launch_bounds__(256, 1) void cache_stream_kernel(CacheArgs a)
             in_list[i] = j - b0;
             in_block[i] = t - j * a.c;
         }
-        last_row = sm_rows[b1 - b0] + (t_end - 1) - b1 * a.c;
     }
 
 
@@ -751,8 +808,8 @@ __global__ __launch_bounds__(256, 1) void cache_stream_kernel(CacheArgs a)
             if constexpr (!is_v) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const bool real = first + 4 * i + r4 < t_end;  // (else the last row again, with weight zero)
-                    rows_of[i] = real ? sm_rows[real ? in_list[i] : 0] + in_block[i] : last_row;
+                    const bool real = first + 4 * i + r4 < t_end;
+                    rows_of[i] = real ? sm_rows[real ? in_list[i] : 0] + in_block[i] : -1;
                     in_list[i] += ahead;
                     in_block[i] += rest;
                     if (in_block[i] >= a.c) {
@@ -761,10 +818,17 @@ __global__ __launch_bounds__(256, 1) void cache_stream_kernel(CacheArgs a)
                     }
                 }
             }
+            auto copy = [&](auto whole) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i)
-                copy16_global_to_lds((const unsigned char *)(rows + (size_t)rows_of[i] * 128) + ((is_v ? voff[i & 1] : koff[i & 3]) - 256 * r4),
-                                     at + 1024 * i);
+                for (int i = 0; i < LOADS; ++i) {
+                    const bf16_t *from = decltype(whole)::value || rows_of[i] >= 0 ? rows + (size_t)rows_of[i] * 128 : (const bf16_t *)kZeroRow;
+                    copy16_global_to_lds((const unsigned char *)from + ((is_v ? voff[i & 1] : koff[i & 3]) - 256 * r4), at + 1024 * i);
+                }
+            };
+            if (first + 32 <= t_end)  // (wave-uniform)
+                copy(std::true_type{});
+            else
+                copy(std::false_type{});
             return;
         }
         if (first + 32 <= plain_end) {  // (wave-uniform)
@@ -775,16 +839,9 @@ __global__ __launch_bounds__(256, 1) void cache_stream_kernel(CacheArgs a)
         }
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            int t = first + 4 * i + r4;
-            const bf16_t *from;
-            if (MODE == CacheMode::tree) {
-                const int j = t - n;
-                const bool draft = t < t_end && j >= 0 && (sm_seen[(j >> 5) & 31] >> (j & 31) & 1u);
-                from = t < n ? rows + (size_t)t * 128 : draft ? (is_v ? Vd : Kd) + (size_t)j * 128 : (const bf16_t *)kZeroRow;
-            } else {
-                t = t < t_end ? t : t_end - 1;  // (its weight will be zero)
-                from = rows + (size_t)t * 128;
-            }
+            const int t = first + 4 * i + r4, j = t - n;
+            const bf16_t *from = t < plain_end ? rows + (size_t)t * 128 : (const bf16_t *)kZeroRow;
+            if (MODE == CacheMode::tree && t < t_end && j >= 0 && (sm_seen[(j >> 5) & 31] >> (j & 31) & 1u)) from = (is_v ? Vd : Kd) + (size_t)j * 128;
             copy16_global_to_lds((const unsigned char *)from + ((is_v ? voff[i & 1] : koff[i & 3]) - 256 * r4), at + 1024 * i);
         }
     };
@@ -895,6 +952,8 @@ __global__ __launch_bounds__(256, 1) void cache_stream_kernel(CacheArgs a)
         else
             XKV_WAIT_VMCNT(0);
         asm volatile("" : : : "memory");
+        if (MODE == CacheMode::tree && t_end > n && t + 32 > n)
+            note_odd(sm_odd, clear_odd<LOADS>(smem + 4 * KTILE * w + 2 * KTILE * buf + KTILE + 16 * lane, n - t), t - n);
 #pragma unroll
         for (int db = 0; db < 8; ++db) {
             // position e of lane (channel, kk): token 16 (e / 4) + 4 kk + e % 4, as in P
@@ -928,6 +987,7 @@ __global__ __launch_bounds__(256, 1) void cache_stream_kernel(CacheArgs a)
 #pragma unroll
     for (int db = 0; db < 8; ++db) ot[32 * n16 + ((4 * db + kk + n16) & 31)] = f * O[db];
     __syncthreads();
+    const bool odd = MODE == CacheMode::tree && t_end > n && __ballot(sm_odd[lane & 31] != 0u);
     for (int item = threadIdx.x; item < 512; item += 256) {
         const int row = item >> 5, p = item & 31;
         if (row >= M) continue;
@@ -946,6 +1006,7 @@ __global__ __launch_bounds__(256, 1) void cache_stream_kernel(CacheArgs a)
             for (int e = 0; e < 4; ++e) out[e] = f32_to_bf16(x[e] / den);
             continue;
         }
+        if (odd) x = add_odd(a, sm_odd, Vd, seq, row / n_rep, 4 * p, x);
         const size_t slot = part_row(a, MODE, u.part, row / n_rep, g * n_rep + row % n_rep);
         *reinterpret_cast<f32x4_t *>(a.part_o + slot * 128 + 4 * p) = x;
         if (p == 0) {

@@ -61,7 +61,8 @@ __device__ __forceinline__ float sum8(const f32x8_t &p, float sum)
 }
 
 // Eight weights as operands of two products: their upper 16 bits (one instruction for two weights), and what is left of each, rounded.
-// Together they hold a weight to 2^-15.
+// Together they hold a weight to 2^-15.  2^-22 of a weight more is left of each, so that it is not zero, which infinite values must not be
+// multiplied with.
 __device__ __forceinline__ bf16x8_t upper8(const f32x8_t &p)
 {
     u32x4_t x;
@@ -73,7 +74,7 @@ __device__ __forceinline__ bf16x8_t lower8(const f32x8_t &p)
 {
     f32x8_t x;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = p[e] - __uint_as_float(__float_as_uint(p[e]) & 0xFFFF0000u);
+    for (int e = 0; e < 8; ++e) x[e] = fmaf(p[e], 1.0f + 0x1p-22f, -__uint_as_float(__float_as_uint(p[e]) & 0xFFFF0000u));
     return __builtin_convertvector(x, bf16x8_t);
 }
 

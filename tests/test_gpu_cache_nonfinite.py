@@ -232,8 +232,44 @@ DRAFTS = ("nan", "inf_values", "inf_in_places", "inf_and_minus_inf")
 
 @pytest.mark.parametrize("empty", (False, True))
 @pytest.mark.parametrize("how", DRAFTS)
-@pytest.mark.parametrize("name", GENERAL)
+@pytest.mark.parametrize("name", [n for n in TREES if TREES[n][4] > 1])
 def test_what_a_drafted_token_holds_reaches_only_those_who_see_it(name, how, empty):
     s, N, lengths, x, sees = tree_inputs(name, 905)
     spoil_draft(x, sees, how)
     check_tree(s, N, [0, 33] if empty else lengths, x, sees, how)
+
+
+@pytest.mark.parametrize("name", [n for n in TREES if TREES[n][4] > 1])
+def test_many_drafted_tokens_with_infinite_values(name):
+    """Most of the draft: every word and every row of a tile has some."""
+    s, N, lengths, x, sees = tree_inputs(name, 906)
+    for t in range(0, N, 3):
+        x[4][:, :, t, t % s.d_h] = INF if t % 2 else NAN
+    x[2][1, 1, lengths[1] - 1, 2] = INF  # and the last row of the cache, which all see
+    check_tree(s, N, lengths, x, sees, "many")
+
+
+@pytest.mark.parametrize("name", list(ONE))
+def test_infinite_values_of_the_last_row(name):
+    """Tokens behind the last one are not that one again, with weight zero."""
+    dtype, n_rep, d, L = ONE[name]
+    lengths, c, k = [L, 1, 33], 60, 600
+    s = shape_of(2, n_rep, d, L, 3, dtype, k=k)
+    g = torch.Generator().manual_seed(907)
+    q, K, V = (torch.randn(x, generator=g).to(DT[dtype]) for x in ((3, s.H_q, d), (3, 2, L, d), (3, 2, L, d)))
+    for b, n in enumerate(lengths):
+        V[b, :, n - 1], V[b, 1, n - 1, 3] = INF, -INF
+    marks = torch.randn((3, 2, L // c, d), generator=g).to(DT[dtype])
+    dev = [x.cuda() for x in (K, V, q, marks)]
+    out, sparse = torch.full_like(q, 7.0, device="cuda"), torch.full_like(q, 7.0, device="cuda")
+    blocks, ws = torch.full((3, 1, 2, k // c), -7, dtype=torch.int32, device="cuda"), workspace(s, 1, c)
+    xb.xkv_dense_decode_weights(s, dev[0], dev[1], ints(lengths), dev[2], out, torch.zeros((3, 2, L), device="cuda"), ws)
+    xb.xkv_block_decode(s, dev[0], dev[1], ints(lengths), dev[2], 1, dev[3], c, sparse, blocks, ws)
+    torch.cuda.synchronize()
+    for b, n in enumerate(lengths):
+        for h in range(2):
+            heads = slice(h * n_rep, (h + 1) * n_rep)
+            t = torch.tensor([j * c + x for j in blocks.cpu()[b, 0, h].tolist() for x in range(c) if j * c + x < n], dtype=torch.long)
+            for got, rows in ((out, torch.arange(n)), (sparse, t)):
+                want, _, bound, _ = attend(q[b, heads], K[b, h, rows], V[b, h, rows], torch.ones((n_rep, len(rows)), dtype=torch.bool), scale_of(s))
+                same(got.cpu()[b, heads], want, bound, f"{b} {h}")
