@@ -13,6 +13,7 @@ template <typename T> static inline T *at(void *ws, size_t off) { return reinter
 static inline xkv_status hip_status(hipError_t e) { return e == hipSuccess ? XKV_OK : XKV_ERR_HIP; }
 
 constexpr int kMaxDraft = 1024;        // drafted tokens of a sequence
+constexpr int kMaxBlocks = kMaxCacheParts * (kPartBlocks - 128);  // blocks of a query, as many as all parts of the longest round hold, for any type
 constexpr int kMaxPlaces = 1 << 30;    // rows and drafted tokens of a sequence: sums of two places are ints
 
 // Scratch of launch_topk for p.sel_shape, and room for what it selects from and for the ids.
@@ -49,7 +50,7 @@ xkv_status plan_cache_attend(const xkv_shape &s, CacheMode mode, int N, int c, C
         p.n_c = ceil_div(s.L, c);
         p.k_ch = ceil_div(s.k, c) < p.n_c ? ceil_div(s.k, c) : p.n_c;
         if ((long long)p.k_ch * c < most) most = (long long)p.k_ch * c;
-        if ((long long)p.k_ch * c > kMaxPlaces) return XKV_ERR_UNSUPPORTED;
+        if ((long long)p.k_ch * c > kMaxPlaces || p.k_ch > kMaxBlocks) return XKV_ERR_UNSUPPORTED;
         p.sel_shape = xkv_shape{1, s.H_kv, s.H_kv, 1, 1, 1, p.n_c, p.k_ch, (int32_t)(batch * N), XKV_F32, 1.0f};
         if (block_select_ok(p.n_c)) {
             const size_t rows = (size_t)batch * N * s.H_kv;
@@ -81,8 +82,7 @@ xkv_status plan_cache_attend(const xkv_shape &s, CacheMode mode, int N, int c, C
     if (mode == CacheMode::blocks) {
         p.parts = clampi(ceil_div(want, tiles * batch * N), 1, clampi(longest, 1, kMaxCacheParts));
         // (a part is a multiple of the round: blocks of few rows, up to a round more of them)
-        const int least = ceil_div(p.k_ch, kPartBlocks - p.round);
-        if (least > kMaxCacheParts) return XKV_ERR_UNSUPPORTED;
+        const int least = ceil_div(p.k_ch, kPartBlocks - p.round);  // (at most kMaxCacheParts)
         if (p.parts < least) p.parts = least;
     } else {
         const long long all = batch * longest;

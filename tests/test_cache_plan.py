@@ -55,3 +55,11 @@ def test_blocks_of_a_part_fit_their_list(plan_of):
         assert p["k_ch"] == min(-(-s["k"] // s["c"]), p["n_c"])
         seen += p["parts"] > 1
     assert seen
+
+
+@pytest.mark.parametrize("dtype,d_h", [(1, 128), (1, 64), (0, 128), (0, 33)])
+def test_queries_of_any_type_have_the_same_number_of_blocks(plan_of, dtype, d_h):
+    most = 491520
+    shapes = [dict(mode=BLOCKS, L=600_000, k=k, dtype=dtype, d_h=d_h, N=1, c=c, batch=b)
+              for k, c, b in ((most, 1, 1), (most + 1, 1, 1), (507_904, 1, 1), (600_000, 1, 2), (600_000, 2, 2))]
+    assert [p["status"] for p in plan_of(shapes)] == [0, -2, -2, -2, 0]
