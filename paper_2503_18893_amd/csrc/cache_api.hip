@@ -41,7 +41,8 @@ xkv_status plan_cache_attend(const xkv_shape &s, CacheMode mode, int N, int c, C
     p.words = ceil_div(N, 32);
     p.scale = s.scale > 0.0f ? s.scale : 1.0f / std::sqrt((float)s.d_h);
     const long long batch = s.batch > 0 ? s.batch : 1;
-    if (batch * N * s.H_kv > 65535LL) return XKV_ERR_UNSUPPORTED;  // rows of the selection and of the merge are y of a grid
+    // One limit for all calls.  It is needed where blocks are selected by launch_topk or scored by block_scores_kernel: rows are y, queries z of a grid.
+    if (batch * N * s.H_kv > 65535LL) return XKV_ERR_UNSUPPORTED;
     if ((long long)s.L + N > kMaxPlaces) return XKV_ERR_UNSUPPORTED;
     size_t off = 0;
     long long most = s.L + (mode == CacheMode::tree ? N : 0);  // tokens of a query

@@ -63,3 +63,23 @@ def test_queries_of_any_type_have_the_same_number_of_blocks(plan_of, dtype, d_h)
     shapes = [dict(mode=BLOCKS, L=600_000, k=k, dtype=dtype, d_h=d_h, N=1, c=c, batch=b)
               for k, c, b in ((most, 1, 1), (most + 1, 1, 1), (507_904, 1, 1), (600_000, 1, 2), (600_000, 2, 2))]
     assert [p["status"] for p in plan_of(shapes)] == [0, -2, -2, -2, 0]
+
+
+def rounds_of_a_part(lengths, p):
+    """The smallest part, in rounds, with which all sequences' parts are at most p["parts"]."""
+    r = [-(-n // p["round"]) for n in lengths]
+    return next(m for m in range(1, max(r) + 1) if sum(-(-x // m) for x in r) <= p["parts"])
+
+
+def test_the_cases_of_many_tiles_have_many_tiles(plan_of):
+    """tests/test_gpu_cache_tiles.py means to run the loops over a part's tiles, with every number of rows."""
+    import test_gpu_cache_tiles as tiles
+    shapes = [dict(mode=TREE, H_kv=h, H_q=h * r, d_h=d, L=max(n), batch=len(n), N=N, dtype=int(t == "bf16")) for t, h, r, d, n, N, _, _ in tiles.TREES.values()]
+    for name, p in zip(tiles.TREES, plan_of(shapes)):
+        _, _, _, _, lengths, N, rows, rounds = tiles.TREES[name]
+        assert p["rows"] == rows, (name, p)
+        assert rounds_of_a_part([n + N for n in lengths], p) >= rounds, (name, p)
+    shapes = [dict(mode=BLOCKS, H_kv=h, H_q=h * r, d_h=d, L=L, k=k, batch=b, N=N, c=24, dtype=int(t == "bf16")) for t, h, r, d, b, N, L, k, _ in tiles.BLOCKS.values()]
+    for name, p in zip(tiles.BLOCKS, plan_of(shapes)):
+        k, parts = tiles.BLOCKS[name][-2:]
+        assert p["parts"] == parts and k / parts / p["round"] >= 5, (name, p)

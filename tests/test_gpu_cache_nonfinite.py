@@ -50,6 +50,7 @@ TREES = {
     "rows_128": ("bf16", 4, 128, 700, 32),
     "rows_256": ("bf16", 4, 128, 700, 64),
     "rows_400": ("bf16", 4, 128, 90, 100),
+    "rows_1024": ("bf16", 1, 128, 70, 1024),  # every word of a mask
 }
 
 
