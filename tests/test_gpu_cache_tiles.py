@@ -152,3 +152,31 @@ def test_evictions_at_the_borders_of_the_selection(L, in_place):
                 assert torch.equal(x[b, h, :k].cpu(), y[b, h, keep]), (b, h)
                 if in_place:
                     assert torch.equal(x[b, h, k:].cpu(), y[b, h, k:]), (b, h)
+
+
+@pytest.mark.parametrize("dtype,d,n_rep,N", [("f32", 40, 1, 3), ("bf16", 128, 4, 2), ("bf16", 128, 4, 8), ("bf16", 128, 2, 40)])
+@pytest.mark.parametrize("batch", (33, 65, 150))
+def test_many_sequences_of_any_lengths(dtype, d, n_rep, N, batch):
+    """More sequences than a wavefront has lanes, with fewer and more parts than sequences."""
+    g = torch.Generator(device="cuda").manual_seed(1400 + batch)
+    L = 700
+    lengths = torch.randint(0, L + 1, (batch,), generator=g, device="cuda", dtype=torch.int32)
+    lengths[3], lengths[-1], lengths[7] = 0, L, 1
+    s = shape_of(1, n_rep, d, L, batch, dtype)
+    q, K, V, Kd, Vd = (torch.randn(x, generator=g, device="cuda").to(DT[dtype]) for x in ((batch, N, n_rep, d), (batch, 1, L, d), (batch, 1, L, d), (batch, 1, N, d),
+                                                                                      (batch, 1, N, d)))
+    sees = random_trees(torch.Generator().manual_seed(2), batch, N)
+    out = run_tree(s, lengths, N, K, V, q, Kd, Vd, ref.pack_mask(sees).cuda()).cuda()
+    q1, one, total = q[:, 0].contiguous(), torch.full((batch, n_rep, d), float("nan"), dtype=DT[dtype], device="cuda"), torch.zeros((batch, 1, L), device="cuda")
+    xb.xkv_dense_decode_weights(s, K, V, lengths, q1, one, total, workspace(s))
+    for b, n in enumerate(lengths.tolist()):
+        mask = torch.cat((torch.ones((N, n), dtype=torch.bool), sees[b]), 1).repeat_interleave(n_rep, 0).cuda()
+        want, _, bound, _ = ref.attend(q[b].reshape(-1, d), torch.cat((K[b, 0, :n], Kd[b, 0])), torch.cat((V[b, 0, :n], Vd[b, 0])), mask, scale_of(s))
+        within(out[b].reshape(-1, d), want, bound, f"{b}")
+        if n == 0:
+            assert (one[b] == 0).all()
+            continue
+        want, p, bound, rel = ref.attend(q1[b], K[b, 0, :n], V[b, 0, :n], mask[:n_rep, :1].new_ones((n_rep, n)), scale_of(s))
+        within(one[b], want, bound, f"{b}")
+        assert ((total[b, 0, :n].double() - p.sum(0)).abs() <= (2 * rel + (n_rep + 2) * 2.0 ** -24) * p.sum(0) + 1e-30).all(), b
+        assert (total[b, 0, n:] == 0).all()
