@@ -54,8 +54,11 @@ __device__ __forceinline__ int cache_tokens(const CacheArgs &a, CacheMode mode, 
 // ------------------------------------------------------------------------------------------
 // Which workgroup takes what.  How many tokens a sequence has is known on the device only, and a cache may have far more room than
 // rows in use: every workgroup reads the lengths and finds for itself the smallest part, a multiple of `round` tokens, with which the
-// parts of all sequences are at most a.parts.  So any lengths fill the chip once, evenly.  One lane per sequence, then one per
-// candidate; about 1 us.
+// parts of all sequences are at most a.parts.  One lane per sequence, then one per candidate; about 1 us.
+// That is even where a.parts is a few times the number of sequences.  The parts planned include one of every sequence, so towards as many sequences
+// as parts they round up badly, and from there on a sequence is one part: with 8 KV heads and 64 drafted tokens (32 parts of 256 rows) 11 equal
+// sequences give 176 workgroups to 256 compute units, 17 of them 136; and one of 65536 tokens beside 32 of 1024 takes 1025 rounds where an
+// even share is 49.
 // ------------------------------------------------------------------------------------------
 struct CacheUnit {
     int seq, g, tile;    // sequence (blocks: of batch N queries), KV head, row tile

@@ -67,8 +67,8 @@ xkv_status plan_cache_attend(const xkv_shape &s, CacheMode mode, int N, int c, C
     }
     // The matrix-core kernel: as many rows per workgroup as there are, up to 256 (128 where that leaves fewer of them empty), one workgroup
     // to a compute unit (two of 128 rows).  The general one: 16 rows, rounds of 64 tokens, four workgroups.  384 rows by 128 / by 256, us:
-    // one sequence of 32768 tokens 81 / 85, four of 65536 513 / 570, two of 9457 67 / 57, two of 1000 36 / 33; 640 rows, 32768 tokens 134 /
-    // 172; just over 256 rows it makes no difference at 32768 tokens (260 rows 73 / 74), and 280 rows of four sequences 231 / 266.
+    // one sequence of 32768 tokens 99 / 103, four of 65536 571 / 680, two of 9457 73 / 65, two of 1000 28 / 29; 640 rows, 32768 tokens 161 /
+    // 226; 260 rows, 32768 tokens 91 / 93, 280 rows of four sequences 302 / 350; 512 rows of four sequences 728 / 716.
     const int M = mode == CacheMode::blocks ? p.n_rep : N * p.n_rep;
     p.mfma = s.dtype == XKV_BF16 && s.d_h == 128;
     p.rows = !p.mfma || M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : (ceil_div(M, 128) & 1) ? 128 : 256;

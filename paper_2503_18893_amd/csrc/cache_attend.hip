@@ -39,7 +39,8 @@ __device__ __forceinline__ uint32_t draft_bits(const CacheArgs &a, int seq, int 
 // General path, any type, width and alignment.  A round takes 64 tokens, whose keys and values go to LDS in single precision (the
 // next round's are requested before this one is computed).  For the logits a lane multiplies one of the keys with the four queries
 // of its wavefront, four channels a time; for the sums lanes run over the channels, and the weights go through LDS.  With few rows its time
-// is that of one round, latencies: 8 drafted tokens of 4 heads after 512 tokens, fp32, 9.7 us.
+// is that of one round, latencies: 8 drafted tokens of 4 heads after 512 tokens, fp32, 9.1 us.  Long caches are far from their bytes: 32768 tokens
+// of 8 KV heads with 4 query heads, one token, fp32 x 64 72 us (26 at the rate of a copy), x 128 107 (53), bf16 x 64 67 (13), x 256 296 (53).
 // ------------------------------------------------------------------------------------------
 __host__ __device__ inline int general_pitch(int d) { return ((d + 3) / 4 | 1) * 4; }  // floats; an odd number of 16-byte pieces
 
@@ -724,7 +725,8 @@ __global__ __launch_bounds__(64 * WR * WT, WR == 1 ? 1 : 2) void cache_tree_kern
 //   S^T: lane (row l % 16, kk = l / 16), part h, register r: token 16 h + 4 kk + r;  O^T: block db, register r: channel 16 db + 4 kk + r
 // LDS: the 16-byte piece p of row t of K at p ^ t % 16 (a fragment read takes two neighbouring pieces of 8 rows each at a time), the 32-byte
 // piece u of row t of V at (u + t) % 8 (a transposing read takes one piece of 8 rows at a time).
-// In 32 x 32 tiles, half of them empty: 256 queries of a 128K prompt 240 us, now 223; weights over 8 x 32768 tokens 26.3, now 25.6.
+// In 32 x 32 tiles, half of them empty, against 16 x 16 (with one product for a weight): 256 queries of a 128K prompt 240 / 223 us, weights over
+// 8 x 32768 tokens 26.3 / 25.6.  The second product: the whole calls 263 -> 269 and 31.0 -> 31.4.
 // ------------------------------------------------------------------------------------------
 constexpr int kHeldLogits = 32;  // rows of 32 logits that a wavefront holds back
 
