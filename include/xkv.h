@@ -381,8 +381,9 @@ XKV_API xkv_status xkv_sr_decode_absorbed_q4(const xkv_shape *shape, int32_t lay
  * [batch][H_kv][L][d_h] have room for L = shape->L rows; lengths [batch] int32 (device, nullable: all L) says how many of a
  * sequence's rows are in use, from 0 to L (other values count as the nearer end).  Rows that are not in use may hold anything and are
  * not read into any result.  shape->G, r_k, r_v are ignored (any positive numbers).  Results do not depend on the order in which
- * workgroups run.  Softmax statistics and sums are fp32, weights enter the sums with 15 bits or more; out is rounded once.  Only a query that sees no token has a result of zeros:
- * a NaN in a query or in a key that it sees, a logit of +inf, or logits of -inf alone give NaN, as the formulas do.
+ * workgroups run.  Softmax statistics and sums are fp32, weights enter the sums held to 2^-15 or better; out is rounded once.  Only a
+ * query that sees no token has a result of zeros: a NaN in a query or in a key that it sees, a logit of +inf, or logits of -inf alone
+ * give NaN, as the formulas do.
  *
  * xkv_tree_decode: N drafted tokens of every sequence, whose keys and values are not in the cache yet, attend to the cache and to one
  *   another (the verification of a speculated tree).  q, out [batch][N][H_q][d_h], K_draft, V_draft [batch][H_kv][N][d_h]; tree

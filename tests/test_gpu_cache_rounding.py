@@ -1,4 +1,4 @@
-"""Softmax weights enter the sums of attention over an uncompressed cache with 16 bits and more: results are rounded once, at the end.
+"""Softmax weights enter the sums of attention over an uncompressed cache held to 2^-15: results are rounded once, at the end.
 
 The bound is that of cache_reference.attend without the half step that it allows for weights rounded to the storage type.  Instead: a
 weight as two bf16 numbers, the second one for what the first one leaves (at most 2^-7 of it), itself rounded (half a step, 2^-8):
