@@ -437,6 +437,79 @@ XKV_API xkv_status xkv_evict(const xkv_shape *shape, const void *K, const void *
                              int32_t sink, int32_t recent, int32_t L_out, void *K_out, void *V_out, float *weights_out,
                              int32_t *rows_out, int32_t *lengths_out, void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/*
+ * Rotary positions of queries and keys, as every call here that says "already rotated" expects them.  A rotation turns pairs of channels
+ * (a, b) of a head by the angle p f_j: p the token's position, f_j the pair's frequency in radians per position.  The first d_rot channels of a
+ * head take part, the others are copied.  Pairs j = 0 .. d_rot / 2 - 1 are channels (j, j + d_rot / 2) (XKV_ROPE_HALF, the arrangement of
+ * rope_theta above) or (2j, 2j + 1) (XKV_ROPE_INTERLEAVED).  With the amplitude m (0 means 1; scalings for long contexts use others):
+ *   XKV_ROPE_FORWARD   a' = m (a cos - b sin), b' = m (b cos + a sin)
+ *   XKV_ROPE_INVERSE   what undoes it: the angle -p f_j and 1 / m (a cache of rotated keys back to what xkv_factorize takes)
+ *   XKV_ROPE_GRADIENT  a gradient by the outputs to one by the inputs: the angle -p f_j and m
+ *
+ * xkv_rotate: q [batch][N][H_q][d_h] and K [batch][N][H_kv][d_h] in shape->dtype to q_out, K_out of the same sizes (either pair may be NULL,
+ *   not both); the rows of d_h numbers may lie anywhere: `*_at` (HOST pointers, nullable: contiguous as above) give the numbers from one
+ *   sequence, token and head to the next, so that slices of a projection's result, drafted keys [batch][H_kv][N][d_h] and rows of a cache
+ *   are taken as they lie.  Strides are not negative; rows of an output must not overlap (in the order of their strides each reaches
+ *   beyond all that is inside it).  In place: out = in with the same strides; otherwise outputs must not overlap inputs.  positions
+ *   [batch][N] int32 (device, nullable: 0 .. N - 1).  frequencies [d_rot / 2] double (device).  Angles are taken in double precision,
+ *   the rest in fp32, rounded once.  shape->G, r_k, r_v, L, k, scale are ignored.
+ * xkv_rope_frequencies: such a table, once per model (frequencies: device, [d_rot / 2]).  f_j = theta^(-2j / d_rot), and for contexts that are
+ *   longer than those a model was trained on, by `factor` (the other arguments are ignored where they are not named):
+ *     XKV_ROPE_PLAIN   as it is               XKV_ROPE_LINEAR  f_j / factor
+ *     XKV_ROPE_BASE    theta factor^(d_rot / (d_rot - 2)) in the place of theta (d_rot > 2)
+ *     XKV_ROPE_TURNS   f_j (t + (1 - t) / factor), t = (context f_j / (2 pi) - low) / (high - low) between 0 and 1: pairs with more than `high`
+ *                      turns over the `context` that the model was trained on stay, those with less than `low` are stretched
+ * XKV_ERR_INVALID_ARG for d_rot odd, < 2 or > d_h (xkv_rope_frequencies: > 256), N < 1, an amplitude or parameter that is negative or not finite,
+ * factor, theta or context of 0, low >= high, strides as above, in place with other strides; XKV_ERR_UNSUPPORTED where batch * N exceeds 2^30 or
+ * batch * N * (H_q + H_kv) 2^40.
+ */
+typedef struct xkv_rows {
+    int64_t sequence, token, head;  /* numbers (not bytes) from one to the next */
+} xkv_rows;
+typedef enum { XKV_ROPE_HALF = 0, XKV_ROPE_INTERLEAVED = 1 } xkv_rope_layout;
+typedef enum { XKV_ROPE_FORWARD = 0, XKV_ROPE_INVERSE = 1, XKV_ROPE_GRADIENT = 2 } xkv_rope_direction;
+typedef enum { XKV_ROPE_PLAIN = 0, XKV_ROPE_LINEAR = 1, XKV_ROPE_BASE = 2, XKV_ROPE_TURNS = 3 } xkv_rope_scaling;
+XKV_API xkv_status xkv_rope_frequencies(int32_t d_rot, float theta, int32_t scaling, float factor, float low, float high, float context,
+                                        double *frequencies, void *hip_stream);
+XKV_API xkv_status xkv_rotate(const xkv_shape *shape, int32_t d_rot, int32_t layout, int32_t direction, float amplitude,
+                              const double *frequencies, const int32_t *positions, int32_t N, const void *q, const xkv_rows *q_at,
+                              void *q_out, const xkv_rows *q_out_at, const void *K, const xkv_rows *K_at, void *K_out,
+                              const xkv_rows *K_out_at, void *hip_stream);
+
+/*
+ * An uncompressed cache held in 8 bits: codes K8, V8 [batch][H_kv][L][d_h], a byte each, and scales k_scales, v_scales [batch][H_kv][n_c] fp32,
+ * one for every block of c rows of a KV head, n_c = ceil(L / c), c a power of two (1: every row its own).  A row is its codes times its
+ * block's scale.  Codes are XKV_E4M3 (4 bits of exponent, 3 of mantissa, largest value H = 448, 0x7F and 0xFF NaN, no infinities) or XKV_INT8
+ * (two's complement, H = 127; -128 counts as what it is).  Rows that are not in use may hold anything.
+ *
+ * xkv_cache8_append: the new rows K, V [batch][N][H_kv][d_h] in shape->dtype (`*_at` as in xkv_rotate) of every sequence go to its rows lengths[b],
+ *   lengths[b] + 1, .. .  lengths [batch] int32 (device, nullable: 0) are the rows in use before; counts [batch] (device, nullable: N) how many of a
+ *   sequence's N rows there are, the others are padding; both count as the nearer of their bounds (0 and L, 0 and N) and rows beyond L are
+ *   dropped.  The caller raises its lengths afterwards.  For a block that gets rows, a the largest magnitude of those:
+ *     no rows in use before, or a scale of 0:  s = max(a / H, 2^-126), or 0 where a = 0
+ *     otherwise:  s = 2^i times its scale with the smallest i >= 0 for which a <= H s (in fp32); where i > 0 its rows in use get the codes of
+ *       2^-i of their values, so that an int8 row, however often its block's scale grows, is off by at most one step of it
+ *   and new rows the codes of x / s (0 where s = 0); quotients in fp32, codes the nearest, ties to even.  An infinity or NaN in a new row makes
+ *   the block's scale NaN until the block begins anew, and new codes are 0 under a scale that is NaN.  Other rows and scales are left as they are.
+ * xkv_cache8_decode: query i of sequence b, q [batch][N][H_q][d_h], attends to the first visible[b][i] rows (device int32 [batch][N], nullable: all L; counts as
+ *   the nearer of 0 and L): a token after a cache, a drafted chain, or the tokens of a prompt, each with the rows up to its own.
+ *     z_t = scale k_scale[t / c] <q, K8_t>,  out = sum_t softmax(z)_t v_scale[t / c] V8_t;  out [batch][N][H_q][d_h] in shape->dtype.
+ *   Zeros for a query that sees nothing.  Sums and statistics are fp32; weights times scales enter the sums held to 2^-15 or better (fp32 shapes: fp32); rounded
+ *   once.  A NaN in a code or scale that a query sees gives NaN, one that it does not see does not reach it.  Scales are numbers from
+ *   2^-100 to 2^100, 0 or NaN: infinities, and products of a weight with a smaller scale, need not come out as the formula says.
+ *   Results do not depend on the order in which workgroups run.  workspace: xkv_cache8_workspace_bytes(shape, N) bytes, 256-byte aligned.
+ * shape->G, r_k, r_v, k are ignored.  XKV_ERR_INVALID_ARG for N < 1, c < 1, a code that is none of the two, strides as in xkv_rotate (negative);
+ * XKV_ERR_UNSUPPORTED for c that is not a power of two, L > 2^30, batch * N * H_q > 2^26, or more than 2^31 - 1 workgroups of blocks that an append can touch.
+ */
+typedef enum { XKV_E4M3 = 0, XKV_INT8 = 1 } xkv_code;
+XKV_API xkv_status xkv_cache8_append(const xkv_shape *shape, const void *K, const xkv_rows *K_at, const void *V, const xkv_rows *V_at,
+                                     const int32_t *lengths, const int32_t *counts, int32_t N, int32_t code, int32_t c, void *K8, void *V8,
+                                     float *k_scales, float *v_scales, void *hip_stream);
+XKV_API xkv_status xkv_cache8_workspace_bytes(const xkv_shape *shape, int32_t N, size_t *bytes);
+XKV_API xkv_status xkv_cache8_decode(const xkv_shape *shape, const void *K8, const void *V8, const float *k_scales, const float *v_scales,
+                                     int32_t code, int32_t c, const int32_t *visible, const void *q, int32_t N, void *out, void *workspace,
+                                     size_t workspace_bytes, void *hip_stream);
+
 /* Measurement aid for callers that want the duration of one kernel rather than of a whole call.
  * Not part of the method.  For stage = 0 (low-rank score kernel), 1 (gather-reconstruct + sparse
  * attention kernel), 2 (dense decode kernel), 3 (the Gram-matrix product X_cat^T X_cat of xkv_factorize, all

@@ -16,6 +16,10 @@ LIB_PATH = os.path.join(_HERE, "libxkv.so")
 XKV_OK, XKV_ERR_INVALID_ARG, XKV_ERR_UNSUPPORTED, XKV_ERR_WORKSPACE, XKV_ERR_HIP = 0, -1, -2, -3, -4
 XKV_F32, XKV_BF16 = 0, 1
 DTYPES = {"f32": XKV_F32, "bf16": XKV_BF16}
+CODES = {"e4m3": 0, "int8": 1}
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_DIRECTIONS = {"forward": 0, "inverse": 1, "gradient": 2}
+ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "turns": 3}
 
 ENTRY_POINTS = ("xkv_workspace_bytes", "xkv_sr_decode", "xkv_sr_decode_static", "xkv_packed_b_bytes", "xkv_pack_b",
                 "xkv_sr_decode_packed", "xkv_sr_decode_tail", "xkv_dense_decode", "xkv_score",
@@ -28,6 +32,7 @@ ENTRY_POINTS = ("xkv_workspace_bytes", "xkv_sr_decode", "xkv_sr_decode_static", 
                 "xkv_sr_decode_landmark_packed", "xkv_sr_decode_tail_packed",
                 "xkv_cache_workspace_bytes", "xkv_tree_decode", "xkv_block_decode", "xkv_landmarks_update",
                 "xkv_dense_decode_weights", "xkv_evict",
+                "xkv_rope_frequencies", "xkv_rotate", "xkv_cache8_append", "xkv_cache8_workspace_bytes", "xkv_cache8_decode",
                 "xkv_profile_kernel", "xkv_status_string", "xkv_version")
 
 
@@ -41,6 +46,10 @@ class xkv_shape(ctypes.Structure):
     _fields_ = [("G", ctypes.c_int32), ("H_kv", ctypes.c_int32), ("H_q", ctypes.c_int32), ("d_h", ctypes.c_int32),
                 ("r_k", ctypes.c_int32), ("r_v", ctypes.c_int32), ("L", ctypes.c_int32), ("k", ctypes.c_int32),
                 ("batch", ctypes.c_int32), ("dtype", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class xkv_rows(ctypes.Structure):
+    _fields_ = [("sequence", ctypes.c_int64), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
 
 
 @dataclass(frozen=True)
@@ -124,6 +133,12 @@ def load() -> ctypes.CDLL:
         lib.xkv_landmarks_update.argtypes = [sp, vp, vp, i32, i32, vp, vp]
         lib.xkv_dense_decode_weights.argtypes = [sp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         lib.xkv_evict.argtypes = [sp, vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+        rp, f32 = ctypes.POINTER(xkv_rows), ctypes.c_float
+        lib.xkv_rope_frequencies.argtypes = [i32, f32, i32, f32, f32, f32, f32, vp, vp]
+        lib.xkv_rotate.argtypes = [sp, i32, i32, i32, f32, vp, vp, i32, vp, rp, vp, rp, vp, rp, vp, rp, vp]
+        lib.xkv_cache8_append.argtypes = [sp, vp, rp, vp, rp, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp]
+        lib.xkv_cache8_workspace_bytes.argtypes = [sp, i32, ctypes.POINTER(sz)]
+        lib.xkv_cache8_decode.argtypes = [sp, vp, vp, vp, vp, i32, i32, vp, vp, i32, vp, vp, sz, vp]
         lib.xkv_profile_kernel.argtypes = [i32, vp, vp]
         lib.xkv_status_string.argtypes = [ctypes.c_int]
         lib.xkv_status_string.restype = ctypes.c_char_p
@@ -435,6 +450,49 @@ def xkv_evict(shape, K, V, weights, lengths, sink, recent, L_out, K_out, V_out, 
     _check(load().xkv_evict(ctypes.byref(shape.c()), _ptr(K), _ptr(V), _ptr(weights), _ptr(lengths), int(sink), int(recent),
                             int(L_out), _ptr(K_out), _ptr(V_out), _ptr(weights_out), _ptr(rows_out), _ptr(lengths_out),
                             _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)), "xkv_evict")
+
+
+def _rows(t):
+    """Where the rows of a tensor [batch][N][heads][d_h] lie, whose last axis is contiguous; None for no tensor."""
+    if t is None:
+        return None
+    if t.dim() != 4 or (t.stride(3) != 1 and t.shape[3] != 1):
+        raise ValueError("rows are wanted as a tensor [batch][N][heads][d_h] with a contiguous last axis")
+    return ctypes.byref(xkv_rows(t.stride(0), t.stride(1), t.stride(2)))
+
+
+def xkv_rope_frequencies(d_rot, theta, scaling, factor, low, high, context, frequencies, stream=None):
+    """scaling: "plain", "linear", "base" or "turns"."""
+    _check(load().xkv_rope_frequencies(int(d_rot), float(theta), ROPE_SCALINGS[scaling], float(factor), float(low), float(high),
+                                       float(context), _ptr(frequencies), _stream(stream)), "xkv_rope_frequencies")
+
+
+def xkv_rotate(shape, d_rot, layout, direction, amplitude, frequencies, positions, N, q, q_out, K, K_out, stream=None):
+    """layout: "half" or "interleaved"; direction: "forward", "inverse" or "gradient".  q, q_out, K, K_out are [batch][N][heads][d_h] with any
+    strides over the first three axes (views are taken as they are); q and q_out, or K and K_out, may be None."""
+    _check(load().xkv_rotate(ctypes.byref(shape.c()), int(d_rot), ROPE_LAYOUTS[layout], ROPE_DIRECTIONS[direction], float(amplitude),
+                             _ptr(frequencies), _ptr(positions), int(N), _ptr(q), _rows(q), _ptr(q_out), _rows(q_out), _ptr(K), _rows(K),
+                             _ptr(K_out), _rows(K_out), _stream(stream)), "xkv_rotate")
+
+
+def xkv_cache8_append(shape, K, V, lengths, counts, N, code, c, K8, V8, k_scales, v_scales, stream=None):
+    """code: "e4m3" or "int8".  K, V are [batch][N][H_kv][d_h] with any strides over the first three axes."""
+    _check(load().xkv_cache8_append(ctypes.byref(shape.c()), _ptr(K), _rows(K), _ptr(V), _rows(V), _ptr(lengths), _ptr(counts), int(N),
+                                    CODES[code], int(c), _ptr(K8), _ptr(V8), _ptr(k_scales), _ptr(v_scales), _stream(stream)),
+           "xkv_cache8_append")
+
+
+def xkv_cache8_workspace_bytes(shape: Shape, N: int = 1) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().xkv_cache8_workspace_bytes(ctypes.byref(shape.c()), int(N), ctypes.byref(n)), "xkv_cache8_workspace_bytes")
+    return int(n.value)
+
+
+def xkv_cache8_decode(shape, K8, V8, k_scales, v_scales, code, c, visible, q, N, out, workspace, stream=None):
+    """code: "e4m3" or "int8"."""
+    _check(load().xkv_cache8_decode(ctypes.byref(shape.c()), _ptr(K8), _ptr(V8), _ptr(k_scales), _ptr(v_scales), CODES[code], int(c),
+                                    _ptr(visible), _ptr(q), int(N), _ptr(out), _ptr(workspace),
+                                    workspace.numel() * workspace.element_size(), _stream(stream)), "xkv_cache8_decode")
 
 
 STAGE_SCORE, STAGE_GATHER_ATTEND, STAGE_DENSE, STAGE_FACTORIZE_GRAM, STAGE_ABSORB_ROWS = 0, 1, 2, 3, 4

@@ -102,7 +102,8 @@ __device__ __forceinline__ int ceil_div_dev(int a, int b) { return (int)(((unsig
 // so m is at least R / parts, and R / (parts - batch) is enough.  A lane counts for one m between the two.  Divisions are
 // products with a reciprocal, a factor of 1 + 2^-20 upwards: never too few, and exact up to 2^20 rounds of a sequence ((r + m - 1) / m
 // is a multiple of 1 / m).
-__device__ __forceinline__ int cache_chunk(const CacheArgs &a, CacheMode mode, int t)
+// ARGS: CacheArgs, or another problem with parts, round, batch, H_kv and table of the same meaning and its own cache_rows and cache_tokens.
+template <typename ARGS> __device__ __forceinline__ int cache_chunk(const ARGS &a, CacheMode mode, int t)
 {
     const int lane = lane_id(), shift = __builtin_ctz(a.round);  // (a power of two)
     constexpr float UP = 1.0f + 0x1p-20f;
@@ -136,7 +137,7 @@ __device__ __forceinline__ int cache_chunk(const CacheArgs &a, CacheMode mode, i
     return (best > 0 && best < top ? best : top) << shift;
 }
 
-__device__ __forceinline__ CacheUnit cache_unit(const CacheArgs &a, CacheMode mode, int tiles)
+template <typename ARGS> __device__ __forceinline__ CacheUnit cache_unit(const ARGS &a, CacheMode mode, int tiles)
 {
     CacheUnit u{};
     const int lane = lane_id();

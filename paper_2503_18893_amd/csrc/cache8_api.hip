@@ -1,0 +1,218 @@
+// C ABI of rotary positions and of the cache held in 8 bits: argument checks, plans, workspace.
+#include <cmath>
+#include <cstring>
+
+#include "cache8.h"
+
+namespace xkv {
+
+static inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+static inline int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
+static inline int clampi(int x, int lo, int hi) { return x < lo ? lo : (x > hi ? hi : x); }
+static inline xkv_status hip_status(hipError_t e) { return e == hipSuccess ? XKV_OK : XKV_ERR_HIP; }
+
+namespace {
+
+// Where rows [sequences][tokens][heads] of d numbers lie; false for negative strides.
+bool rows_at(const xkv_rows *at, int N, int heads, int d, xkv_rows &r)
+{
+    r = at ? *at : xkv_rows{(int64_t)N * heads * d, (int64_t)heads * d, d};
+    return r.sequence >= 0 && r.token >= 0 && r.head >= 0;
+}
+
+// Whether no two rows share a number: in the order of their strides, each reaches beyond all that is inside it.
+bool rows_apart(const xkv_rows &r, int batch, int N, int heads, int d)
+{
+    struct { int64_t stride; int64_t count; } axis[3] = {{r.sequence, batch}, {r.token, N}, {r.head, heads}};
+    for (int i = 0; i < 2; ++i)
+        for (int j = 0; j < 2 - i; ++j)
+            if (axis[j].stride > axis[j + 1].stride) std::swap(axis[j], axis[j + 1]);
+    unsigned __int128 reach = d;
+    for (const auto &x : axis) {
+        if (x.count <= 1) continue;
+        if ((unsigned __int128)x.stride < reach) return false;
+        reach += (unsigned __int128)x.stride * (uint64_t)(x.count - 1);
+    }
+    return reach < ((unsigned __int128)1 << 62);
+}
+
+bool same_rows(const xkv_rows &x, const xkv_rows &y, int batch, int N, int heads)
+{
+    return (batch <= 1 || x.sequence == y.sequence) && (N <= 1 || x.token == y.token) && (heads <= 1 || x.head == y.head);
+}
+
+xkv_status check_blocks(const xkv_shape &s, int32_t code, int32_t c, int &shift, int &n_c)
+{
+    if (code != XKV_E4M3 && code != XKV_INT8) return XKV_ERR_INVALID_ARG;
+    if (c < 1) return XKV_ERR_INVALID_ARG;
+    if ((c & (c - 1)) != 0 || s.L > (1 << 30)) return XKV_ERR_UNSUPPORTED;
+    shift = __builtin_ctz((unsigned)c);
+    n_c = ceil_div(s.L, c);
+    return XKV_OK;
+}
+
+xkv_status plan_cache8(const xkv_shape &s, int N, Cache8Plan &p)
+{
+    std::memset(&p, 0, sizeof p);
+    if (N < 1) return XKV_ERR_INVALID_ARG;
+    const long long batch = s.batch > 0 ? s.batch : 1;
+    if (s.L > (1 << 30) || batch * N > (1LL << 26) || batch * N * s.H_q > (1LL << 26)) return XKV_ERR_UNSUPPORTED;
+    p.n_rep = s.H_q / s.H_kv;
+    p.scale = s.scale > 0.0f ? s.scale : 1.0f / std::sqrt((float)s.d_h);
+    const long long M = (long long)N * p.n_rep;
+    p.mfma = false;
+    p.rows = 16;
+    p.round = 64;
+    const int want = 1024;
+    const int row_tiles = ceil_div(M, p.rows), longest = ceil_div(s.L, p.round);
+    p.by_length = row_tiles == 1;
+    const long long units = (long long)s.H_kv * row_tiles * (p.by_length ? 1 : batch);
+    if (p.by_length) {
+        const long long all = batch * longest;
+        p.parts = clampi(ceil_div(want, units), (int)batch, (int)(all < (1 << 30) ? all : 1 << 30));
+        if (p.parts > batch + kMaxCacheParts - 1) p.parts = (int)batch + kMaxCacheParts - 1;
+    } else {
+        p.parts = clampi(ceil_div(want, units), 1, clampi(longest, 1, kMaxCacheParts));
+    }
+    const size_t part_rows = (size_t)p.parts * (p.by_length ? 1 : batch) * N * s.H_q;
+    size_t off = align_up(((size_t)batch + 1) * sizeof(int32_t), 256);
+    p.off_part_o = off;
+    off = align_up(off + part_rows * s.d_h * sizeof(float), 256);
+    p.off_part_ml = off;
+    p.total = align_up(off + part_rows * 2 * sizeof(float), 256);
+    return XKV_OK;
+}
+
+}  // namespace
+}  // namespace xkv
+
+using namespace xkv;
+
+extern "C" {
+
+xkv_status xkv_rope_frequencies(int32_t d_rot, float theta, int32_t scaling, float factor, float low, float high, float context,
+                                double *frequencies, void *hip_stream)
+{
+    if (!frequencies || d_rot < 2 || d_rot % 2 || d_rot > 256 || scaling < XKV_ROPE_PLAIN || scaling > XKV_ROPE_TURNS) return XKV_ERR_INVALID_ARG;
+    if (!(theta > 0.0f) || !std::isfinite(theta)) return XKV_ERR_INVALID_ARG;
+    if (scaling != XKV_ROPE_PLAIN && (!(factor > 0.0f) || !std::isfinite(factor))) return XKV_ERR_INVALID_ARG;
+    if (scaling == XKV_ROPE_BASE && d_rot == 2) return XKV_ERR_INVALID_ARG;
+    if (scaling == XKV_ROPE_TURNS && (!(low >= 0.0f) || !(high > low) || !std::isfinite(high) || !(context > 0.0f) || !std::isfinite(context)))
+        return XKV_ERR_INVALID_ARG;
+    return hip_status(launch_rope_frequencies(d_rot, theta, scaling, factor, low, high, context, frequencies, (hipStream_t)hip_stream));
+}
+
+xkv_status xkv_rotate(const xkv_shape *shape, int32_t d_rot, int32_t layout, int32_t direction, float amplitude, const double *frequencies,
+                      const int32_t *positions, int32_t N, const void *q, const xkv_rows *q_at, void *q_out, const xkv_rows *q_out_at,
+                      const void *K, const xkv_rows *K_at, void *K_out, const xkv_rows *K_out_at, void *hip_stream)
+{
+    xkv_status st = validate(shape);
+    if (st != XKV_OK) return st;
+    const xkv_shape &s = *shape;
+    if (N < 1 || d_rot < 2 || d_rot % 2 || d_rot > s.d_h || !frequencies) return XKV_ERR_INVALID_ARG;
+    if ((layout != XKV_ROPE_HALF && layout != XKV_ROPE_INTERLEAVED) || direction < XKV_ROPE_FORWARD || direction > XKV_ROPE_GRADIENT)
+        return XKV_ERR_INVALID_ARG;
+    if (!(amplitude >= 0.0f) || !std::isfinite(amplitude) || (amplitude > 0.0f && !std::isfinite(1.0f / amplitude))) return XKV_ERR_INVALID_ARG;
+    if (!q != !q_out || !K != !K_out || (!q && !K)) return XKV_ERR_INVALID_ARG;
+    if ((long long)s.batch * N > (1LL << 30) || (long long)s.batch * N * ((long long)s.H_q + s.H_kv) > (1LL << 40)) return XKV_ERR_UNSUPPORTED;
+    const float m = amplitude > 0.0f ? amplitude : 1.0f;
+    RotateArgs a{};
+    a.x[0] = q, a.x[1] = K;
+    a.y[0] = q_out, a.y[1] = K_out;
+    const xkv_rows *in[2] = {q_at, K_at}, *to[2] = {q_out_at, K_out_at};
+    for (int i = 0; i < 2; ++i) {
+        if (!a.x[i]) continue;
+        a.heads[i] = i == 0 ? s.H_q : s.H_kv;
+        if (!rows_at(in[i], N, a.heads[i], s.d_h, a.x_at[i]) || !rows_at(to[i], N, a.heads[i], s.d_h, a.y_at[i])) return XKV_ERR_INVALID_ARG;
+        if (!rows_apart(a.y_at[i], s.batch, N, a.heads[i], s.d_h)) return XKV_ERR_INVALID_ARG;
+        if (a.x[i] == a.y[i] && !same_rows(a.x_at[i], a.y_at[i], s.batch, N, a.heads[i])) return XKV_ERR_INVALID_ARG;
+    }
+    if (s.batch == 0) return XKV_OK;
+    a.positions = positions;
+    a.frequencies = frequencies;
+    a.batch = s.batch;
+    a.N = N;
+    a.d_h = s.d_h;
+    a.d_rot = d_rot;
+    a.amplitude = direction == XKV_ROPE_INVERSE ? 1.0f / m : m;
+    a.sign = direction == XKV_ROPE_FORWARD ? 1.0f : -1.0f;
+    return hip_status(launch_rotate(s, a, layout == XKV_ROPE_INTERLEAVED, (hipStream_t)hip_stream));
+}
+
+xkv_status xkv_cache8_append(const xkv_shape *shape, const void *K, const xkv_rows *K_at, const void *V, const xkv_rows *V_at,
+                             const int32_t *lengths, const int32_t *counts, int32_t N, int32_t code, int32_t c, void *K8, void *V8,
+                             float *k_scales, float *v_scales, void *hip_stream)
+{
+    xkv_status st = validate(shape);
+    if (st != XKV_OK) return st;
+    const xkv_shape &s = *shape;
+    Cache8Append a{};
+    if (N < 1 || !K || !V || !K8 || !V8 || !k_scales || !v_scales) return XKV_ERR_INVALID_ARG;
+    if ((st = check_blocks(s, code, c, a.shift, a.n_c)) != XKV_OK) return st;
+    if (!rows_at(K_at, N, s.H_kv, s.d_h, a.K_at) || !rows_at(V_at, N, s.H_kv, s.d_h, a.V_at)) return XKV_ERR_INVALID_ARG;
+    const int most = N < s.L ? N : s.L;  // rows that there is room for
+    a.blocks = (int)(((long long)most - 1) / c) + 2 < a.n_c ? (int)(((long long)most - 1) / c) + 2 : a.n_c;
+    if ((long long)a.blocks * 2 * s.H_kv * s.batch > 0x7FFFFFFFLL) return XKV_ERR_UNSUPPORTED;
+    if (s.batch == 0) return XKV_OK;
+    a.K = K, a.V = V;
+    a.lengths = lengths;
+    a.counts = counts;
+    a.K8 = (uint8_t *)K8, a.V8 = (uint8_t *)V8;
+    a.k_scales = k_scales, a.v_scales = v_scales;
+    a.N = N;
+    a.L = s.L;
+    a.H_kv = s.H_kv;
+    a.d_h = s.d_h;
+    a.batch = s.batch;
+    return hip_status(launch_cache8_append(s, a, code, (hipStream_t)hip_stream));
+}
+
+xkv_status xkv_cache8_workspace_bytes(const xkv_shape *shape, int32_t N, size_t *bytes)
+{
+    if (!bytes) return XKV_ERR_INVALID_ARG;
+    xkv_status st = validate(shape);
+    if (st != XKV_OK) return st;
+    Cache8Plan p;
+    if ((st = plan_cache8(*shape, N, p)) != XKV_OK) return st;
+    *bytes = p.total;
+    return XKV_OK;
+}
+
+xkv_status xkv_cache8_decode(const xkv_shape *shape, const void *K8, const void *V8, const float *k_scales, const float *v_scales,
+                             int32_t code, int32_t c, const int32_t *visible, const void *q, int32_t N, void *out, void *workspace,
+                             size_t workspace_bytes, void *hip_stream)
+{
+    xkv_status st = validate(shape);
+    if (st != XKV_OK) return st;
+    const xkv_shape &s = *shape;
+    Cache8Args a{};
+    Cache8Plan p;
+    if (!K8 || !V8 || !k_scales || !v_scales || !q || !out) return XKV_ERR_INVALID_ARG;
+    if ((st = check_blocks(s, code, c, a.shift, a.n_c)) != XKV_OK) return st;
+    if ((st = plan_cache8(s, N, p)) != XKV_OK) return st;
+    if (!workspace || ((uintptr_t)workspace & 255u)) return XKV_ERR_INVALID_ARG;
+    if (workspace_bytes < p.total) return XKV_ERR_WORKSPACE;
+    if (s.batch == 0) return XKV_OK;
+    a.K8 = (const uint8_t *)K8, a.V8 = (const uint8_t *)V8;
+    a.k_scales = k_scales, a.v_scales = v_scales;
+    a.q = q;
+    a.visible = visible;
+    a.out = out;
+    a.table = (int32_t *)((char *)workspace + p.off_table);
+    a.part_o = (float *)((char *)workspace + p.off_part_o);
+    a.part_ml = (float *)((char *)workspace + p.off_part_ml);
+    a.L = s.L;
+    a.H_kv = s.H_kv;
+    a.H_q = s.H_q;
+    a.d_h = s.d_h;
+    a.batch = s.batch;
+    a.N = N;
+    a.rows = p.rows;
+    a.round = p.round;
+    a.parts = p.parts;
+    a.by_length = p.by_length;
+    a.scale = p.scale;
+    return hip_status(launch_cache8_attend(s, a, code, p.mfma, (hipStream_t)hip_stream));
+}
+
+}  // extern "C"

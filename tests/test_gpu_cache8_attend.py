@@ -1,0 +1,331 @@
+"""xkv_cache8_decode through the C ABI against a plain implementation in double precision (cache_reference.py, which also derives the
+tolerances), and a serving step of all the calls on a cache held in 8 bits.  Rows that no query sees hold NaN codes or NaN scales."""
+import pytest
+import torch
+
+import cache8_reference as ref8
+import cache_reference as ref
+from paper_2503_18893_amd import binding as xb
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(autouse=True)
+def need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+def shape_of(H_kv, n_rep, d, L, batch, dtype, scale=0.0):
+    return xb.Shape(1, H_kv, H_kv * n_rep, d, 1, 1, L, 1, batch, dtype, scale)
+
+
+def workspace(s, N=1):
+    return torch.full((xb.xkv_cache8_workspace_bytes(s, N),), 0xFF, dtype=torch.uint8, device="cuda")
+
+
+def cache(s, code, c, longest, seed, key_scale=1.0):
+    """K8, V8, k_scales, v_scales on the CPU: rows from longest[b] on hold NaN codes (e4m3) or anything, blocks of such rows alone a NaN scale."""
+    g = torch.Generator().manual_seed(seed)
+    n_c = -(-s.L // c)
+    c = min(c, s.L)
+    got = []
+    for which in "KV":
+        x = torch.randn((s.batch, s.H_kv, s.L, s.d_h), generator=g) * (key_scale if which == "K" else 1.0)
+        # blocks of very different magnitude
+        x = x * torch.randn((s.batch, s.H_kv, n_c, 1), generator=g).exp().repeat_interleave(c, 2)[:, :, : s.L]
+        pad = torch.nn.functional.pad(x, (0, 0, 0, n_c * c - s.L)).view(s.batch, s.H_kv, n_c, c * s.d_h)
+        scales = (pad.abs().amax(3) / ref8.HIGHEST[code]).clamp_min(2.0 ** -126)
+        codes = ref8.encode(x / scales.repeat_interleave(c, 2)[:, :, : s.L, None], code)
+        for b, n in enumerate(longest):
+            codes.view(torch.uint8)[b, :, n:] = 0x7F
+            scales[b, :, -(-n // c):] = float("nan")
+        got += [codes, scales]
+    return g, got[0], got[2], got[1], got[3]
+
+
+def within(got, want, bound, what):
+    err = (got.double() - want).abs()
+    assert torch.isfinite(got.double()).all(), what
+    worst = (err / bound).max().item()
+    assert worst <= 1.0, f"{what}: {worst:.3g} of the bound, largest error {err.max().item():.3g}"
+
+
+def run(s, code, c, visible, q, state, ws=None):
+    N = q.shape[1]
+    out = torch.full((s.batch, N, s.H_q, s.d_h), float("nan"), dtype=DT[s.dtype], device="cuda")
+    v = None if visible is None else torch.tensor(visible, dtype=torch.int32, device="cuda")
+    K8, V8, ks, vs = (x.cuda() for x in state)
+    xb.xkv_cache8_decode(s, K8, V8, ks, vs, code, c, v, q.cuda(), N, out, workspace(s, N) if ws is None else ws)
+    torch.cuda.synchronize()
+    return out.cpu()
+
+
+def check(s, code, c, visible, q, state, out, what):
+    n_rep, N = s.H_q // s.H_kv, q.shape[1]
+    K, V = ref8.rows(state[0], state[2], c), ref8.rows(state[1], state[3], c)
+    for b in range(s.batch):
+        seen = [min(max(x, 0), s.L) for x in visible[b]] if visible else [s.L] * N
+        n = max(seen)
+        sees = (torch.arange(n)[None] < torch.tensor(seen)[:, None]).repeat_interleave(n_rep, 0)
+        for g in range(s.H_kv):
+            heads = slice(g * n_rep, (g + 1) * n_rep)
+            want, _, bound, _ = ref.attend(q[b, :, heads].reshape(-1, s.d_h), K[b, g, :n], V[b, g, :n], sees, s.scale or s.d_h ** -0.5)
+            within(out[b, :, heads].reshape(-1, s.d_h), want, bound, f"{what} sequence {b} head {g}")
+        for i, x in enumerate(seen):
+            if x == 0:
+                assert (out[b, i] == 0).all()
+
+
+CASES = {
+    # name: dtype, H_kv, n_rep, d, L, c, visible (or N), key scale
+    "f32_tiny": ("f32", 1, 4, 64, 512, 16, [[512]], 1.0),
+    "f32_one_of_everything": ("f32", 1, 1, 1, 1, 1, [[1]], 1.0),
+    "f32_odd_width": ("f32", 2, 3, 33, 130, 4, [[130], [0], [7]], 1.0),
+    "f32_wide": ("f32", 1, 2, 256, 200, 32, [[65, 64, 0], [200, 1, 199]], 1.0),
+    "f32_128": ("f32", 2, 4, 128, 700, 64, [[700, 650], [64, 65]], 1.0),
+    "f32_every_row_its_own": ("f32", 1, 4, 64, 300, 1, [[300], [299]], 1.0),
+    "bf16_odd_width": ("bf16", 2, 5, 96, 300, 8, [[300], [64]], 1.0),
+    "bf16_64": ("bf16", 2, 8, 64, 500, 16, [[1], [500], [499]], 1.0),
+    "bf16_256": ("bf16", 1, 8, 256, 400, 16, [[399, 400], [1, 2]], 1.0),
+    "bf16_step": ("bf16", 8, 4, 128, 1000, 32, [[1000], [999], [33], [32], [31], [1], [0]], 1.0),
+    "bf16_seven_heads": ("bf16", 4, 7, 128, 1500, 16, [[1500], [777], [0]], 1.0),
+    "bf16_sixteen_heads": ("bf16", 1, 16, 128, 700, 64, [[700], [129]], 1.0),
+    "bf16_one_head": ("bf16", 3, 1, 128, 1200, 128, [[1200], [5]], 1.0),
+    "bf16_blocks_of_4": ("bf16", 2, 4, 128, 1001, 4, [[1001], [1000], [3]], 1.0),
+    "bf16_pairs": ("bf16", 2, 4, 128, 301, 2, [[301], [300]], 1.0),
+    "bf16_every_row_its_own": ("bf16", 2, 4, 128, 700, 1, [[700], [13]], 1.0),
+    "bf16_one_block": ("bf16", 2, 4, 128, 900, 1 << 30, [[900], [100]], 1.0),
+    "bf16_chain": ("bf16", 2, 7, 128, 1700, 16, [[1696, 1697, 1698, 1699, 1700], [0, 0, 1, 2, 3]], 1.0),
+    "bf16_four_rows": ("bf16", 2, 4, 128, 1100, 32, [[1097, 1098, 1099, 1100], [31, 32, 33, 34]], 1.0),
+    "bf16_nine": ("bf16", 2, 4, 128, 800, 32, [list(range(792, 801)), list(range(9))], 1.0),
+    "bf16_any_order": ("bf16", 2, 4, 128, 640, 32, [[640, 3, 0, 500, 77, 639, 64, 65, 1, 320], [9, 8, 7, 6, 5, 4, 3, 2, 1, 0]], 1.0),
+    "bf16_prompt": ("bf16", 2, 4, 128, 600, 16, [list(range(1, 601)), list(range(-100, 500))], 1.0),
+    "bf16_prompt_seven_heads": ("bf16", 1, 7, 128, 1000, 64, [list(range(900, 1000))], 1.0),
+    "bf16_prompt_64": ("bf16", 2, 4, 64, 400, 16, [list(range(300, 400))], 1.0),
+    "bf16_peaked": ("bf16", 2, 4, 128, 2000, 32, [[2000], [1500]], 12.0),
+    "bf16_long": ("bf16", 1, 4, 128, 20011, 32, [[20011]], 1.0),
+    "bf16_all_of_it": ("bf16", 2, 4, 128, 515, 32, None, 1.0),
+}
+
+
+@pytest.mark.parametrize("code", ["e4m3", "int8"])
+@pytest.mark.parametrize("case", list(CASES))
+def test_attend(case, code):
+    dtype, H_kv, n_rep, d, L, c, visible, key_scale = CASES[case]
+    batch, N = (len(visible), len(visible[0])) if visible else (2, 3)
+    s = shape_of(H_kv, n_rep, d, L, batch, dtype)
+    longest = [min(max(max(x), 0), L) for x in visible] if visible else [L] * batch
+    g, *state = cache(s, code, c, longest, 100 + len(case), key_scale)
+    q = torch.randn((batch, N, s.H_q, d), generator=g).to(DT[dtype])
+    out = run(s, code, c, visible, q, state)
+    check(s, code, c, visible, q, state, out, f"{case} {code}")
+
+
+def test_many_sequences_and_a_scale():
+    s = shape_of(1, 4, 128, 300, 70, "bf16", 0.02)
+    visible = [[(37 * b) % 301] for b in range(70)]
+    g, *state = cache(s, "e4m3", 16, [x[0] for x in visible], 1)
+    q = torch.randn((70, 1, 4, 128), generator=g).bfloat16()
+    check(s, "e4m3", 16, visible, q, state, run(s, "e4m3", 16, visible, q, state), "many sequences")
+
+
+def test_visible_outside_the_cache_counts_as_the_nearer_end():
+    s = shape_of(1, 4, 128, 100, 2, "bf16")
+    g, *state = cache(s, "int8", 16, [100, 100], 6)
+    q = torch.randn((2, 2, 4, 128), generator=g).bfloat16()
+    a = run(s, "int8", 16, [[1000, -5], [2 ** 31 - 1, -2 ** 31]], q, state)
+    assert torch.equal(a, run(s, "int8", 16, [[100, 0], [100, 0]], q, state)) and (a[:, 1] == 0).all()
+
+
+@pytest.mark.parametrize("code", ["e4m3", "int8"])
+@pytest.mark.parametrize("dtype,d,N", [("f32", 64, 3), ("bf16", 128, 1), ("bf16", 128, 4), ("bf16", 128, 40)])
+def test_nan_reaches_those_that_see_it(dtype, d, N, code):
+    """A NaN scale of keys or values, and (e4m3) a NaN code: rows of NaN, or one channel, for the queries that see it, and nothing for the others."""
+    s, c, L = shape_of(2, 4, d, 400, 2, dtype), 16, 400
+    seen = [list(range(300 - N + 1, 301))] * 2
+    g, *state = cache(s, code, c, [L, L], 8)
+    q = torch.randn((2, N, 8, d), generator=g).to(DT[dtype])
+    clean = run(s, code, c, seen, q, state)
+    for what in ("k_scale", "v_scale") + (("k_code", "v_code") if code == "e4m3" else ()):
+        for t in (5, 298 if N > 1 else 299):  # in the middle, and where the last queries end
+            bad = [x.clone() for x in state]
+            if what.endswith("scale"):
+                bad[2 if what[0] == "k" else 3][1, 0, t // c] = float("nan")
+                t = t // c * c
+            else:
+                bad[0 if what[0] == "k" else 1].view(torch.uint8)[1, 0, t, 7] = 0xFF
+            out = run(s, code, c, seen, q, bad)
+            hit = torch.zeros_like(clean, dtype=torch.bool)
+            for i in range(N):
+                if t < seen[1][i]:
+                    hit[1, i, :4, 7 if what == "v_code" else slice(None)] = True
+            assert torch.equal(out.isnan(), hit), (what, t)
+            assert torch.equal(out[~hit], clean[~hit]), (what, t)
+
+
+def test_a_query_that_is_nan():
+    s = shape_of(1, 4, 128, 300, 1, "bf16")
+    g, *state = cache(s, "e4m3", 32, [300], 8)
+    q = torch.randn((1, 2, 4, 128), generator=g).bfloat16()
+    q[0, 0, 1, 3] = float("nan")
+    out = run(s, "e4m3", 32, [[300, 299]], q, state)
+    assert out[0, 0, 1].isnan().all() and out.isnan().sum() == 128
+
+
+@pytest.mark.parametrize("N", [1, 6, 50])
+def test_pointers_that_are_not_aligned(N):
+    s, c = shape_of(2, 4, 128, 500, 2, "bf16"), 32
+    seen = [[500 - N + 1 + i for i in range(N)], [100 + i for i in range(N)]]
+    g, *state = cache(s, "e4m3", c, [500, 99 + N], 9)
+    q = torch.randn((2, N, 8, 128), generator=g).bfloat16()
+    want = run(s, "e4m3", c, seen, q, state)
+    check(s, "e4m3", c, seen, q, state, want, "aligned")
+    v = torch.tensor(seen, dtype=torch.int32, device="cuda")
+    for which in range(3):
+        def shifted(x, by):
+            room = torch.zeros(x.numel() * x.element_size() + 16, dtype=torch.uint8, device="cuda")
+            y = room[by:by + x.numel() * x.element_size()].view(x.dtype).view(x.shape)
+            y.view(torch.uint8).copy_(x.cuda().view(torch.uint8))
+            return y
+        K8, V8 = shifted(state[0], 1 if which == 0 else 0), shifted(state[1], 4 if which == 1 else 0)
+        qd = shifted(q, 2 if which == 2 else 0)
+        out = torch.empty_like(qd)
+        xb.xkv_cache8_decode(s, K8, V8, state[2].cuda(), state[3].cuda(), "e4m3", c, v, qd, N, out, workspace(s, N))
+        check(s, "e4m3", c, seen, q, state, out.cpu(), f"not aligned {which}")
+
+
+@pytest.mark.parametrize("dtype,code", [("bf16", "e4m3"), ("bf16", "int8"), ("f32", "e4m3")])
+def test_results_repeat_and_parts_do_not_matter_to_others(dtype, code):
+    """Twice the same, bit for bit; and a sequence's result does not change beyond rounding with what else is in the batch."""
+    s = shape_of(2, 4, 128, 3000, 3, dtype)
+    g, *state = cache(s, code, 32, [3000, 1234, 2999], 10)
+    q = torch.randn((3, 1, 8, 128), generator=g).to(DT[dtype])
+    seen = [[3000], [1234], [2999]]
+    a, b = run(s, code, 32, seen, q, state), run(s, code, 32, seen, q, state)
+    assert torch.equal(a, b)
+    check(s, code, 32, seen, q, state, a, "batch")
+
+
+def test_another_stream_and_a_captured_step():
+    """Rotate, append and attend as a serving loop does, captured once and replayed for token after token, on a stream of its own; every
+    replay against the same calls made one by one, and the last one against a plain implementation."""
+    s, c, code, N = shape_of(2, 4, 128, 300, 2, "bf16"), 16, "e4m3", 1
+    g = torch.Generator().manual_seed(2)
+    f = ref8.frequencies(128, 1e4)
+    fd = f.cuda()
+
+    def fresh():
+        t = [torch.zeros((2, 2, 300, 128), dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn) for _ in "KV"]
+        t += [torch.zeros((2, 2, -(-300 // c)), device="cuda") for _ in "KV"]
+        return dict(state=t, lengths=torch.zeros(2, dtype=torch.int32, device="cuda"), ws=workspace(s, N),
+                    qkv=torch.zeros((2, N, 12, 128), dtype=torch.bfloat16, device="cuda"),
+                    q=torch.zeros((2, N, 8, 128), dtype=torch.bfloat16, device="cuda"),
+                    K=torch.zeros((2, N, 2, 128), dtype=torch.bfloat16, device="cuda"),
+                    out=torch.zeros((2, N, 8, 128), dtype=torch.bfloat16, device="cuda"))
+
+    def step(t):
+        x = t["qkv"]
+        xb.xkv_rotate(s, 128, "half", "forward", 1.0, fd, t["lengths"], N, x[:, :, :8], t["q"], x[:, :, 8:10], t["K"])
+        xb.xkv_cache8_append(s, t["K"], x[:, :, 10:], t["lengths"], None, N, code, c, *t["state"])
+        t["lengths"] += 1
+        xb.xkv_cache8_decode(s, *t["state"], code, c, t["lengths"], t["q"], N, t["out"], t["ws"])
+
+    # a prompt of 40 tokens for the one, 23 for the other
+    prompt = torch.randn((2, 40, 12, 128), generator=g).bfloat16()
+    eager, held = fresh(), fresh()
+    for t in (eager, held):
+        K = torch.empty((2, 40, 2, 128), dtype=torch.bfloat16, device="cuda")
+        x = prompt.cuda()
+        xb.xkv_rotate(s, 128, "half", "forward", 1.0, fd, None, 40, None, None, x[:, :, 8:10], K)
+        xb.xkv_cache8_append(s, K, x[:, :, 10:], None, torch.tensor([40, 23], dtype=torch.int32, device="cuda"), 40, code, c, *t["state"])
+        t["lengths"].copy_(torch.tensor([40, 23], dtype=torch.int32))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    saved = [x.clone() for x in held["state"]] + [held["lengths"].clone()]
+    with torch.cuda.stream(side):
+        step(held)  # warm
+    torch.cuda.synchronize()
+    for x, y in zip(held["state"] + [held["lengths"]], saved):
+        x.view(torch.uint8).copy_(y.view(torch.uint8))
+    with torch.cuda.graph(graph, stream=side):
+        step(held)
+    for i in range(30):
+        x = torch.randn((2, N, 12, 128), generator=g).bfloat16().mul(1.0 + 0.2 * i)
+        for t in (eager, held):
+            t["qkv"].copy_(x)
+        step(eager)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(eager["state"] + [eager["out"], eager["lengths"]], held["state"] + [held["out"], held["lengths"]]):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), i
+    n = eager["lengths"].tolist()
+    assert n == [70, 53]
+    state = [x.cpu() for x in eager["state"]]
+    check(s, code, c, [[70], [53]], eager["q"].cpu(), state, eager["out"].cpu(), "serving")
+    # what is in the cache is what came in, rotated, within the codes' steps
+    p = torch.arange(40)[None].repeat(2, 1)
+    K, bound = ref8.rotate(prompt[:, :, 8:10], p, f, "half", "forward", 1.0)
+    got = ref8.rows(state[0], state[2], c)[0, :, :40].transpose(0, 1)
+    step_of = state[2][0].double().repeat_interleave(c, 1)[:, :40].transpose(0, 1)[..., None]
+    assert ((got - K[0]).abs() <= 2.0 ** -4 * K[0].abs() * (1 + 2.0 ** -8) + 2.0 ** -9 * step_of + 2 * bound[0]).all()
+
+
+def test_two_graphs_with_workspaces_of_their_own():
+    s, c = shape_of(2, 4, 128, 2000, 2, "bf16"), 32
+    g, *state = cache(s, "e4m3", c, [2000, 700], 11)
+    dev = [x.cuda() for x in state]
+    v = torch.tensor([[2000], [700]], dtype=torch.int32, device="cuda")
+    qs = [torch.randn((2, 1, 8, 128), generator=g).bfloat16() for _ in range(2)]
+    want = [run(s, "e4m3", c, [[2000], [700]], q, state) for q in qs]
+    graphs, outs, keep = [], [], []
+    for q in qs:
+        out, ws, qd, graph = torch.zeros((2, 1, 8, 128), dtype=torch.bfloat16, device="cuda"), workspace(s), q.cuda(), torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph):
+            xb.xkv_cache8_decode(s, *dev, "e4m3", c, v, qd, 1, out, ws)
+        graphs.append(graph)
+        outs.append(out)
+        keep.append((ws, qd))
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(5):
+        for graph, stream, out in zip(graphs, streams, outs):
+            out.zero_()
+            stream.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(stream):
+                graph.replay()
+        torch.cuda.synchronize()
+        for out, w in zip(outs, want):
+            assert torch.equal(out.cpu(), w)
+
+
+def test_more_than_two_gigabytes_of_codes():
+    """Offsets beyond 32 bits: the last sequence's rows are found, 2.2e9 codes behind the first."""
+    s, c = shape_of(4, 4, 128, 1 << 21, 2, "bf16"), 128
+    if torch.cuda.mem_get_info()[0] < 12 << 30:
+        pytest.skip("not enough memory")
+    K8, V8 = (torch.zeros((2, 4, s.L, 128), dtype=torch.int8, device="cuda") for _ in "KV")
+    ks, vs = (torch.zeros((2, 4, s.L // c), device="cuda") for _ in "KV")
+    n = s.L - 50
+    g = torch.Generator().manual_seed(1)
+    K, V = (torch.randn((2, 60, 4, 128), generator=g).bfloat16() for _ in "KV")
+    xb.xkv_cache8_append(s, K.cuda(), V.cuda(), torch.tensor([n, n], dtype=torch.int32, device="cuda"), None, 60, "int8", c, K8, V8, ks, vs)
+    q = torch.randn((2, 1, 16, 128), generator=g).bfloat16()
+    out = torch.empty((2, 1, 16, 128), dtype=torch.bfloat16, device="cuda")
+    xb.xkv_cache8_decode(s, K8, V8, ks, vs, "int8", c, None, q.cuda(), 1, out, workspace(s))
+    last = slice(s.L - c, s.L)
+    small = [K8[:, :, last].cpu(), V8[:, :, last].cpu(), ks[:, :, -1:].cpu(), vs[:, :, -1:].cpu()]
+    assert (small[0][:, :, -50:] != 0).any(-1).all()
+    # all other rows have keys and values of zero: their weights are known
+    for b in range(2):
+        for h in range(16):
+            kk, vv = ref8.rows(small[0], small[2], c)[b, h // 4], ref8.rows(small[1], small[3], c)[b, h // 4]
+            z = kk @ q[b, 0, h].double() / 128 ** 0.5
+            p = z.exp() / (z.exp().sum() + (s.L - c))
+            want, reach = p @ vv, p @ vv.abs()
+            # sums over 2^21 rows in fp32, of parts of at most 2^13 rows each in lanes: 2^-24 (2^10 + 2^8) relative, exponentials 2^-20, and bf16
+            assert ((out[b, 0, h].double().cpu() - want).abs() <= (2.0 ** -13 + 2.0 ** -7) * reach).all()
