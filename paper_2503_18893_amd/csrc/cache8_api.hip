@@ -60,19 +60,19 @@ xkv_status plan_cache8(const xkv_shape &s, int N, Cache8Plan &p)
     p.n_rep = s.H_q / s.H_kv;
     p.scale = s.scale > 0.0f ? s.scale : 1.0f / std::sqrt((float)s.d_h);
     const long long M = (long long)N * p.n_rep;
-    p.mfma = false;
-    p.rows = 16;
-    p.round = 64;
-    const int want = 1024;
+    p.mfma = s.dtype == XKV_BF16 && (s.d_h == 64 || s.d_h == 128 || s.d_h == 256);
+    p.rows = !p.mfma || M <= 16 ? 16 : M <= 32 || s.d_h == 256 ? 32 : 64;
+    p.round = p.mfma ? 128 : 64;
+    const int want = !p.mfma ? 1024 : p.rows == 16 ? 512 : 256;
     const int row_tiles = ceil_div(M, p.rows), longest = ceil_div(s.L, p.round);
     p.by_length = row_tiles == 1;
-    const long long units = (long long)s.H_kv * row_tiles * (p.by_length ? 1 : batch);
+    const long long units = (long long)s.H_kv * row_tiles;
     if (p.by_length) {
         const long long all = batch * longest;
         p.parts = clampi(ceil_div(want, units), (int)batch, (int)(all < (1 << 30) ? all : 1 << 30));
         if (p.parts > batch + kMaxCacheParts - 1) p.parts = (int)batch + kMaxCacheParts - 1;
     } else {
-        p.parts = clampi(ceil_div(want, units), 1, clampi(longest, 1, kMaxCacheParts));
+        p.parts = clampi(ceil_div(want, units * batch), 1, clampi(longest, 1, kMaxCacheParts));
     }
     const size_t part_rows = (size_t)p.parts * (p.by_length ? 1 : batch) * N * s.H_q;
     size_t off = align_up(((size_t)batch + 1) * sizeof(int32_t), 256);

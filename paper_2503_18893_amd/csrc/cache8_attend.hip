@@ -3,9 +3,12 @@
 // over the rows that a query sees, split over the rows: every workgroup leaves (maximum, sum, unnormalised output) of its part, in
 // powers of two, and a second kernel merges them.
 #include "cache8.h"
+#include "cache_tile.h"
 
 namespace xkv {
 namespace {
+
+using namespace cache_tile;
 
 constexpr int kGenTokens = 64;  // rows of the cache a round of the general kernel, a lane each
 constexpr int kGenRows = 16;    // its rows (query, head) per workgroup, four per wavefront
@@ -41,15 +44,20 @@ __device__ __forceinline__ int tile_chunk(const Cache8Args &a, int n)
 __device__ __forceinline__ Unit8 unit8(const Cache8Args &a)
 {
     Unit8 u{};
+    const int tiles = ceil_div_dev(a.N * (a.H_q / a.H_kv), a.rows);
     if (a.by_length) {
-        const CacheUnit c = cache_unit(a, CacheMode::weights, 1);
-        u.seq = c.seq, u.g = c.g, u.part = c.part, u.t_begin = c.t_begin, u.t_end = c.t_end, u.some = c.some;
+        const CacheUnit c = cache_unit(a, CacheMode::weights, tiles);
+        u.seq = c.seq, u.g = c.g, u.tile = c.tile, u.part = c.part, u.t_begin = c.t_begin, u.t_end = c.t_end, u.some = c.some;
         return u;
     }
-    const int tiles = (int)(((long long)a.N * (a.H_q / a.H_kv) + a.rows - 1) / a.rows);
-    int id = (int)blockIdx.x;
-    u.tile = tiles - 1 - id % tiles;  // (of a prompt the last ones see most)
-    id /= tiles;
+    // workgroups go to the eight XCDs in turn: the row tiles of a part, which share its rows of the cache, to one XCD, one after the other
+    const int x = (int)blockIdx.x;
+    int id = x / tiles, tile = x % tiles;
+    if ((int)gridDim.x % (8 * tiles) == 0) {
+        tile = x / 8 % tiles;
+        id = x / (8 * tiles) * 8 + x % 8;
+    }
+    u.tile = tiles - 1 - tile;  // (of a prompt the last ones see most)
     const int p = id % a.parts;
     id /= a.parts;
     u.g = id % a.H_kv;
@@ -177,6 +185,321 @@ __global__ __launch_bounds__(256) void cache8_general_kernel(Cache8Args a)
 }
 
 // ------------------------------------------------------------------------------------------
+// Matrix-core path: bf16, D channels, blocks of at least 4 rows.  A wavefront takes tiles of 32 rows of the cache on its own and 16 RT rows (query,
+// head):
+//   S^T [32 tokens x rows] = codes of K x Q^T,  P^T = exp2(c ks S^T - m),  O^T [channels x rows] += codes of V^T x (vs P^T)
+// Codes are bf16 numbers as they are (3 or 7 bits of mantissa), so both products take them exactly, and the scales, one for four tokens of a
+// lane, multiply logits and weights.  A lane holds one row of S^T, P^T and O^T (rows n16), so that the statistics are its own, and P^T is the second
+// product's operand as it comes.  Weights times scales enter as two bf16 terms, 2^-15.  Keys and values go from memory to registers: a lane's
+// pieces of K are its operands but for the conversion; of V it reads the tokens that it has weights of, D / 16 channels of each (a row of the
+// cache is read by 16 lanes), and pairs up neighbouring tokens by permuting bytes.  The next tile is requested as soon as this one's bytes
+// are converted.  The maximum is only raised when a logit outgrows it by 2^8.
+// ------------------------------------------------------------------------------------------
+template <int CODE> __device__ __forceinline__ u32x4_t codes8(uint32_t lo, uint32_t hi)
+{
+    u32x4_t x;
+    if constexpr (CODE == XKV_E4M3) {
+        x[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false));
+        x[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true));
+        x[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false));
+        x[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t w = (i < 2 ? lo : hi) >> (16 * (i & 1));
+            x[i] = __builtin_amdgcn_perm(__float_as_uint((float)(int8_t)(w >> 8)), __float_as_uint((float)(int8_t)w), 0x07060302u);  // (exact)
+        }
+    }
+    return x;
+}
+
+// Four channels of eight tokens, w[e] those of token e, as operands: x[j] channel j of the tokens.
+template <int CODE> __device__ __forceinline__ void codes_by_channel(const uint32_t (&w)[8], u32x4_t (&x)[4])
+{
+    if constexpr (CODE == XKV_E4M3) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t a = __builtin_bit_cast(uint32_t, h ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * i], 1.0f, true)
+                                                                  : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * i], 1.0f, false));
+                const uint32_t b = __builtin_bit_cast(uint32_t, h ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * i + 1], 1.0f, true)
+                                                                  : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * i + 1], 1.0f, false));
+                x[2 * h][i] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+                x[2 * h + 1][i] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+            }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                x[j][i] = __builtin_amdgcn_perm(__float_as_uint((float)(int8_t)(w[2 * i + 1] >> (8 * j))),
+                                                __float_as_uint((float)(int8_t)(w[2 * i] >> (8 * j))), 0x07060302u);
+    }
+}
+
+template <int N> struct Words {
+    uint32_t x[N];
+};
+template <int N> __device__ __forceinline__ Words<N> load_words(const uint8_t *from)
+{
+    typedef __attribute__((ext_vector_type(N))) uint32_t vec_t;
+    Words<N> r;
+    if constexpr (N == 1) {
+        r.x[0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(from));
+    } else {
+        const vec_t v = __builtin_nontemporal_load(reinterpret_cast<const vec_t *>(from));
+#pragma unroll
+        for (int i = 0; i < N; ++i) r.x[i] = v[i];
+    }
+    return r;
+}
+
+template <int CODE, int D, int RT>
+__global__ __launch_bounds__(256, RT == 1 && D < 256 ? 2 : 1) void cache8_mfma_kernel(Cache8Args a, bool direct)
+{
+    constexpr int KP = D / 64, VW = D / 64, JC = D / 16, STEPS = D / 32, PITCH = D / 4;  // pieces of K, words of V, channels of a lane; products; 16-byte pieces of a row
+    __shared__ f32x4_t sm_o[4][16 * PITCH];
+    __shared__ float sm_m[4][16], sm_l[4][16];
+    const Unit8 u = unit8(a);
+    const int lane = lane_id(), w = wave_id(), n16 = lane & 15, kk = lane >> 4, n_rep = a.H_q / a.H_kv, M = a.N * n_rep;
+    if (!u.some && !direct) return;  // (the merge knows)
+    const size_t head = (size_t)u.seq * a.H_kv + u.g;
+    const uint8_t *K = a.K8 + head * a.L * D, *V = a.V8 + head * a.L * D;
+    const float *ks = a.k_scales + head * a.n_c, *vs = a.v_scales + head * a.n_c, c = a.scale * kLog2e;
+
+    // Q^T operands: lane (row n16, kk), product s, position e: channel 64 (s / 2) + 16 kk + 8 (s % 2) + e, as the pieces of K have them
+    bf16x8_t Q[RT][STEPS];
+    int sees[RT], least = 0x7FFFFFFF;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int m = (u.tile * RT + rt) * 16 + n16, m_in = m < M ? m : M - 1, i = m_in / n_rep;
+        const bf16_t *q = (const bf16_t *)a.q + (((size_t)u.seq * a.N + i) * a.H_q + u.g * n_rep + m_in % n_rep) * D;
+        sees[rt] = visible8(a, u.seq, i);
+        least = sees[rt] < least ? sees[rt] : least;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) Q[rt][s] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t *>(q + 64 * (s / 2) + 16 * kk + 8 * (s % 2)));
+    }
+    least = -wave_all(-least, MaxOp());  // rows that all of them see
+    least = __builtin_amdgcn_readfirstlane(least < u.t_end ? least : u.t_end);
+
+    f32x4_t O[RT][JC];
+    float m_run[RT], l_run[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        m_run[rt] = -INFINITY;
+        l_run[rt] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < JC; ++j) O[rt][j] = f32x4_t(0.0f);
+    }
+
+    Words<4> kr[2][KP];
+    Words<VW> vr[8];
+    float ksr[2], vsr[2];
+    const uint32_t k_off = n16 * D + 16 * kk, v_off = 4 * kk * D + 4 * VW * n16;
+    auto request_k = [&](int t) __attribute__((always_inline)) {
+        const uint8_t *base = K + (size_t)t * D;
+        const int last = u.t_end - 1 - t;  // (rows behind the last one: that one again)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int row = 16 * h + n16;
+            const uint32_t off = last >= 31 ? k_off + 16 * h * D : (row < last ? row : last) * D + 16 * kk;
+#pragma unroll
+            for (int f = 0; f < KP; ++f) kr[h][f] = load_words<4>(base + off + 64 * f);
+            const int quad = 16 * h + 4 * kk;
+            ksr[h] = ks[(t + (quad < last ? quad : last)) >> a.shift];
+        }
+    };
+    auto request_v = [&](int t) __attribute__((always_inline)) {
+        const uint8_t *base = V + (size_t)t * D;
+        const int last = u.t_end - 1 - t;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int row = 16 * (e / 4) + e % 4 + 4 * kk;
+            const uint32_t off = last >= 31 ? v_off + (16 * (e / 4) + e % 4) * D : (row < last ? row : last) * D + 4 * VW * n16;
+            vr[e] = load_words<VW>(base + off);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int quad = 16 * h + 4 * kk;
+            vsr[h] = vs[(t + (quad < last ? quad : last)) >> a.shift];
+        }
+    };
+
+    constexpr int STEP = 128;  // of a workgroup
+    int t = u.t_begin + 32 * w;
+    if (t < u.t_end) {
+        request_k(t);
+        request_v(t);
+    }
+    for (; t < u.t_end; t += STEP) {
+        const bool next = t + STEP < u.t_end;
+        const bool mixed = t + 32 > least;  // rows see different tokens of this tile
+        f32x4_t S[RT][2];
+        u32x4_t kb[2][STEPS];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) kb[h][s] = codes8<CODE>(kr[h][s / 2].x[2 * (s % 2)], kr[h][s / 2].x[2 * (s % 2) + 1]);
+        float kc[2] = {ksr[0] * c, ksr[1] * c};
+        if (next) request_k(t + STEP);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) S[rt][0] = S[rt][1] = f32x4_t(0.0f);
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+                    S[rt][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kb[h][s]), Q[rt][s], S[rt][h], 0, 0, 0);
+        // element v of half h: token t + 16 h + 4 kk + v
+        bf16x8_t P[RT], R[RT];
+        uint32_t seen[RT];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            f32x8_t z;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) z[e] = S[rt][e / 4][e % 4] * kc[e / 4];
+            if (mixed) {
+                int left = sees[rt] < u.t_end ? sees[rt] - t : u.t_end - t;
+                seen[rt] = left >= 32 ? 0xFFFFFFFFu : left > 0 ? (1u << left) - 1u : 0u;
+                seen[rt] >>= 4 * kk;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) z[e] = seen[rt] >> (16 * (e / 4) + e % 4) & 1u ? z[e] : -INFINITY;
+            }
+            float top = fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7]))), lo, hi;
+            quarters(top, lo, hi);
+            halves(fmaxf(lo, hi), lo, hi);
+            top = fmaxf(lo, hi);
+            if (__ballot(!(top - m_run[rt] <= 8.0f))) {
+                const float m_new = fmaxf(m_run[rt], top), alpha = m_run[rt] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run[rt] - m_new);
+                l_run[rt] *= alpha;
+#pragma unroll
+                for (int j = 0; j < JC; ++j) O[rt][j] *= alpha;
+                m_run[rt] = m_new;
+            }
+            const float less = m_run[rt] == -INFINITY ? 0.0f : m_run[rt];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) z[e] = __builtin_amdgcn_exp2f(z[e] - less);
+            l_run[rt] = sum8(z, l_run[rt]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) z[e] *= vsr[e / 4];
+            if (mixed) {  // (a scale that is not seen may be NaN)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) z[e] = seen[rt] >> (16 * (e / 4) + e % 4) & 1u ? z[e] : 0.0f;
+            }
+            P[rt] = upper8(z);
+            R[rt] = lower8(z);
+        }
+        if (CODE == XKV_E4M3 && mixed) {
+            // Codes of V that are NaN reach the rows that see them, not the others: where there are any, the NaN of a channel that a row sees are
+            // counted, a product of ones, and the codes become zeros.
+            uint32_t odd = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+#pragma unroll
+                for (int i = 0; i < VW; ++i) odd |= ((vr[e].x[i] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+            if (__ballot(odd != 0)) {
+#pragma unroll
+                for (int i = 0; i < VW; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        u32x4_t ones;
+#pragma unroll
+                        for (int p = 0; p < 4; ++p)
+                            ones[p] = ((vr[2 * p].x[i] >> (8 * j) & 0x7Fu) == 0x7Fu ? 0x3F80u : 0u) |
+                                      ((vr[2 * p + 1].x[i] >> (8 * j) & 0x7Fu) == 0x7Fu ? 0x3F800000u : 0u);
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt) {
+                            u32x4_t sees_it;
+#pragma unroll
+                            for (int p = 0; p < 4; ++p) {
+                                const uint32_t two = seen[rt] >> (16 * (p / 2) + 2 * (p % 2));
+                                sees_it[p] = (two & 1u ? 0x3F80u : 0u) | (two & 2u ? 0x3F800000u : 0u);
+                            }
+                            const f32x4_t count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ones), __builtin_bit_cast(bf16x8_t, sees_it),
+                                                                                          f32x4_t(0.0f), 0, 0, 0);
+#pragma unroll
+                            for (int v = 0; v < 4; ++v) O[rt][4 * i + j][v] = count[v] > 0.0f ? __builtin_nanf("") : O[rt][4 * i + j][v];
+                        }
+                    }
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+#pragma unroll
+                    for (int i = 0; i < VW; ++i)
+                        vr[e].x[i] &= ~(((((vr[e].x[i] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) >> 7) * 255u);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < VW; ++i) {
+            u32x4_t vb[4];
+            const uint32_t word[8] = {vr[0].x[i], vr[1].x[i], vr[2].x[i], vr[3].x[i], vr[4].x[i], vr[5].x[i], vr[6].x[i], vr[7].x[i]};
+            codes_by_channel<CODE>(word, vb);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    f32x4_t &o = O[rt][4 * i + j];
+                    o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, vb[j]), R[rt], o, 0, 0, 0);
+                    o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, vb[j]), P[rt], o, 0, 0, 0);
+                }
+        }
+        if (next) request_v(t + STEP);
+    }
+
+    // merge the wavefronts through LDS, 16 rows at a time: 16-byte piece p of row n16 sits at (p + n16) % PITCH; channel JC (4 kk + v) + j is
+    // register v of O[j]
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        float lo, hi;
+        quarters(l_run[rt], lo, hi);
+        halves(lo + hi, lo, hi);
+        if (rt > 0) __syncthreads();
+        if (kk == 0) {
+            sm_m[w][n16] = m_run[rt];
+            sm_l[w][n16] = lo + hi;
+        }
+        __syncthreads();
+        const float top = fmaxf(fmaxf(sm_m[0][n16], sm_m[1][n16]), fmaxf(sm_m[2][n16], sm_m[3][n16]));
+        const float f = m_run[rt] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run[rt] - top);
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+#pragma unroll
+            for (int j = 0; j < JC; j += 4)
+                sm_o[w][PITCH * n16 + (((4 * kk + v) * JC + j) / 4 + n16) % PITCH] =
+                    f32x4_t{f * O[rt][j][v], f * O[rt][j + 1][v], f * O[rt][j + 2][v], f * O[rt][j + 3][v]};
+        __syncthreads();
+        for (int item = (int)threadIdx.x; item < 16 * PITCH; item += 256) {
+            const int row = item / PITCH, p = item % PITCH, m = (u.tile * RT + rt) * 16 + row;
+            if (m >= M) continue;
+            f32x4_t x = f32x4_t(0.0f);
+            float den = 0.0f, most = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                x += sm_o[i][PITCH * row + (p + row) % PITCH];
+                most = fmaxf(most, sm_m[i][row]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)  // (a wavefront without a maximum: 0, or NaN)
+                den += sm_l[i][row] * (sm_m[i][row] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(sm_m[i][row] - most));
+            if (direct) {
+                const bool none = visible8(a, u.seq, m / n_rep) == 0;
+                bf16_t *out = (bf16_t *)a.out + (((size_t)u.seq * a.N + m / n_rep) * a.H_q + u.g * n_rep + m % n_rep) * D + 4 * p;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) out[e] = result<bf16_t>(none ? 0.0f : x[e] / den);
+                continue;
+            }
+            const size_t slot = ((size_t)u.part * a.N + m / n_rep) * a.H_q + u.g * n_rep + m % n_rep;
+            *reinterpret_cast<f32x4_t *>(a.part_o + slot * D + 4 * p) = x;
+            if (p == 0) {
+                a.part_ml[2 * slot] = most;
+                a.part_ml[2 * slot + 1] = den;
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------
 // Merge: a wavefront per row (query, head).  Partials of parts that have no rows were not written and are not read.
 // ------------------------------------------------------------------------------------------
 template <typename T>
@@ -217,16 +540,20 @@ __global__ __launch_bounds__(256) void cache8_merge_kernel(Cache8Args a, int row
     }
 }
 
+dim3 unit_grid(const Cache8Args &a)
+{
+    const int M = a.N * (a.H_q / a.H_kv);
+    return dim3((unsigned)a.parts * a.H_kv * ((M + a.rows - 1) / a.rows) * (a.by_length ? 1u : (unsigned)a.batch));
+}
+
 template <typename T, int CODE>
 hipError_t launch_general(const Cache8Args &a, hipStream_t st)
 {
-    const int M = a.N * (a.H_q / a.H_kv);
-    const dim3 grid((unsigned)a.parts * a.H_kv * (a.by_length ? 1 : (unsigned)a.batch * ((M + a.rows - 1) / a.rows)));
     const size_t lds = (2 * (size_t)kGenTokens * general_pitch(a.d_h) + (size_t)kGenRows * ((a.d_h + 3) / 4 * 4) + 4 * 4 * kGenTokens) * sizeof(float);
     auto launch = [&](auto kernel, DynamicLdsOnce &attr) {
         const hipError_t e = attr.ensure((const void *)kernel, 160 * 1024);  // (at most 150 KiB, at 256 channels)
         if (e != hipSuccess) return e;
-        hipLaunchKernelGGL(kernel, grid, dim3(256), lds, st, a);
+        hipLaunchKernelGGL(kernel, unit_grid(a), dim3(256), lds, st, a);
         return hipGetLastError();
     };
     static DynamicLdsOnce attr[3];
@@ -234,17 +561,44 @@ hipError_t launch_general(const Cache8Args &a, hipStream_t st)
          : a.d_h <= 128 ? launch(cache8_general_kernel<T, CODE, 2>, attr[1]) : launch(cache8_general_kernel<T, CODE, 4>, attr[2]);
 }
 
+template <int CODE, int D>
+hipError_t launch_mfma(const Cache8Args &a, bool direct, hipStream_t st)
+{
+    auto launch = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, unit_grid(a), dim3(256), 0, st, a, direct);
+        return hipGetLastError();
+    };
+    if (a.rows == 16) return launch(cache8_mfma_kernel<CODE, D, 1>);
+    if constexpr (D < 256) {
+        if (a.rows == 64) return launch(cache8_mfma_kernel<CODE, D, 4>);
+    }
+    return launch(cache8_mfma_kernel<CODE, D, 2>);
+}
+template <int CODE>
+hipError_t launch_mfma(const Cache8Args &a, bool direct, hipStream_t st)
+{
+    return a.d_h == 64 ? launch_mfma<CODE, 64>(a, direct, st) : a.d_h == 128 ? launch_mfma<CODE, 128>(a, direct, st) : launch_mfma<CODE, 256>(a, direct, st);
+}
+
 }  // namespace
 
-hipError_t launch_cache8_attend(const xkv_shape &s, const Cache8Args &a, int code, bool mfma, hipStream_t st)
+hipError_t launch_cache8_attend(const xkv_shape &s, const Cache8Args &given, int code, bool mfma, hipStream_t st)
 {
-    (void)mfma;
+    Cache8Args a = given;
+    const bool matrix = mfma && a.shift >= 2 && ((uintptr_t)a.K8 | (uintptr_t)a.V8 | (uintptr_t)a.q) % 16 == 0;
+    // one part of every row tile, and a workgroup for it also where it has no rows
+    const bool direct = matrix && a.parts == 1 && (!a.by_length || a.batch == 1);
     hipError_t e;
-    if (s.dtype == XKV_F32)
-        e = code == XKV_E4M3 ? launch_general<float, XKV_E4M3>(a, st) : launch_general<float, XKV_INT8>(a, st);
-    else
-        e = code == XKV_E4M3 ? launch_general<bf16_t, XKV_E4M3>(a, st) : launch_general<bf16_t, XKV_INT8>(a, st);
-    if (e != hipSuccess) return e;
+    if (matrix) {
+        e = code == XKV_E4M3 ? launch_mfma<XKV_E4M3>(a, direct, st) : launch_mfma<XKV_INT8>(a, direct, st);
+    } else {
+        a.rows = kGenRows;  // (its rounds divide those of the plan)
+        if (s.dtype == XKV_F32)
+            e = code == XKV_E4M3 ? launch_general<float, XKV_E4M3>(a, st) : launch_general<float, XKV_INT8>(a, st);
+        else
+            e = code == XKV_E4M3 ? launch_general<bf16_t, XKV_E4M3>(a, st) : launch_general<bf16_t, XKV_INT8>(a, st);
+    }
+    if (e != hipSuccess || direct) return e;
     const int rows = a.batch * a.N * a.H_q;
     if (s.dtype == XKV_F32)
         hipLaunchKernelGGL(cache8_merge_kernel<float>, dim3((rows + 3) / 4), dim3(256), 0, st, a, rows);
