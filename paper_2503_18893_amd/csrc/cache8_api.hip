@@ -61,18 +61,27 @@ xkv_status plan_cache8(const xkv_shape &s, int N, Cache8Plan &p)
     p.scale = s.scale > 0.0f ? s.scale : 1.0f / std::sqrt((float)s.d_h);
     const long long M = (long long)N * p.n_rep;
     p.mfma = s.dtype == XKV_BF16 && (s.d_h == 64 || s.d_h == 128 || s.d_h == 256);
-    p.rows = !p.mfma || M <= 16 ? 16 : M <= 32 || s.d_h == 256 ? 32 : 64;
+    // Rows of a workgroup.  Two workgroups of the matrix-core kernels to a compute unit, one of 256 rows or channels; four of the general one.
+    // (65 rows and more of 128 channels: 256 that share tiles, or 128 where that leaves fewer of them empty: 256 queries of 7 heads after 131072
+    // rows, 1792 rows a KV head, 631 us by 256, 667 by 128, 783 by 32 that do not share.)
+    p.rows = !p.mfma || M <= 16 || s.d_h == 256 ? 16 : M <= 64 || s.d_h != 128 ? 32 : (ceil_div(M, 128) & 1) ? 128 : 256;
     p.round = p.mfma ? 128 : 64;
-    const int want = !p.mfma ? 1024 : p.rows == 16 ? 512 : 256;
+    const int slots = !p.mfma ? 1024 : p.rows == 256 || s.d_h == 256 ? 256 : 512;
     const int row_tiles = ceil_div(M, p.rows), longest = ceil_div(s.L, p.round);
-    p.by_length = row_tiles == 1;
-    const long long units = (long long)s.H_kv * row_tiles;
+    p.by_length = M <= 64;
     if (p.by_length) {
         const long long all = batch * longest;
-        p.parts = clampi(ceil_div(want, units), (int)batch, (int)(all < (1 << 30) ? all : 1 << 30));
+        p.parts = clampi(ceil_div(slots, s.H_kv * row_tiles), (int)batch, (int)(all < (1 << 30) ? all : 1 << 30));
         if (p.parts > batch + kMaxCacheParts - 1) p.parts = (int)batch + kMaxCacheParts - 1;
     } else {
-        p.parts = clampi(ceil_div(want, units * batch), 1, clampi(longest, 1, kMaxCacheParts));
+        // Parts of a row tile: as few as fill the compute units well.  A part costs about what 4 rounds take beside its own.
+        const long long units = (long long)s.H_kv * row_tiles * batch;
+        long long best = 0;
+        p.parts = 1;
+        for (int parts = 1; parts <= 64 && parts <= longest; ++parts) {
+            const long long time = ((units * parts + slots - 1) / slots) * (ceil_div(longest, parts) + 4);
+            if (parts == 1 || time < best) best = time, p.parts = parts;
+        }
     }
     const size_t part_rows = (size_t)p.parts * (p.by_length ? 1 : batch) * N * s.H_q;
     size_t off = align_up(((size_t)batch + 1) * sizeof(int32_t), 256);

@@ -2,6 +2,8 @@
 //   z_t = scale ks[t / c] <q, k8_t>,  out = sum_t exp(z_t - max) vs[t / c] v8_t / sum_t exp(z_t - max)
 // over the rows that a query sees, split over the rows: every workgroup leaves (maximum, sum, unnormalised output) of its part, in
 // powers of two, and a second kernel merges them.
+#include <type_traits>
+
 #include "cache8.h"
 #include "cache_tile.h"
 
@@ -187,15 +189,20 @@ __global__ __launch_bounds__(256) void cache8_general_kernel(Cache8Args a)
 // ------------------------------------------------------------------------------------------
 // Matrix-core path: bf16, D channels, blocks of at least 4 rows.  A wavefront takes tiles of 32 rows of the cache on its own and 16 RT rows (query,
 // head):
-//   S^T [32 tokens x rows] = codes of K x Q^T,  P^T = exp2(c ks S^T - m),  O^T [channels x rows] += codes of V^T x (vs P^T)
-// Codes are bf16 numbers as they are (3 or 7 bits of mantissa), so both products take them exactly, and the scales, one for four tokens of a
-// lane, multiply logits and weights.  A lane holds one row of S^T, P^T and O^T (rows n16), so that the statistics are its own, and P^T is the second
-// product's operand as it comes.  Weights times scales enter as two bf16 terms, 2^-15.  Keys and values go from memory to registers: a lane's
-// pieces of K are its operands but for the conversion; of V it reads the tokens that it has weights of, D / 16 channels of each (a row of the
-// cache is read by 16 lanes), and pairs up neighbouring tokens by permuting bytes.  The next tile is requested as soon as this one's bytes
-// are converted.  The maximum is only raised when a logit outgrows it by 2^8.
+//   S^T [32 tokens x rows] = codes of K x Q^T (bf16),  P^T = exp2(c ks S^T - m),  O^T [channels x rows] += codes of V^T x (vs P^T) (fp16)
+// Codes are bf16 and fp16 numbers as they are (3 or 7 bits of mantissa), so both products take them exactly, and the scales, one for four tokens of
+// a lane, multiply logits and weights.  A lane holds one row of S^T, P^T and O^T (rows n16), so that the statistics are its own, and P^T is the
+// second product's operand as it comes.  Keys and values go from memory to registers: a lane's pieces of K are its operands but for the
+// conversion; of V it reads the tokens that it has weights of, D / 16 channels of each (a row of the cache is read by 16 lanes), and pairs
+// up neighbouring tokens by permuting bytes.
+// The maximum is only raised when a logit outgrows it by 2^8.  Weights times scales enter as fp16, 2^-12: `inv`, a power of two, brings the largest scale met
+// so far to between 2^6 and 2^7, so that they are at most 2^15, and down to 2^-20 of that scale keep their 11 bits (what is smaller is held to 2^-32 of it).
+// Beside the output's own rounding, 2^-9 root mean square of its value, that is not seen: 0.0017 of the root mean square against 64 bits with and without.
 // ------------------------------------------------------------------------------------------
-template <int CODE> __device__ __forceinline__ u32x4_t codes8(uint32_t lo, uint32_t hi)
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8_t;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2_t;
+
+template <int CODE> __device__ __forceinline__ bf16x8_t codes8(uint32_t lo, uint32_t hi)
 {
     u32x4_t x;
     if constexpr (CODE == XKV_E4M3) {
@@ -210,88 +217,98 @@ template <int CODE> __device__ __forceinline__ u32x4_t codes8(uint32_t lo, uint3
             x[i] = __builtin_amdgcn_perm(__float_as_uint((float)(int8_t)(w >> 8)), __float_as_uint((float)(int8_t)w), 0x07060302u);  // (exact)
         }
     }
-    return x;
+    return __builtin_bit_cast(bf16x8_t, x);
+}
+
+// Eight codes as fp16 numbers.
+template <int CODE> __device__ __forceinline__ f16x8_t values8(uint32_t lo, uint32_t hi)
+{
+    u32x4_t x;
+    if constexpr (CODE == XKV_E4M3) {
+        x[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false));
+        x[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true));
+        x[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false));
+        x[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t w = (i < 2 ? lo : hi) ^ 0x80808080u;
+            const uint32_t two = __builtin_amdgcn_perm(w, w, i % 2 ? 0x0C030C02u : 0x0C010C00u) | 0x64006400u;
+            x[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2_t, two) - (_Float16)1152.0f);
+        }
+    }
+    return __builtin_bit_cast(f16x8_t, x);
 }
 
 // Four channels of eight tokens, w[e] those of token e, as operands: x[j] channel j of the tokens.
-template <int CODE> __device__ __forceinline__ void codes_by_channel(const uint32_t (&w)[8], u32x4_t (&x)[4])
+template <int CODE> __device__ __forceinline__ void codes_by_channel(const uint32_t (&w)[8], f16x8_t (&x)[4])
 {
+    u32x4_t y[4];
     if constexpr (CODE == XKV_E4M3) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const uint32_t a = __builtin_bit_cast(uint32_t, h ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * i], 1.0f, true)
-                                                                  : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * i], 1.0f, false));
-                const uint32_t b = __builtin_bit_cast(uint32_t, h ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * i + 1], 1.0f, true)
-                                                                  : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * i + 1], 1.0f, false));
-                x[2 * h][i] = __builtin_amdgcn_perm(b, a, 0x05040100u);
-                x[2 * h + 1][i] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+                const uint32_t a = __builtin_bit_cast(uint32_t, h ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[2 * i], 1.0f, true)
+                                                                  : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[2 * i], 1.0f, false));
+                const uint32_t b = __builtin_bit_cast(uint32_t, h ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[2 * i + 1], 1.0f, true)
+                                                                  : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[2 * i + 1], 1.0f, false));
+                y[2 * h][i] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+                y[2 * h + 1][i] = __builtin_amdgcn_perm(b, a, 0x07060302u);
             }
     } else {
+        // 1024 + 128 + a code is an fp16 number with the code, its sign bit turned, in its lower bits
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t a = w[2 * i] ^ 0x80808080u, b = w[2 * i + 1] ^ 0x80808080u;
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                x[j][i] = __builtin_amdgcn_perm(__float_as_uint((float)(int8_t)(w[2 * i + 1] >> (8 * j))),
-                                                __float_as_uint((float)(int8_t)(w[2 * i] >> (8 * j))), 0x07060302u);
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t two = __builtin_amdgcn_perm(b, a, 0x0C040C00u + 0x00010001u * j) | 0x64006400u;
+                y[j][i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2_t, two) - (_Float16)1152.0f);
+            }
+        }
     }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = __builtin_bit_cast(f16x8_t, y[j]);
 }
 
+// Words of a row of the cache; ONCE: past the caches, where nobody else reads them.
 template <int N> struct Words {
     uint32_t x[N];
 };
-template <int N> __device__ __forceinline__ Words<N> load_words(const uint8_t *from)
+template <int N, bool ONCE> __device__ __forceinline__ Words<N> load_words(const uint8_t *from)
 {
     typedef __attribute__((ext_vector_type(N))) uint32_t vec_t;
     Words<N> r;
     if constexpr (N == 1) {
-        r.x[0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(from));
+        r.x[0] = ONCE ? __builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(from)) : *reinterpret_cast<const uint32_t *>(from);
     } else {
-        const vec_t v = __builtin_nontemporal_load(reinterpret_cast<const vec_t *>(from));
+        const vec_t v = ONCE ? __builtin_nontemporal_load(reinterpret_cast<const vec_t *>(from)) : *reinterpret_cast<const vec_t *>(from);
 #pragma unroll
         for (int i = 0; i < N; ++i) r.x[i] = v[i];
     }
     return r;
 }
 
-template <int CODE, int D, int RT>
-__global__ __launch_bounds__(256, RT == 1 && D < 256 ? 2 : 1) void cache8_mfma_kernel(Cache8Args a, bool direct)
+__device__ __forceinline__ float largest4(const f32x4_t &x) { return fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])); }
+
+constexpr float kFarUp = 0x1p126f;  // `inv` before any scale was met
+constexpr float kLeast = 0x1p-60f;  // scales by `inv` that are less count as this: their weights are zeros in fp16
+
+template <int CODE, int D, int RT, bool ONCE>
+__global__ __launch_bounds__(256, D < 256 ? 2 : 1) void cache8_mfma_kernel(Cache8Args a, bool direct)
 {
     constexpr int KP = D / 64, VW = D / 64, JC = D / 16, STEPS = D / 32, PITCH = D / 4;  // pieces of K, words of V, channels of a lane; products; 16-byte pieces of a row
+    constexpr bool Q_LDS = RT > 1;
     __shared__ f32x4_t sm_o[4][16 * PITCH];
     __shared__ float sm_m[4][16], sm_l[4][16];
+    __shared__ u32x4_t sm_q[Q_LDS ? RT * STEPS * 64 : 1];
     const Unit8 u = unit8(a);
     const int lane = lane_id(), w = wave_id(), n16 = lane & 15, kk = lane >> 4, n_rep = a.H_q / a.H_kv, M = a.N * n_rep;
     if (!u.some && !direct) return;  // (the merge knows)
     const size_t head = (size_t)u.seq * a.H_kv + u.g;
     const uint8_t *K = a.K8 + head * a.L * D, *V = a.V8 + head * a.L * D;
     const float *ks = a.k_scales + head * a.n_c, *vs = a.v_scales + head * a.n_c, c = a.scale * kLog2e;
-
-    // Q^T operands: lane (row n16, kk), product s, position e: channel 64 (s / 2) + 16 kk + 8 (s % 2) + e, as the pieces of K have them
-    bf16x8_t Q[RT][STEPS];
-    int sees[RT], least = 0x7FFFFFFF;
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        const int m = (u.tile * RT + rt) * 16 + n16, m_in = m < M ? m : M - 1, i = m_in / n_rep;
-        const bf16_t *q = (const bf16_t *)a.q + (((size_t)u.seq * a.N + i) * a.H_q + u.g * n_rep + m_in % n_rep) * D;
-        sees[rt] = visible8(a, u.seq, i);
-        least = sees[rt] < least ? sees[rt] : least;
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) Q[rt][s] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t *>(q + 64 * (s / 2) + 16 * kk + 8 * (s % 2)));
-    }
-    least = -wave_all(-least, MaxOp());  // rows that all of them see
-    least = __builtin_amdgcn_readfirstlane(least < u.t_end ? least : u.t_end);
-
-    f32x4_t O[RT][JC];
-    float m_run[RT], l_run[RT];
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        m_run[rt] = -INFINITY;
-        l_run[rt] = 0.0f;
-#pragma unroll
-        for (int j = 0; j < JC; ++j) O[rt][j] = f32x4_t(0.0f);
-    }
 
     Words<4> kr[2][KP];
     Words<VW> vr[8];
@@ -305,7 +322,7 @@ __global__ __launch_bounds__(256, RT == 1 && D < 256 ? 2 : 1) void cache8_mfma_k
             const int row = 16 * h + n16;
             const uint32_t off = last >= 31 ? k_off + 16 * h * D : (row < last ? row : last) * D + 16 * kk;
 #pragma unroll
-            for (int f = 0; f < KP; ++f) kr[h][f] = load_words<4>(base + off + 64 * f);
+            for (int f = 0; f < KP; ++f) kr[h][f] = load_words<4, ONCE>(base + off + 64 * f);
             const int quad = 16 * h + 4 * kk;
             ksr[h] = ks[(t + (quad < last ? quad : last)) >> a.shift];
         }
@@ -317,7 +334,7 @@ __global__ __launch_bounds__(256, RT == 1 && D < 256 ? 2 : 1) void cache8_mfma_k
         for (int e = 0; e < 8; ++e) {
             const int row = 16 * (e / 4) + e % 4 + 4 * kk;
             const uint32_t off = last >= 31 ? v_off + (16 * (e / 4) + e % 4) * D : (row < last ? row : last) * D + 4 * VW * n16;
-            vr[e] = load_words<VW>(base + off);
+            vr[e] = load_words<VW, ONCE>(base + off);
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -325,73 +342,137 @@ __global__ __launch_bounds__(256, RT == 1 && D < 256 ? 2 : 1) void cache8_mfma_k
             vsr[h] = vs[(t + (quad < last ? quad : last)) >> a.shift];
         }
     };
-
     constexpr int STEP = 128;  // of a workgroup
     int t = u.t_begin + 32 * w;
     if (t < u.t_end) {
         request_k(t);
         request_v(t);
     }
-    for (; t < u.t_end; t += STEP) {
+
+    // Q^T operands: lane (row n16, kk), product s, position e: channel 64 (s / 2) + 16 kk + 8 (s % 2) + e, as the pieces of K have them
+    u32x4_t Q[STEPS];
+    int sees[RT], least = 0x7FFFFFFF;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int m = (u.tile * RT + rt) * 16 + n16, m_in = m < M ? m : M - 1, i = m_in / n_rep;
+        const bf16_t *q = (const bf16_t *)a.q + (((size_t)u.seq * a.N + i) * a.H_q + u.g * n_rep + m_in % n_rep) * D;
+        sees[rt] = visible8(a, u.seq, i);
+        least = sees[rt] < least ? sees[rt] : least;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            if (Q_LDS && (rt * STEPS + s) % 4 != w) continue;
+            const u32x4_t x = *reinterpret_cast<const u32x4_t *>(q + 64 * (s / 2) + 16 * kk + 8 * (s % 2));
+            if (Q_LDS)
+                sm_q[(rt * STEPS + s) * 64 + lane] = x;
+            else
+                Q[s] = x;
+        }
+    }
+    least = -wave_all(-least, MaxOp());  // rows that all of them see
+    least = __builtin_amdgcn_readfirstlane(least < u.t_end ? least : u.t_end);
+    if (Q_LDS) __syncthreads();
+
+    f32x4_t O[RT][JC];
+    float m_run[RT], l_run[RT], inv = kFarUp;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        m_run[rt] = -INFINITY;
+        l_run[rt] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < JC; ++j) O[rt][j] = f32x4_t(0.0f);
+    }
+
+    // A tile; MIXED: rows see different tokens of it.
+    auto tile = [&](int t, auto mixed) __attribute__((always_inline)) {
+        constexpr bool MIXED = decltype(mixed)::value;
         const bool next = t + STEP < u.t_end;
-        const bool mixed = t + 32 > least;  // rows see different tokens of this tile
         f32x4_t S[RT][2];
-        u32x4_t kb[2][STEPS];
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int s = 0; s < STEPS; ++s) kb[h][s] = codes8<CODE>(kr[h][s / 2].x[2 * (s % 2)], kr[h][s / 2].x[2 * (s % 2) + 1]);
-        float kc[2] = {ksr[0] * c, ksr[1] * c};
-        if (next) request_k(t + STEP);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) S[rt][0] = S[rt][1] = f32x4_t(0.0f);
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s)
+        for (int s = 0; s < STEPS; ++s) {
+            bf16x8_t kb[2];
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < 2; ++h) kb[h] = codes8<CODE>(kr[h][s / 2].x[2 * (s % 2)], kr[h][s / 2].x[2 * (s % 2) + 1]);
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
-                    S[rt][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kb[h][s]), Q[rt][s], S[rt][h], 0, 0, 0);
+            for (int rt = 0; rt < RT; ++rt) {
+                const bf16x8_t qf = __builtin_bit_cast(bf16x8_t, Q_LDS ? sm_q[(rt * STEPS + s) * 64 + lane] : Q[s]);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) S[rt][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb[h], qf, S[rt][h], 0, 0, 0);
+            }
+        }
+        const float kc[2] = {ksr[0] * c, ksr[1] * c};
+        if (next) request_k(t + STEP);
         // element v of half h: token t + 16 h + 4 kk + v
-        bf16x8_t P[RT], R[RT];
         uint32_t seen[RT];
+        float top[RT];
+        bool raise = !(fmaxf(vsr[0], vsr[1]) * inv <= 128.0f);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-            f32x8_t z;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) z[e] = S[rt][e / 4][e % 4] * kc[e / 4];
-            if (mixed) {
-                int left = sees[rt] < u.t_end ? sees[rt] - t : u.t_end - t;
+            if (MIXED) {
+                const int left = sees[rt] < u.t_end ? sees[rt] - t : u.t_end - t;
                 seen[rt] = left >= 32 ? 0xFFFFFFFFu : left > 0 ? (1u << left) - 1u : 0u;
                 seen[rt] >>= 4 * kk;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) z[e] = seen[rt] >> (16 * (e / 4) + e % 4) & 1u ? z[e] : -INFINITY;
+                for (int e = 0; e < 8; ++e)
+                    S[rt][e / 4][e % 4] = seen[rt] >> (16 * (e / 4) + e % 4) & 1u ? S[rt][e / 4][e % 4] * kc[e / 4] : -INFINITY;
             }
-            float top = fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7]))), lo, hi;
-            quarters(top, lo, hi);
+            float lo, hi, most[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                most[h] = largest4(S[rt][h]);
+                if (!MIXED) most[h] *= kc[h];  // (scales are not negative)
+            }
+            quarters(fmaxf(most[0], most[1]), lo, hi);
             halves(fmaxf(lo, hi), lo, hi);
-            top = fmaxf(lo, hi);
-            if (__ballot(!(top - m_run[rt] <= 8.0f))) {
-                const float m_new = fmaxf(m_run[rt], top), alpha = m_run[rt] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run[rt] - m_new);
+            top[rt] = fmaxf(lo, hi);
+            raise |= !(top[rt] - m_run[rt] <= 8.0f);
+        }
+        if (__ballot(raise)) {
+            const float largest = wave_all(fmaxf(vsr[0], vsr[1]), MaxOp());  // (NaN is passed over)
+            float less = 1.0f;
+            if (largest * inv > 128.0f && largest < INFINITY) {
+                const float now = __uint_as_float((254u + 6u - (__float_as_uint(largest) >> 23 & 0xFFu)) << 23);  // 2^6 by its power of two
+                less = now * __uint_as_float((254u << 23) - __float_as_uint(inv));                                 // (inv is a power of two)
+                inv = now;
+            }
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                const float m_new = fmaxf(m_run[rt], top[rt]), alpha = m_run[rt] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run[rt] - m_new);
                 l_run[rt] *= alpha;
 #pragma unroll
-                for (int j = 0; j < JC; ++j) O[rt][j] *= alpha;
+                for (int j = 0; j < JC; ++j) O[rt][j] *= alpha * less;
                 m_run[rt] = m_new;
             }
-            const float less = m_run[rt] == -INFINITY ? 0.0f : m_run[rt];
+        }
+        // vs P = exp2(z - m + log2 vs), whose sum by 1 / vs is that of the weights
+        float lv[2], rv[2];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) z[e] = __builtin_amdgcn_exp2f(z[e] - less);
-            l_run[rt] = sum8(z, l_run[rt]);
+        for (int h = 0; h < 2; ++h) {
+            const float v = vsr[h] * inv < kLeast ? kLeast : vsr[h] * inv;  // (NaN stays)
+            lv[h] = __builtin_amdgcn_logf(v);
+            rv[h] = __builtin_amdgcn_rcpf(v);
+        }
+        f16x8_t P[RT];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) z[e] *= vsr[e / 4];
-            if (mixed) {  // (a scale that is not seen may be NaN)
+        for (int rt = 0; rt < RT; ++rt) {
+            const float less = m_run[rt] == -INFINITY ? 0.0f : m_run[rt], add[2] = {lv[0] - less, lv[1] - less};
+            f32x8_t z;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                z[e] = __builtin_amdgcn_exp2f(MIXED ? S[rt][e / 4][e % 4] + add[e / 4] : fmaf(S[rt][e / 4][e % 4], kc[e / 4], add[e / 4]));
+            if (MIXED) {  // (a scale that is not seen may be NaN)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) z[e] = seen[rt] >> (16 * (e / 4) + e % 4) & 1u ? z[e] : 0.0f;
             }
-            P[rt] = upper8(z);
-            R[rt] = lower8(z);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float by = MIXED && !(seen[rt] >> (16 * h) & 0xFu) ? 0.0f : rv[h];
+                l_run[rt] = fmaf((z[4 * h] + z[4 * h + 1]) + (z[4 * h + 2] + z[4 * h + 3]), by, l_run[rt]);
+            }
+            P[rt] = __builtin_convertvector(z, f16x8_t);
         }
-        if (CODE == XKV_E4M3 && mixed) {
+        if (CODE == XKV_E4M3 && MIXED) {
             // Codes of V that are NaN reach the rows that see them, not the others: where there are any, the NaN of a channel that a row sees are
             // counted, a product of ones, and the codes become zeros.
             uint32_t odd = 0;
@@ -407,18 +488,18 @@ __global__ __launch_bounds__(256, RT == 1 && D < 256 ? 2 : 1) void cache8_mfma_k
                         u32x4_t ones;
 #pragma unroll
                         for (int p = 0; p < 4; ++p)
-                            ones[p] = ((vr[2 * p].x[i] >> (8 * j) & 0x7Fu) == 0x7Fu ? 0x3F80u : 0u) |
-                                      ((vr[2 * p + 1].x[i] >> (8 * j) & 0x7Fu) == 0x7Fu ? 0x3F800000u : 0u);
+                            ones[p] = ((vr[2 * p].x[i] >> (8 * j) & 0x7Fu) == 0x7Fu ? 0x3C00u : 0u) |
+                                      ((vr[2 * p + 1].x[i] >> (8 * j) & 0x7Fu) == 0x7Fu ? 0x3C000000u : 0u);
 #pragma unroll
                         for (int rt = 0; rt < RT; ++rt) {
                             u32x4_t sees_it;
 #pragma unroll
                             for (int p = 0; p < 4; ++p) {
                                 const uint32_t two = seen[rt] >> (16 * (p / 2) + 2 * (p % 2));
-                                sees_it[p] = (two & 1u ? 0x3F80u : 0u) | (two & 2u ? 0x3F800000u : 0u);
+                                sees_it[p] = (two & 1u ? 0x3C00u : 0u) | (two & 2u ? 0x3C000000u : 0u);
                             }
-                            const f32x4_t count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ones), __builtin_bit_cast(bf16x8_t, sees_it),
-                                                                                          f32x4_t(0.0f), 0, 0, 0);
+                            const f32x4_t count = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, ones), __builtin_bit_cast(f16x8_t, sees_it),
+                                                                                         f32x4_t(0.0f), 0, 0, 0);
 #pragma unroll
                             for (int v = 0; v < 4; ++v) O[rt][4 * i + j][v] = count[v] > 0.0f ? __builtin_nanf("") : O[rt][4 * i + j][v];
                         }
@@ -432,7 +513,7 @@ __global__ __launch_bounds__(256, RT == 1 && D < 256 ? 2 : 1) void cache8_mfma_k
         }
 #pragma unroll
         for (int i = 0; i < VW; ++i) {
-            u32x4_t vb[4];
+            f16x8_t vb[4];
             const uint32_t word[8] = {vr[0].x[i], vr[1].x[i], vr[2].x[i], vr[3].x[i], vr[4].x[i], vr[5].x[i], vr[6].x[i], vr[7].x[i]};
             codes_by_channel<CODE>(word, vb);
 #pragma unroll
@@ -440,15 +521,21 @@ __global__ __launch_bounds__(256, RT == 1 && D < 256 ? 2 : 1) void cache8_mfma_k
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) {
                     f32x4_t &o = O[rt][4 * i + j];
-                    o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, vb[j]), R[rt], o, 0, 0, 0);
-                    o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, vb[j]), P[rt], o, 0, 0, 0);
+                    o = __builtin_amdgcn_mfma_f32_16x16x32_f16(vb[j], P[rt], o, 0, 0, 0);
                 }
         }
         if (next) request_v(t + STEP);
+    };
+    for (; t < u.t_end; t += STEP) {
+        if (t + 32 <= least)
+            tile(t, std::false_type{});
+        else
+            tile(t, std::true_type{});
     }
 
     // merge the wavefronts through LDS, 16 rows at a time: 16-byte piece p of row n16 sits at (p + n16) % PITCH; channel JC (4 kk + v) + j is
     // register v of O[j]
+    const float undo = __uint_as_float((254u << 23) - __float_as_uint(inv));
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         float lo, hi;
@@ -461,7 +548,7 @@ __global__ __launch_bounds__(256, RT == 1 && D < 256 ? 2 : 1) void cache8_mfma_k
         }
         __syncthreads();
         const float top = fmaxf(fmaxf(sm_m[0][n16], sm_m[1][n16]), fmaxf(sm_m[2][n16], sm_m[3][n16]));
-        const float f = m_run[rt] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run[rt] - top);
+        const float f = m_run[rt] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run[rt] - top) * undo;
 #pragma unroll
         for (int v = 0; v < 4; ++v)
 #pragma unroll
@@ -495,6 +582,298 @@ __global__ __launch_bounds__(256, RT == 1 && D < 256 ? 2 : 1) void cache8_mfma_k
                 a.part_ml[2 * slot] = most;
                 a.part_ml[2 * slot + 1] = den;
             }
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------
+// The same for many rows, 128 channels: 32 rows a wavefront, WAVES of them to a workgroup, which share tiles of 64 rows of the cache.  Codes are
+// converted once for all of them, on their way from memory to LDS, K to bf16 and V to fp16, two tiles in turn: while one is multiplied, the next one's codes are
+// converted and those after it requested.  V^T is read by the transposing LDS read.
+// LDS: 16-byte piece p of row t of K sits at p ^ (t % 16), 32-byte piece u of V at (u + t) % 8, so that neither the fragment reads (16
+// rows at a time, one piece each) nor the transposing reads (4 rows at a time, two pieces each) meet in a bank.
+// ------------------------------------------------------------------------------------------
+template <int CODE, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void cache8_rows_kernel(Cache8Args a, bool direct)
+{
+    constexpr int D = 128, RT = 2, TILE = 64, KV = TILE * 2 * D, PIECES = 8 / WAVES;  // bytes of a tile of K or V; pieces of 16 codes of a thread
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * KV];
+    __shared__ uint32_t sm_odd[3][2];  // of this tile, the next one and the one after it
+    const Unit8 u = unit8(a);
+    const int lane = lane_id(), w = wave_id(), n16 = lane & 15, kk = lane >> 4, n_rep = a.H_q / a.H_kv, M = a.N * n_rep;
+    if (!u.some && !direct) return;  // (the merge knows)
+    const size_t head = (size_t)u.seq * a.H_kv + u.g;
+    const uint8_t *K = a.K8 + head * a.L * D, *V = a.V8 + head * a.L * D;
+    const float *ks = a.k_scales + head * a.n_c, *vs = a.v_scales + head * a.n_c, c = a.scale * kLog2e;
+
+    u32x4_t kr[PIECES], vr[PIECES];
+    auto request = [&](int t) __attribute__((always_inline)) {
+        const uint8_t *kb = K + (size_t)t * D, *vb = V + (size_t)t * D;
+        const int last = u.t_end - 1 - t;
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int p = (int)threadIdx.x + 64 * WAVES * i;
+            uint32_t off = 16 * p;
+            if (last < TILE - 1) off = (p / 8 < last ? p / 8 : last) * D + 16 * (p % 8);  // (behind the last one: that one again)
+            kr[i] = *reinterpret_cast<const u32x4_t *>(kb + off);
+            vr[i] = *reinterpret_cast<const u32x4_t *>(vb + off);
+        }
+    };
+    if (u.some) request(u.t_begin);
+
+    // Q^T operands: lane (row n16, kk), product s, position e: channel 32 s + 8 kk + e
+    bf16x8_t Q[RT][4];
+    int sees[RT], least = 0x7FFFFFFF, most = 0;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int m = ((u.tile * WAVES + w) * RT + rt) * 16 + n16, m_in = m < M ? m : M - 1, i = m_in / n_rep;
+        const bf16_t *q = (const bf16_t *)a.q + (((size_t)u.seq * a.N + i) * a.H_q + u.g * n_rep + m_in % n_rep) * D;
+        sees[rt] = visible8(a, u.seq, i);
+        least = sees[rt] < least ? sees[rt] : least;
+        most = sees[rt] > most ? sees[rt] : most;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) Q[rt][s] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t *>(q + 32 * s + 8 * kk));
+    }
+    least = -wave_all(-least, MaxOp());  // rows of the cache that all of this wavefront's rows see, ..
+    least = __builtin_amdgcn_readfirstlane(least < u.t_end ? least : u.t_end);
+    most = __builtin_amdgcn_readfirstlane(wave_all(most, MaxOp()));  // .. any of them, ..
+    int all = 0x7FFFFFFF;                                            // .. all rows of the workgroup
+    {
+        int first, last;
+        tile_queries(a, u.tile, first, last);
+        for (int i = first + lane; i <= last; i += kWave) {
+            const int n = visible8(a, u.seq, i);
+            all = n < all ? n : all;
+        }
+        all = -wave_all(-all, MaxOp());
+        all = __builtin_amdgcn_readfirstlane(all < u.t_end ? all : u.t_end);
+    }
+    if (threadIdx.x < 6) sm_odd[threadIdx.x / 2][threadIdx.x % 2] = 0u;
+    __syncthreads();
+
+    // Converted codes of a tile into LDS.  NaN among the values of a tile that rows see different tokens of become zeros, and their tokens are noted.
+    auto store = [&](int t, int buf, int note) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int p = (int)threadIdx.x + 64 * WAVES * i, row = p / 8, x = p % 8;
+            unsigned char *kt = smem + 2 * KV * buf + 256 * row, *vt = kt + KV + 32 * ((x + row) & 7);
+            *reinterpret_cast<bf16x8_t *>(kt + 16 * ((2 * x) ^ (row & 15))) = codes8<CODE>(kr[i][0], kr[i][1]);
+            *reinterpret_cast<bf16x8_t *>(kt + 16 * ((2 * x + 1) ^ (row & 15))) = codes8<CODE>(kr[i][2], kr[i][3]);
+            if (CODE == XKV_E4M3 && t + TILE > all) {
+                uint32_t odd = 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t nan = (((vr[i][e] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) >> 7;
+                    odd |= nan;
+                    vr[i][e] &= ~(nan * 255u);
+                }
+                if (odd) atomicOr(&sm_odd[note][row >> 5], 1u << (row & 31));
+            }
+            *reinterpret_cast<f16x8_t *>(vt) = values8<CODE>(vr[i][0], vr[i][1]);
+            *reinterpret_cast<f16x8_t *>(vt + 16) = values8<CODE>(vr[i][2], vr[i][3]);
+        }
+    };
+
+    uint32_t kat[4], vat[8];
+#pragma unroll
+    for (int f = 0; f < 4; ++f) kat[f] = 256 * n16 + 16 * ((4 * f + kk) ^ n16);
+    {
+        const int rl = 4 * kk + (n16 >> 2);
+#pragma unroll
+        for (int db = 0; db < 8; ++db) vat[db] = KV + 256 * rl + 32 * ((db + rl) & 7) + 8 * (lane & 3);
+    }
+    f32x4_t O[RT][8];
+    float m_run[RT], l_run[RT], inv = kFarUp;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        m_run[rt] = -INFINITY;
+        l_run[rt] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) O[rt][j] = f32x4_t(0.0f);
+    }
+    float ksr[4], vsr[4];  // of tokens 16 h + 4 kk .. + 3
+    auto request_scales = [&](int t) __attribute__((always_inline)) {
+        const int last = u.t_end - 1 - t;
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            if (a.shift >= 4) {  // one for 16 tokens: the same in all lanes
+                const int at = (t + (16 * h < last ? 16 * h : last)) >> a.shift;
+                ksr[h] = ks[at];
+                vsr[h] = vs[at];
+            } else {
+                const int quad = 16 * h + 4 * kk, at = (t + (quad < last ? quad : last)) >> a.shift;
+                ksr[h] = ks[at];
+                vsr[h] = vs[at];
+            }
+        }
+    };
+
+    auto tile = [&](int t, const unsigned char *lds, int note, auto mixed) __attribute__((always_inline)) {
+        constexpr bool MIXED = decltype(mixed)::value;
+        f32x4_t S[RT][4];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int h = 0; h < 4; ++h) S[rt][h] = f32x4_t(0.0f);
+#pragma unroll
+        for (int f = 0; f < 4; ++f)
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                const bf16x8_t kf = *reinterpret_cast<const bf16x8_t *>(lds + kat[f] + 4096 * h);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) S[rt][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, Q[rt][f], S[rt][h], 0, 0, 0);
+            }
+        float kc[4];
+#pragma unroll
+        for (int h = 0; h < 4; ++h) kc[h] = ksr[h] * c;
+        uint64_t seen[RT];
+        float top[RT], largest = fmaxf(fmaxf(vsr[0], vsr[1]), fmaxf(vsr[2], vsr[3]));
+        bool raise = !(largest * inv <= 128.0f);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            if (MIXED) {
+                const int left = sees[rt] < u.t_end ? sees[rt] - t : u.t_end - t;
+                seen[rt] = left >= 64 ? ~0ull : left > 0 ? (1ull << left) - 1ull : 0ull;
+                seen[rt] >>= 4 * kk;
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    S[rt][e / 4][e % 4] = seen[rt] >> (16 * (e / 4) + e % 4) & 1u ? S[rt][e / 4][e % 4] * kc[e / 4] : -INFINITY;
+            }
+            float lo, hi, x[4];
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                x[h] = largest4(S[rt][h]);
+                if (!MIXED) x[h] *= kc[h];  // (scales are not negative)
+            }
+            quarters(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), lo, hi);
+            halves(fmaxf(lo, hi), lo, hi);
+            top[rt] = fmaxf(lo, hi);
+            raise |= !(top[rt] - m_run[rt] <= 8.0f);
+        }
+        if (__ballot(raise)) {
+            largest = wave_all(largest, MaxOp());  // (NaN is passed over)
+            float less = 1.0f;
+            if (largest * inv > 128.0f && largest < INFINITY) {
+                const float now = __uint_as_float((254u + 6u - (__float_as_uint(largest) >> 23 & 0xFFu)) << 23);  // 2^6 by its power of two
+                less = now * __uint_as_float((254u << 23) - __float_as_uint(inv));                                 // (inv is a power of two)
+                inv = now;
+            }
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                const float m_new = fmaxf(m_run[rt], top[rt]), alpha = m_run[rt] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run[rt] - m_new);
+                l_run[rt] *= alpha;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) O[rt][j] *= alpha * less;
+                m_run[rt] = m_new;
+            }
+        }
+        float lv[4], rv[4];
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            const float v = vsr[h] * inv < kLeast ? kLeast : vsr[h] * inv;  // (NaN stays)
+            lv[h] = __builtin_amdgcn_logf(v);
+            rv[h] = __builtin_amdgcn_rcpf(v);
+        }
+        f16x8_t P[RT][2];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            const float less = m_run[rt] == -INFINITY ? 0.0f : m_run[rt];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                f32x8_t z;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int h = 2 * k + e / 4;
+                    z[e] = __builtin_amdgcn_exp2f(MIXED ? S[rt][h][e % 4] + (lv[h] - less) : fmaf(S[rt][h][e % 4], kc[h], lv[h] - less));
+                    if (MIXED) z[e] = seen[rt] >> (16 * h + e % 4) & 1u ? z[e] : 0.0f;  // (a scale that is not seen may be NaN)
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const float by = MIXED && !(seen[rt] >> (16 * (2 * k + i)) & 0xFu) ? 0.0f : rv[2 * k + i];
+                    l_run[rt] = fmaf((z[4 * i] + z[4 * i + 1]) + (z[4 * i + 2] + z[4 * i + 3]), by, l_run[rt]);
+                }
+                P[rt][k] = __builtin_convertvector(z, f16x8_t);
+            }
+        }
+#pragma unroll
+        for (int db = 0; db < 8; ++db)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                // position e of lane (channel, kk): token 32 k + 16 (e / 4) + 4 kk + e % 4, as in P
+                const unsigned char *from = lds + vat[db] + 8192 * k;
+                const s16x4_t a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)from);
+                const s16x4_t a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(from + 4096));
+                const f16x8_t v = __builtin_bit_cast(f16x8_t, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) O[rt][db] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, P[rt][k], O[rt][db], 0, 0, 0);
+            }
+        if (CODE == XKV_E4M3 && t + TILE > all) {  // NaN of noted tokens to the rows that see them
+            for (int i = 0; i < 2; ++i)
+                for (uint32_t bits = __builtin_amdgcn_readfirstlane(sm_odd[note][i]); bits; bits &= bits - 1) {
+                    const int j = t + 32 * i + __builtin_ctz(bits);
+                    const uint8_t *v = V + (size_t)(j < u.t_end ? j : u.t_end - 1) * D + 4 * kk;
+#pragma unroll
+                    for (int db = 0; db < 8; ++db)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const bool nan = (v[16 * db + e] & 0x7F) == 0x7F;
+#pragma unroll
+                            for (int rt = 0; rt < RT; ++rt) O[rt][db][e] = nan && j < sees[rt] && j < u.t_end ? __builtin_nanf("") : O[rt][db][e];
+                        }
+                }
+        }
+    };
+
+    if (u.some) {
+        store(u.t_begin, 0, 0);
+        if (u.t_begin + TILE < u.t_end) request(u.t_begin + TILE);
+        request_scales(u.t_begin);
+    }
+    lds_barrier();
+    int buf = 0, note = 0;
+    for (int t = u.t_begin; t < u.t_end; t += TILE, buf ^= 1) {
+        const unsigned char *lds = smem + 2 * KV * buf;
+        const bool next = t + TILE < u.t_end;
+        const int then = note < 2 ? note + 1 : 0;
+        if (CODE == XKV_E4M3 && threadIdx.x < 2) sm_odd[then < 2 ? then + 1 : 0][threadIdx.x] = 0u;  // (read before the last barrier, written after the next)
+        if (next) {
+            store(t + TILE, buf ^ 1, then);
+            if (t + 2 * TILE < u.t_end) request(t + 2 * TILE);
+        }
+        if (t + TILE <= least)
+            tile(t, lds, note, std::false_type{});
+        else if (t < most)
+            tile(t, lds, note, std::true_type{});
+        if (next) request_scales(t + TILE);
+        lds_barrier();
+        note = then;
+    }
+
+    const float undo = __uint_as_float((254u << 23) - __float_as_uint(inv));
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        float lo, hi;
+        quarters(l_run[rt], lo, hi);
+        halves(lo + hi, lo, hi);
+        const float den = lo + hi;
+        const int m = ((u.tile * WAVES + w) * RT + rt) * 16 + n16;
+        if (m >= M) continue;
+        const size_t row = ((size_t)(direct ? u.seq : u.part) * a.N + m / n_rep) * a.H_q + u.g * n_rep + m % n_rep;
+#pragma unroll
+        for (int db = 0; db < 8; ++db) {
+            if (direct) {
+                typedef __attribute__((ext_vector_type(4))) uint16_t u16x4_t;
+                u16x4_t x;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = result<bf16_t>(sees[rt] == 0 ? 0.0f : undo * O[rt][db][e] / den);
+                *reinterpret_cast<u16x4_t *>((bf16_t *)a.out + row * D + 16 * db + 4 * kk) = x;
+            } else {
+                *reinterpret_cast<f32x4_t *>(a.part_o + row * D + 16 * db + 4 * kk) = undo * O[rt][db];
+            }
+        }
+        if (!direct && kk == 0) {
+            a.part_ml[2 * row] = m_run[rt];
+            a.part_ml[2 * row + 1] = den;
         }
     }
 }
@@ -568,11 +947,18 @@ hipError_t launch_mfma(const Cache8Args &a, bool direct, hipStream_t st)
         hipLaunchKernelGGL(kernel, unit_grid(a), dim3(256), 0, st, a, direct);
         return hipGetLastError();
     };
-    if (a.rows == 16) return launch(cache8_mfma_kernel<CODE, D, 1>);
-    if constexpr (D < 256) {
-        if (a.rows == 64) return launch(cache8_mfma_kernel<CODE, D, 4>);
+    const bool once = a.rows >= a.N * (a.H_q / a.H_kv);
+    if (a.rows == 16) return once ? launch(cache8_mfma_kernel<CODE, D, 1, true>) : launch(cache8_mfma_kernel<CODE, D, 1, false>);
+    if constexpr (D == 128) {
+        auto rows = [&](auto kernel, int waves) {
+            hipLaunchKernelGGL(kernel, unit_grid(a), dim3(64 * waves), 0, st, a, direct);
+            return hipGetLastError();
+        };
+        if (a.rows == 128) return rows(cache8_rows_kernel<CODE, 4>, 4);
+        if (a.rows == 256) return rows(cache8_rows_kernel<CODE, 8>, 8);
     }
-    return launch(cache8_mfma_kernel<CODE, D, 2>);
+    if constexpr (D < 256) return once ? launch(cache8_mfma_kernel<CODE, D, 2, true>) : launch(cache8_mfma_kernel<CODE, D, 2, false>);
+    return hipErrorInvalidValue;
 }
 template <int CODE>
 hipError_t launch_mfma(const Cache8Args &a, bool direct, hipStream_t st)
