@@ -494,8 +494,8 @@ XKV_API xkv_status xkv_rotate(const xkv_shape *shape, int32_t d_rot, int32_t lay
  * xkv_cache8_decode: query i of sequence b, q [batch][N][H_q][d_h], attends to the first visible[b][i] rows (device int32 [batch][N], nullable: all L; counts as
  *   the nearer of 0 and L): a token after a cache, a drafted chain, or the tokens of a prompt, each with the rows up to its own.
  *     z_t = scale k_scale[t / c] <q, K8_t>,  out = sum_t softmax(z)_t v_scale[t / c] V8_t;  out [batch][N][H_q][d_h] in shape->dtype.
- *   Zeros for a query that sees nothing.  Sums and statistics are fp32.  A weight times its scale enters the sums held to 2^-12, or to 2^-31 of the largest such
- *   product that a workgroup's rows can have where that is more (fp32 shapes: fp32); results are rounded once.  A NaN in a code or scale that a query
+ *   Zeros for a query that sees nothing.  Sums and statistics are fp32.  A weight times its scale enters the sums held to 2^-12 (fp32 shapes: 2^-22), or to
+ *   2^-31 of the largest such product that a workgroup's rows can have where that is more; results are rounded once.  A NaN in a code or scale that a query
  *   sees gives NaN, one that it does not see does not reach it.  Scales are numbers from 2^-100 to 2^100, 0 or NaN: infinities, and products
  *   of a weight with a smaller scale, need not come out as the formula says.
  *   Results do not depend on the order in which workgroups run.  workspace: xkv_cache8_workspace_bytes(shape, N) bytes, 256-byte aligned.

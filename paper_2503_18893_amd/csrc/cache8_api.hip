@@ -60,11 +60,11 @@ xkv_status plan_cache8(const xkv_shape &s, int N, Cache8Plan &p)
     p.n_rep = s.H_q / s.H_kv;
     p.scale = s.scale > 0.0f ? s.scale : 1.0f / std::sqrt((float)s.d_h);
     const long long M = (long long)N * p.n_rep;
-    p.mfma = s.dtype == XKV_BF16 && (s.d_h == 64 || s.d_h == 128 || s.d_h == 256);
+    p.mfma = s.d_h == 64 || s.d_h == 128 || s.d_h == 256;
     // Rows of a workgroup.  Two workgroups of the matrix-core kernels to a compute unit, one of 256 rows or channels; four of the general one.
     // (65 rows and more of 128 channels: 256 that share tiles, or 128 where that leaves fewer of them empty: 256 queries of 7 heads after 131072
     // rows, 1792 rows a KV head, 631 us by 256, 667 by 128, 783 by 32 that do not share.)
-    p.rows = !p.mfma || M <= 16 || s.d_h == 256 ? 16 : M <= 64 || s.d_h != 128 ? 32 : (ceil_div(M, 128) & 1) ? 128 : 256;
+    p.rows = !p.mfma || M <= 16 || s.d_h == 256 || s.dtype == XKV_F32 ? 16 : M <= 64 || s.d_h != 128 ? 32 : (ceil_div(M, 128) & 1) ? 128 : 256;
     p.round = p.mfma ? 128 : 64;
     const int slots = !p.mfma ? 1024 : p.rows == 256 || s.d_h == 256 ? 256 : 512;
     const int row_tiles = ceil_div(M, p.rows), longest = ceil_div(s.L, p.round);

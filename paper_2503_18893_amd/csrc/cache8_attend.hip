@@ -88,6 +88,7 @@ template <typename T, int CODE, int JP>
 __global__ __launch_bounds__(256) void cache8_general_kernel(Cache8Args a)
 {
     extern __shared__ __attribute__((aligned(16))) float smem_f[];
+    constexpr int TOGETHER = 16 / JP;  // rows of a wavefront that are requested together
     const Unit8 u = unit8(a);
     if (!u.some) return;  // (the merge knows)
     const int lane = lane_id(), w = wave_id(), n_rep = a.H_q / a.H_kv, d = a.d_h, d4 = (d + 3) / 4 * 4, pitch = general_pitch(d);
@@ -117,16 +118,30 @@ __global__ __launch_bounds__(256) void cache8_general_kernel(Cache8Args a)
     }
     for (int t0 = u.t_begin; t0 < u.t_end; t0 += kGenTokens) {
         __syncthreads();
-        for (int i = w; i < kGenTokens; i += 4) {
-            const int t = t0 + i < u.t_end ? t0 + i : u.t_end - 1;
-            const float k_scale = ks[t >> a.shift], v_scale = vs[t >> a.shift];
+        for (int i0 = w; i0 < kGenTokens; i0 += 4 * TOGETHER) {
+            uint8_t kx[TOGETHER][JP], vx[TOGETHER][JP];
+            float k_scale[TOGETHER], v_scale[TOGETHER];
 #pragma unroll
-            for (int jj = 0; jj < JP; ++jj) {
-                const int j = lane + jj * kWave;
-                if (j >= d4) continue;
-                kt[i * pitch + j] = j < d ? k_scale * value8<CODE>(K[(size_t)t * d + j]) : 0.0f;
-                vt[i * pitch + j] = j < d ? v_scale * value8<CODE>(V[(size_t)t * d + j]) : 0.0f;
+            for (int x = 0; x < TOGETHER; ++x) {
+                const int t = t0 + i0 + 4 * x < u.t_end ? t0 + i0 + 4 * x : u.t_end - 1;
+                k_scale[x] = ks[t >> a.shift];
+                v_scale[x] = vs[t >> a.shift];
+#pragma unroll
+                for (int jj = 0; jj < JP; ++jj) {
+                    const int j = lane + jj * kWave, jc = j < d ? j : 0;
+                    kx[x][jj] = K[(size_t)t * d + jc];
+                    vx[x][jj] = V[(size_t)t * d + jc];
+                }
             }
+#pragma unroll
+            for (int x = 0; x < TOGETHER; ++x)
+#pragma unroll
+                for (int jj = 0; jj < JP; ++jj) {
+                    const int j = lane + jj * kWave, i = i0 + 4 * x;
+                    if (j >= d4) continue;
+                    kt[i * pitch + j] = j < d ? k_scale[x] * value8<CODE>(kx[x][jj]) : 0.0f;
+                    vt[i * pitch + j] = j < d ? v_scale[x] * value8<CODE>(vx[x][jj]) : 0.0f;
+                }
         }
         __syncthreads();
         const int t = t0 + lane;
@@ -295,9 +310,12 @@ __device__ __forceinline__ float largest4(const f32x4_t &x) { return fmaxf(fmaxf
 constexpr float kFarUp = 0x1p126f;  // `inv` before any scale was met
 constexpr float kLeast = 0x1p-60f;  // scales by `inv` that are less count as this: their weights are zeros in fp16
 
-template <int CODE, int D, int RT, bool ONCE>
+template <typename T, int CODE, int D, int RT, bool ONCE>
 __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void cache8_mfma_kernel(Cache8Args a, bool direct)
 {
+    constexpr bool F32 = sizeof(T) == 4;
+    constexpr int TERMS = F32 ? 3 : 1;  // of a query
+    static_assert(!F32 || RT == 1, "queries in registers");
     constexpr int KP = D / 64, VW = D / 64, JC = D / 16, STEPS = D / 32, PITCH = D / 4;  // pieces of K, words of V, channels of a lane; products; 16-byte pieces of a row
     constexpr bool Q_LDS = RT > 1;
     __shared__ f32x4_t sm_o[4][16 * PITCH];
@@ -350,22 +368,33 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void cache8_mfma_kernel(Cache
     }
 
     // Q^T operands: lane (row n16, kk), product s, position e: channel 64 (s / 2) + 16 kk + 8 (s % 2) + e, as the pieces of K have them
-    u32x4_t Q[STEPS];
+    u32x4_t Q[TERMS][STEPS];
     int sees[RT], least = 0x7FFFFFFF;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         const int m = (u.tile * RT + rt) * 16 + n16, m_in = m < M ? m : M - 1, i = m_in / n_rep;
-        const bf16_t *q = (const bf16_t *)a.q + (((size_t)u.seq * a.N + i) * a.H_q + u.g * n_rep + m_in % n_rep) * D;
+        const T *q = (const T *)a.q + (((size_t)u.seq * a.N + i) * a.H_q + u.g * n_rep + m_in % n_rep) * D;
         sees[rt] = visible8(a, u.seq, i);
         least = sees[rt] < least ? sees[rt] : least;
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
             if (Q_LDS && (rt * STEPS + s) % 4 != w) continue;
-            const u32x4_t x = *reinterpret_cast<const u32x4_t *>(q + 64 * (s / 2) + 16 * kk + 8 * (s % 2));
-            if (Q_LDS)
-                sm_q[(rt * STEPS + s) * 64 + lane] = x;
-            else
-                Q[s] = x;
+            const T *from = q + 64 * (s / 2) + 16 * kk + 8 * (s % 2);
+            if constexpr (F32) {  // three terms of bf16 hold a query's 24 bits
+                f32x8_t x = *reinterpret_cast<const f32x8_t *>(from);
+#pragma unroll
+                for (int i = 0; i < TERMS; ++i) {
+                    const bf16x8_t y = __builtin_convertvector(x, bf16x8_t);
+                    Q[i][s] = __builtin_bit_cast(u32x4_t, y);
+                    x -= __builtin_convertvector(y, f32x8_t);
+                }
+            } else {
+                const u32x4_t x = *reinterpret_cast<const u32x4_t *>(from);
+                if (Q_LDS)
+                    sm_q[(rt * STEPS + s) * 64 + lane] = x;
+                else
+                    Q[0][s] = x;
+            }
         }
     }
     least = -wave_all(-least, MaxOp());  // rows that all of them see
@@ -396,9 +425,12 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void cache8_mfma_kernel(Cache
             for (int h = 0; h < 2; ++h) kb[h] = codes8<CODE>(kr[h][s / 2].x[2 * (s % 2)], kr[h][s / 2].x[2 * (s % 2) + 1]);
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
-                const bf16x8_t qf = __builtin_bit_cast(bf16x8_t, Q_LDS ? sm_q[(rt * STEPS + s) * 64 + lane] : Q[s]);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) S[rt][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb[h], qf, S[rt][h], 0, 0, 0);
+                for (int i = TERMS - 1; i >= 0; --i) {
+                    const bf16x8_t qf = __builtin_bit_cast(bf16x8_t, Q_LDS ? sm_q[(rt * STEPS + s) * 64 + lane] : Q[i][s]);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) S[rt][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb[h], qf, S[rt][h], 0, 0, 0);
+                }
             }
         }
         const float kc[2] = {ksr[0] * c, ksr[1] * c};
@@ -445,15 +477,15 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void cache8_mfma_kernel(Cache
                 m_run[rt] = m_new;
             }
         }
-        // vs P = exp2(z - m + log2 vs), whose sum by 1 / vs is that of the weights
+        // vs P = exp2(z - m + log2 vs), whose sum by 1 / vs is that of the weights (fp32: one after the other)
         float lv[2], rv[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const float v = vsr[h] * inv < kLeast ? kLeast : vsr[h] * inv;  // (NaN stays)
-            lv[h] = __builtin_amdgcn_logf(v);
-            rv[h] = __builtin_amdgcn_rcpf(v);
+            lv[h] = F32 ? 0.0f : __builtin_amdgcn_logf(v);
+            rv[h] = F32 ? 1.0f : __builtin_amdgcn_rcpf(v);
         }
-        f16x8_t P[RT];
+        f16x8_t P[RT], R[RT];  // .. (fp32) and what P leaves
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             const float less = m_run[rt] == -INFINITY ? 0.0f : m_run[rt], add[2] = {lv[0] - less, lv[1] - less};
@@ -470,7 +502,12 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void cache8_mfma_kernel(Cache
                 const float by = MIXED && !(seen[rt] >> (16 * h) & 0xFu) ? 0.0f : rv[h];
                 l_run[rt] = fmaf((z[4 * h] + z[4 * h + 1]) + (z[4 * h + 2] + z[4 * h + 3]), by, l_run[rt]);
             }
+            if constexpr (F32) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) z[e] *= MIXED && !(seen[rt] >> (16 * (e / 4)) & 0xFu) ? 0.0f : vsr[e / 4] * inv;
+            }
             P[rt] = __builtin_convertvector(z, f16x8_t);
+            if constexpr (F32) R[rt] = __builtin_convertvector(z - __builtin_convertvector(P[rt], f32x8_t), f16x8_t);
         }
         if (CODE == XKV_E4M3 && MIXED) {
             // Codes of V that are NaN reach the rows that see them, not the others: where there are any, the NaN of a channel that a row sees are
@@ -521,6 +558,7 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void cache8_mfma_kernel(Cache
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) {
                     f32x4_t &o = O[rt][4 * i + j];
+                    if (F32) o = __builtin_amdgcn_mfma_f32_16x16x32_f16(vb[j], R[rt], o, 0, 0, 0);
                     o = __builtin_amdgcn_mfma_f32_16x16x32_f16(vb[j], P[rt], o, 0, 0, 0);
                 }
         }
@@ -571,9 +609,9 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void cache8_mfma_kernel(Cache
                 den += sm_l[i][row] * (sm_m[i][row] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(sm_m[i][row] - most));
             if (direct) {
                 const bool none = visible8(a, u.seq, m / n_rep) == 0;
-                bf16_t *out = (bf16_t *)a.out + (((size_t)u.seq * a.N + m / n_rep) * a.H_q + u.g * n_rep + m % n_rep) * D + 4 * p;
+                T *out = (T *)a.out + (((size_t)u.seq * a.N + m / n_rep) * a.H_q + u.g * n_rep + m % n_rep) * D + 4 * p;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) out[e] = result<bf16_t>(none ? 0.0f : x[e] / den);
+                for (int e = 0; e < 4; ++e) out[e] = result<T>(none ? 0.0f : x[e] / den);
                 continue;
             }
             const size_t slot = ((size_t)u.part * a.N + m / n_rep) * a.H_q + u.g * n_rep + m % n_rep;
@@ -879,44 +917,92 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_rows_kernel(Cache8Args a
 }
 
 // ------------------------------------------------------------------------------------------
-// Merge: a wavefront per row (query, head).  Partials of parts that have no rows were not written and are not read.
+// Merge.  A group of 2^lg lanes covers the columns of a row (query, head), VEC a lane.  Where there are many rows, a group per row; where there are few,
+// the groups of a workgroup share a row's partials and are added up in LDS: latency is all there is to it then, and the first partials are
+// requested before their weights are known.  Partials of parts that have no rows were not written and are not read.
 // ------------------------------------------------------------------------------------------
-template <typename T>
-__global__ __launch_bounds__(256) void cache8_merge_kernel(Cache8Args a, int rows)
+template <typename T, int VEC>
+__global__ __launch_bounds__(256) void cache8_merge_kernel(Cache8Args a, int lg, int share, int rows)
 {
-    __shared__ float sm_w[4][kMaxCacheParts];
-    const int lane = lane_id(), w = wave_id(), row = (int)blockIdx.x * 4 + w;
-    if (row >= rows) return;  // (nothing below is waited for by other wavefronts)
+    typedef __attribute__((ext_vector_type(VEC))) float vec_t;
+    constexpr int BATCH = 8;
+    __shared__ vec_t sm[256];
+    __shared__ float sm_w[32][kMaxCacheParts];
+    const int width = 1 << lg, l = (int)threadIdx.x & (width - 1), grp = (int)threadIdx.x >> lg, groups = 256 >> lg;
+    const int col = ((int)blockIdx.y * width + l) * VEC;
+    const int item = share ? (int)blockIdx.x : (int)blockIdx.x * groups + grp, row = item < rows ? item : rows - 1;
     const int n_rep = a.H_q / a.H_kv, head = row % a.H_q, i = row / a.H_q % a.N, seq = row / a.H_q / a.N;
     int first, parts;
     if (a.by_length) {
         first = a.table[seq];
         parts = a.table[seq + 1] - first;
     } else {
-        const int n = tile_sees(a, seq, (i * n_rep + head % n_rep) / a.rows);
+        int lo, hi, n = 0;
+        tile_queries(a, (i * n_rep + head % n_rep) / a.rows, lo, hi);
+        for (int j = lo + l; j <= hi; j += width) n = MaxOp()(n, visible8(a, seq, j));
+        for (int off = 1; off < width; off <<= 1) n = MaxOp()(n, __shfl_xor(n, off, kWave));
         first = seq * a.parts;
         parts = ceil_div_dev(n, tile_chunk(a, n));
     }
+    const bool none = visible8(a, seq, i) == 0;  // (the logits of all that a row sees may be -inf: 0 / 0; a NaN among them is in its sum)
     const size_t stride = (size_t)a.N * a.H_q, at = first * stride + (size_t)i * a.H_q + head;
+    const float *ml = a.part_ml + 2 * at, *po = a.part_o + at * a.d_h + (col < a.d_h ? col : 0);
+    const int step = share ? groups : 1, begin = share ? grp : 0;
+    vec_t v[BATCH];
+    auto request = [&](int s0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < BATCH; ++u) {
+            const int s = s0 + u * step < parts ? s0 + u * step : 0;
+            v[u] = parts > 0 ? *reinterpret_cast<const vec_t *>(po + (size_t)s * stride * a.d_h) : vec_t(0.0f);
+        }
+    };
+    request(begin);
     float m = -INFINITY, den = 0.0f;
-    for (int s = lane; s < parts; s += kWave) m = fmaxf(m, a.part_ml[2 * (at + s * stride)]);
-    m = wave_all(m, MaxOp());
-    for (int s = lane; s < parts; s += kWave) {
-        const float top = a.part_ml[2 * (at + s * stride)], wt = top == -INFINITY ? 0.0f : exp2f(top - m);
-        sm_w[w][s] = wt;
-        den = fmaf(wt, a.part_ml[2 * (at + s * stride) + 1], den);
+    for (int s = l; s < parts; s += width) m = fmaxf(m, ml[2 * s * stride]);
+    for (int off = 1; off < width; off <<= 1) m = fmaxf(m, __shfl_xor(m, off, kWave));
+    for (int s = l; s < parts; s += width) {
+        const float top = ml[2 * s * stride], wt = top == -INFINITY ? 0.0f : exp2f(top - m);
+        sm_w[grp][s] = wt;
+        den = fmaf(top == -INFINITY ? 1.0f : wt, ml[2 * s * stride + 1], den);  // (a part without a maximum: 0, or NaN)
     }
-    den = wave_all(den, AddOp());
-    // (the logits of all that a row sees may be -inf: 0 / 0; a NaN among them is in its sum)
-    const bool none = visible8(a, seq, i) == 0;
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    for (int off = 1; off < width; off <<= 1) den += __shfl_xor(den, off, kWave);
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");  // (a group is part of a wavefront)
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    for (int j = lane; j < a.d_h; j += kWave) {
-        float o = 0.0f;
-        for (int s = 0; s < parts; ++s) o = fmaf(sm_w[w][s], a.part_o[(at + s * stride) * a.d_h + j], o);
-        ((T *)a.out)[(size_t)row * a.d_h + j] = result<T>(none ? 0.0f : o / den);
+    vec_t acc = vec_t(0.0f);
+    for (int s0 = begin; s0 < parts; s0 += BATCH * step) {
+        if (s0 > begin) request(s0);
+#pragma unroll
+        for (int u = 0; u < BATCH; ++u) {
+            const int s = s0 + u * step;
+            if (s < parts) acc += sm_w[grp][s] * v[u];
+        }
     }
+    if (share) {
+        sm[threadIdx.x] = acc;
+        __syncthreads();
+        if (grp > 0) return;
+        for (int k = 1; k < groups; ++k) acc += sm[(k << lg) + l];
+    }
+    if (item >= rows || col >= a.d_h) return;
+    T *out = (T *)a.out + (size_t)row * a.d_h + col;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) out[e] = result<T>(none ? 0.0f : acc[e] / den);
+}
+
+template <typename T>
+hipError_t launch_merge(const Cache8Args &a, hipStream_t st)
+{
+    const int vec = a.d_h % 4 == 0 ? 4 : 1, rows = a.batch * a.N * a.H_q;
+    int lg = 3;
+    while (lg < 6 && (vec << lg) < a.d_h) ++lg;
+    const int share = rows < 2048, groups = 256 >> lg;
+    const dim3 grid(share ? rows : (rows + groups - 1) / groups, (a.d_h + (vec << lg) - 1) / (vec << lg));
+    if (vec == 4)
+        hipLaunchKernelGGL((cache8_merge_kernel<T, 4>), grid, dim3(256), 0, st, a, lg, share, rows);
+    else
+        hipLaunchKernelGGL((cache8_merge_kernel<T, 1>), grid, dim3(256), 0, st, a, lg, share, rows);
+    return hipGetLastError();
 }
 
 dim3 unit_grid(const Cache8Args &a)
@@ -940,30 +1026,29 @@ hipError_t launch_general(const Cache8Args &a, hipStream_t st)
          : a.d_h <= 128 ? launch(cache8_general_kernel<T, CODE, 2>, attr[1]) : launch(cache8_general_kernel<T, CODE, 4>, attr[2]);
 }
 
-template <int CODE, int D>
+template <typename T, int CODE, int D>
 hipError_t launch_mfma(const Cache8Args &a, bool direct, hipStream_t st)
 {
-    auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, unit_grid(a), dim3(256), 0, st, a, direct);
+    auto launch = [&](auto kernel, int threads = 256) {
+        hipLaunchKernelGGL(kernel, unit_grid(a), dim3(threads), 0, st, a, direct);
         return hipGetLastError();
     };
     const bool once = a.rows >= a.N * (a.H_q / a.H_kv);
-    if (a.rows == 16) return once ? launch(cache8_mfma_kernel<CODE, D, 1, true>) : launch(cache8_mfma_kernel<CODE, D, 1, false>);
-    if constexpr (D == 128) {
-        auto rows = [&](auto kernel, int waves) {
-            hipLaunchKernelGGL(kernel, unit_grid(a), dim3(64 * waves), 0, st, a, direct);
-            return hipGetLastError();
-        };
-        if (a.rows == 128) return rows(cache8_rows_kernel<CODE, 4>, 4);
-        if (a.rows == 256) return rows(cache8_rows_kernel<CODE, 8>, 8);
+    if (a.rows == 16) return once ? launch(cache8_mfma_kernel<T, CODE, D, 1, true>) : launch(cache8_mfma_kernel<T, CODE, D, 1, false>);
+    if constexpr (sizeof(T) == 2 && D < 256) {
+        if (a.rows == 32) return once ? launch(cache8_mfma_kernel<T, CODE, D, 2, true>) : launch(cache8_mfma_kernel<T, CODE, D, 2, false>);
+        if constexpr (D == 128) return a.rows == 128 ? launch(cache8_rows_kernel<CODE, 4>, 256) : launch(cache8_rows_kernel<CODE, 8>, 512);
     }
-    if constexpr (D < 256) return once ? launch(cache8_mfma_kernel<CODE, D, 2, true>) : launch(cache8_mfma_kernel<CODE, D, 2, false>);
     return hipErrorInvalidValue;
 }
-template <int CODE>
-hipError_t launch_mfma(const Cache8Args &a, bool direct, hipStream_t st)
+
+template <typename T, int CODE>
+hipError_t launch_of(Cache8Args a, bool matrix, bool direct, hipStream_t st)
 {
-    return a.d_h == 64 ? launch_mfma<CODE, 64>(a, direct, st) : a.d_h == 128 ? launch_mfma<CODE, 128>(a, direct, st) : launch_mfma<CODE, 256>(a, direct, st);
+    if (matrix)
+        return a.d_h == 64 ? launch_mfma<T, CODE, 64>(a, direct, st) : a.d_h == 128 ? launch_mfma<T, CODE, 128>(a, direct, st)
+                                                                                     : launch_mfma<T, CODE, 256>(a, direct, st);
+    return launch_general<T, CODE>(a, st);
 }
 
 }  // namespace
@@ -974,23 +1059,12 @@ hipError_t launch_cache8_attend(const xkv_shape &s, const Cache8Args &given, int
     const bool matrix = mfma && a.shift >= 2 && ((uintptr_t)a.K8 | (uintptr_t)a.V8 | (uintptr_t)a.q) % 16 == 0;
     // one part of every row tile, and a workgroup for it also where it has no rows
     const bool direct = matrix && a.parts == 1 && (!a.by_length || a.batch == 1);
-    hipError_t e;
-    if (matrix) {
-        e = code == XKV_E4M3 ? launch_mfma<XKV_E4M3>(a, direct, st) : launch_mfma<XKV_INT8>(a, direct, st);
-    } else {
-        a.rows = kGenRows;  // (its rounds divide those of the plan)
-        if (s.dtype == XKV_F32)
-            e = code == XKV_E4M3 ? launch_general<float, XKV_E4M3>(a, st) : launch_general<float, XKV_INT8>(a, st);
-        else
-            e = code == XKV_E4M3 ? launch_general<bf16_t, XKV_E4M3>(a, st) : launch_general<bf16_t, XKV_INT8>(a, st);
-    }
+    if (!matrix) a.rows = kGenRows;  // (its rounds divide those of the plan)
+    const hipError_t e = s.dtype == XKV_F32 ? code == XKV_E4M3 ? launch_of<float, XKV_E4M3>(a, matrix, direct, st) : launch_of<float, XKV_INT8>(a, matrix, direct, st)
+                       : code == XKV_E4M3   ? launch_of<bf16_t, XKV_E4M3>(a, matrix, direct, st)
+                                            : launch_of<bf16_t, XKV_INT8>(a, matrix, direct, st);
     if (e != hipSuccess || direct) return e;
-    const int rows = a.batch * a.N * a.H_q;
-    if (s.dtype == XKV_F32)
-        hipLaunchKernelGGL(cache8_merge_kernel<float>, dim3((rows + 3) / 4), dim3(256), 0, st, a, rows);
-    else
-        hipLaunchKernelGGL(cache8_merge_kernel<bf16_t>, dim3((rows + 3) / 4), dim3(256), 0, st, a, rows);
-    return hipGetLastError();
+    return s.dtype == XKV_F32 ? launch_merge<float>(a, st) : launch_merge<bf16_t>(a, st);
 }
 
 }  // namespace xkv

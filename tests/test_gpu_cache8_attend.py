@@ -64,8 +64,8 @@ def run(s, code, c, visible, q, state, ws=None):
 
 
 def check(s, code, c, visible, q, state, out, what):
-    """Weights times scales are fp16 operands: to 2^-12 of each (less than the storage type's half step, which the reference allows a weight), but
-    for those below 2^-14, whose steps are 2^-24.  The largest scale that a query may see is brought to at least 2^6 there, and the largest
+    """Weights times scales are fp16 operands: to 2^-12 of each (less than the storage type's half step, which the reference allows a weight;
+    fp32: two of them, 2^-22, within the 2^-20 for its exponential), but for those below 2^-14, whose steps are 2^-24.  The largest scale that a query may see is brought to at least 2^6 there, and the largest
     weight to at least 1, so such a step's half is 2^-31 of that scale beside a sum of weights of at least 1, for every token, times its code."""
     n_rep, N = s.H_q // s.H_kv, q.shape[1]
     K, V = ref8.rows(state[0], state[2], c), ref8.rows(state[1], state[3], c)
@@ -76,7 +76,7 @@ def check(s, code, c, visible, q, state, out, what):
         for g in range(s.H_kv):
             heads = slice(g * n_rep, (g + 1) * n_rep)
             want, _, bound, _ = ref.attend(q[b, :, heads].reshape(-1, s.d_h), K[b, g, :n], V[b, g, :n], sees, s.scale or s.d_h ** -0.5)
-            if s.dtype == "bf16" and n > 0:
+            if n > 0:
                 codes = state[1][b, g, :n].float().abs().double()
                 bound = bound + 2.0 ** -31 * state[3][b, g, : -(-n // c)].max().double() * codes.sum(0)
             within(out[b, :, heads].reshape(-1, s.d_h), want, bound, f"{what} sequence {b} head {g}")
