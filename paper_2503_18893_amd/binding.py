@@ -7,6 +7,7 @@ There is no CPU fallback: if the HIP library is not built, loading raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from dataclasses import dataclass
 
@@ -69,6 +70,11 @@ class Shape:
     def c(self) -> xkv_shape:
         return xkv_shape(self.G, self.H_kv, self.H_q, self.d_h, self.r_k, self.r_v, self.L, self.k, self.batch,
                          DTYPES[self.dtype], self.scale)
+
+    @functools.cached_property
+    def ref(self):
+        """c() by reference, made once: a call that is made for every token takes longer to set up than to run otherwise."""
+        return ctypes.byref(self.c())
 
     @staticmethod
     def of(w, **kw) -> "Shape":
@@ -159,14 +165,14 @@ def xkv_version() -> int:
 
 
 def _ptr(t):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
 def _stream(stream):
     if stream is None:
         import torch
         stream = torch.cuda.current_stream().cuda_stream
-    return ctypes.c_void_p(int(stream))
+    return int(stream)
 
 
 def _check(status: int, where: str):
@@ -456,9 +462,10 @@ def _rows(t):
     """Where the rows of a tensor [batch][N][heads][d_h] lie, whose last axis is contiguous; None for no tensor."""
     if t is None:
         return None
-    if t.dim() != 4 or (t.stride(3) != 1 and t.shape[3] != 1):
+    strides = t.stride()
+    if len(strides) != 4 or (strides[3] != 1 and t.shape[3] != 1):
         raise ValueError("rows are wanted as a tensor [batch][N][heads][d_h] with a contiguous last axis")
-    return ctypes.byref(xkv_rows(t.stride(0), t.stride(1), t.stride(2)))
+    return xkv_rows(strides[0], strides[1], strides[2])
 
 
 def xkv_rope_frequencies(d_rot, theta, scaling, factor, low, high, context, frequencies, stream=None):
@@ -470,28 +477,28 @@ def xkv_rope_frequencies(d_rot, theta, scaling, factor, low, high, context, freq
 def xkv_rotate(shape, d_rot, layout, direction, amplitude, frequencies, positions, N, q, q_out, K, K_out, stream=None):
     """layout: "half" or "interleaved"; direction: "forward", "inverse" or "gradient".  q, q_out, K, K_out are [batch][N][heads][d_h] with any
     strides over the first three axes (views are taken as they are); q and q_out, or K and K_out, may be None."""
-    _check(load().xkv_rotate(ctypes.byref(shape.c()), int(d_rot), ROPE_LAYOUTS[layout], ROPE_DIRECTIONS[direction], float(amplitude),
-                             _ptr(frequencies), _ptr(positions), int(N), _ptr(q), _rows(q), _ptr(q_out), _rows(q_out), _ptr(K), _rows(K),
+    _check(load().xkv_rotate(shape.ref, d_rot, ROPE_LAYOUTS[layout], ROPE_DIRECTIONS[direction], amplitude,
+                             _ptr(frequencies), _ptr(positions), N, _ptr(q), _rows(q), _ptr(q_out), _rows(q_out), _ptr(K), _rows(K),
                              _ptr(K_out), _rows(K_out), _stream(stream)), "xkv_rotate")
 
 
 def xkv_cache8_append(shape, K, V, lengths, counts, N, code, c, K8, V8, k_scales, v_scales, stream=None):
     """code: "e4m3" or "int8".  K, V are [batch][N][H_kv][d_h] with any strides over the first three axes."""
-    _check(load().xkv_cache8_append(ctypes.byref(shape.c()), _ptr(K), _rows(K), _ptr(V), _rows(V), _ptr(lengths), _ptr(counts), int(N),
-                                    CODES[code], int(c), _ptr(K8), _ptr(V8), _ptr(k_scales), _ptr(v_scales), _stream(stream)),
+    _check(load().xkv_cache8_append(shape.ref, _ptr(K), _rows(K), _ptr(V), _rows(V), _ptr(lengths), _ptr(counts), int(N),
+                                    CODES[code], c, _ptr(K8), _ptr(V8), _ptr(k_scales), _ptr(v_scales), _stream(stream)),
            "xkv_cache8_append")
 
 
 def xkv_cache8_workspace_bytes(shape: Shape, N: int = 1) -> int:
     n = ctypes.c_size_t(0)
-    _check(load().xkv_cache8_workspace_bytes(ctypes.byref(shape.c()), int(N), ctypes.byref(n)), "xkv_cache8_workspace_bytes")
+    _check(load().xkv_cache8_workspace_bytes(shape.ref, int(N), ctypes.byref(n)), "xkv_cache8_workspace_bytes")
     return int(n.value)
 
 
 def xkv_cache8_decode(shape, K8, V8, k_scales, v_scales, code, c, visible, q, N, out, workspace, stream=None):
     """code: "e4m3" or "int8"."""
-    _check(load().xkv_cache8_decode(ctypes.byref(shape.c()), _ptr(K8), _ptr(V8), _ptr(k_scales), _ptr(v_scales), CODES[code], int(c),
-                                    _ptr(visible), _ptr(q), int(N), _ptr(out), _ptr(workspace),
+    _check(load().xkv_cache8_decode(shape.ref, _ptr(K8), _ptr(V8), _ptr(k_scales), _ptr(v_scales), CODES[code], int(c),
+                                    _ptr(visible), _ptr(q), N, _ptr(out), _ptr(workspace),
                                     workspace.numel() * workspace.element_size(), _stream(stream)), "xkv_cache8_decode")
 
 

@@ -25,7 +25,7 @@ struct Cache8Args {
     int rows;       // rows (query, head) per workgroup
     int round;      // rows of the cache that a workgroup takes at a time: parts are multiples of it
     int parts;      // by_length: of all sequences, else of every row tile
-    bool by_length; // one row tile: the parts of all sequences are cut as cache_unit does
+    bool by_length; // the parts of all sequences are cut as cache_unit does
     float scale;
 };
 
