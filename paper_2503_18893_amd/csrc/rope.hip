@@ -40,67 +40,76 @@ template <typename T, int VEC> __device__ __forceinline__ void store_piece(T *to
 }
 
 // ------------------------------------------------------------------------------------------
-// A workgroup takes `tokens` tokens of a sequence: first the cosines and sines of their pairs (angles p f_j in double precision, whole turns
-// taken off there, then fp32), which all heads share, into LDS; then, `width` threads a row (token, head), the pieces of the rows.
+// A workgroup takes `tokens` tokens of a sequence, 2^lg_width threads a row (token, head), a piece each (two that belong together in the half
+// layout).  The cosines and sines of the tokens' pairs, which all heads share, go to LDS first: angles p f_j in double precision, whole turns
+// taken off there, then fp32.  The first rows are requested before that, and ROWS of them at a time.
 // ------------------------------------------------------------------------------------------
 template <typename T, int VEC, bool INTERLEAVED>
 __global__ __launch_bounds__(kRopeThreads) void rotate_kernel(RotateArgs a, int tokens, int lg_width)
 {
+    constexpr int PAIRS = INTERLEAVED ? (VEC > 1 ? VEC / 2 : 1) : VEC;  // pairs of a piece
+    constexpr bool ONE = INTERLEAVED && VEC > 1;                        // a piece holds both channels of its pairs
+    constexpr int ROWS = 4;
     extern __shared__ float2 sm_unit[];  // [tokens][d_rot / 2]
     const int m = a.d_rot / 2, groups = (a.N + tokens - 1) / tokens;
     const int b = (int)(blockIdx.x / (unsigned)groups), first = (int)(blockIdx.x % (unsigned)groups) * tokens;
-    const int here = a.N - first < tokens ? a.N - first : tokens;
-    for (int i = (int)threadIdx.x; i < here * m; i += kRopeThreads) {
-        const int t = first + i / m;
+    const int here = a.N - first < tokens ? a.N - first : tokens, heads = a.heads[0] + a.heads[1], rows = here * heads;
+    const int turned = m / PAIRS, items = turned + (a.d_h - a.d_rot) / VEC;
+    const int i = (int)threadIdx.x & ((1 << lg_width) - 1), row0 = (int)threadIdx.x >> lg_width, step = kRopeThreads >> lg_width;
+    const bool turns = i < turned, works = i < items;
+    // this thread's places in a row
+    const int jl = !turns ? a.d_rot + (i - turned) * VEC : ONE ? i * VEC : INTERLEAVED ? 2 * i : i * VEC;
+    const int jh = !turns || ONE ? jl : INTERLEAVED ? 2 * i + 1 : m + i * VEC;
+    const float inv_heads = 1.0f / (float)heads;
+
+    Piece<T, VEC> l[ROWS], r[ROWS];
+    T *to[ROWS];
+    int token[ROWS];
+    auto request = [&](int row) __attribute__((always_inline)) {
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+            const int at = row + k * step;
+            if (!works || at >= rows) break;
+            int t = (int)((float)at * inv_heads), h = at - t * heads;  // (at most 8, one off at most)
+            if (h < 0) h += heads, --t;
+            if (h >= heads) h -= heads, ++t;
+            token[k] = t;
+            const int of = h < a.heads[0] ? 0 : 1, head = h - (of ? a.heads[0] : 0);
+            const xkv_rows &xs = a.x_at[of], &ys = a.y_at[of];
+            const T *x = (const T *)a.x[of] + (b * xs.sequence + (first + t) * xs.token + head * xs.head);
+            to[k] = (T *)a.y[of] + (b * ys.sequence + (first + t) * ys.token + head * ys.head);
+            load_piece(l[k], x + jl);
+            if (!ONE && turns) load_piece(r[k], x + jh);
+        }
+    };
+    request(row0);
+    for (int j = (int)threadIdx.x; j < here * m; j += kRopeThreads) {
+        const int t = first + j / m;
         const int p = a.positions ? a.positions[(size_t)b * a.N + t] : t;
-        const double turns = (double)p * (a.frequencies[i % m] * 0.15915494309189533577);
+        const double revolutions = (double)p * (a.frequencies[j % m] * 0.15915494309189533577);
         float s, c;
-        sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
-        sm_unit[i] = float2{a.amplitude * c, a.amplitude * a.sign * s};
+        sincospif(2.0f * (float)(revolutions - rint(revolutions)), &s, &c);
+        sm_unit[j] = float2{a.amplitude * c, a.amplitude * a.sign * s};
     }
     __syncthreads();
-    const int heads = a.heads[0] + a.heads[1], width = 1 << lg_width;
-    constexpr int PAIRS = INTERLEAVED ? (VEC > 1 ? VEC / 2 : 1) : VEC;  // pairs of a piece
-    const int turned = m / PAIRS, items = turned + (a.d_h - a.d_rot) / VEC;
-    for (int row = (int)threadIdx.x >> lg_width; row < here * heads; row += kRopeThreads >> lg_width) {
-        const int t = row / heads, h = row % heads, of = h < a.heads[0] ? 0 : 1, head = h - (of ? a.heads[0] : 0);
-        const T *x = (const T *)a.x[of] + (b * a.x_at[of].sequence + (first + t) * a.x_at[of].token + head * a.x_at[of].head);
-        T *y = (T *)a.y[of] + (b * a.y_at[of].sequence + (first + t) * a.y_at[of].token + head * a.y_at[of].head);
-        for (int i = (int)threadIdx.x & (width - 1); i < items; i += width) {
-            if (i >= turned) {
-                const int j = a.d_rot + (i - turned) * VEC;
-                Piece<T, VEC> p;
-                load_piece(p, x + j);
-                store_piece(y + j, p);
-                continue;
-            }
-            const float2 *unit = sm_unit + t * m + i * PAIRS;
-            if constexpr (INTERLEAVED && VEC > 1) {
-                Piece<T, VEC> p;
-                load_piece(p, x + i * VEC);
+    for (int row = row0; row < rows; row += ROWS * step) {
+        if (row > row0) request(row);
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+            if (!works || row + k * step >= rows) break;
+            if (turns) {
+                const float2 *unit = sm_unit + token[k] * m + i * PAIRS;
 #pragma unroll
                 for (int e = 0; e < PAIRS; ++e) {
                     const float2 u = unit[e];
-                    const float lo = to_f32(p.x[2 * e]), hi = to_f32(p.x[2 * e + 1]);
-                    p.x[2 * e] = result<T>(fmaf(lo, u.x, -(hi * u.y)));
-                    p.x[2 * e + 1] = result<T>(fmaf(hi, u.x, lo * u.y));
+                    T &x = ONE ? l[k].x[2 * e] : l[k].x[e], &y = ONE ? l[k].x[2 * e + 1] : r[k].x[e];
+                    const float lo = to_f32(x), hi = to_f32(y);
+                    x = result<T>(fmaf(lo, u.x, -(hi * u.y)));
+                    y = result<T>(fmaf(hi, u.x, lo * u.y));
                 }
-                store_piece(y + i * VEC, p);
-            } else {
-                const int jl = INTERLEAVED ? 2 * i : i * VEC, jh = INTERLEAVED ? 2 * i + 1 : m + i * VEC;
-                Piece<T, VEC> l, r;
-                load_piece(l, x + jl);
-                load_piece(r, x + jh);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float2 u = unit[e];
-                    const float lo = to_f32(l.x[e]), hi = to_f32(r.x[e]);
-                    l.x[e] = result<T>(fmaf(lo, u.x, -(hi * u.y)));
-                    r.x[e] = result<T>(fmaf(hi, u.x, lo * u.y));
-                }
-                store_piece(y + jl, l);
-                store_piece(y + jh, r);
+                if (!ONE) store_piece(to[k] + jh, r[k]);
             }
+            store_piece(to[k] + jl, l[k]);
         }
     }
 }
