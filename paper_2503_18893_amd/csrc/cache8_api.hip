@@ -64,7 +64,7 @@ xkv_status plan_cache8(const xkv_shape &s, int N, Cache8Plan &p)
     // Rows of a workgroup.  Two workgroups of the matrix-core kernels to a compute unit, one of 256 rows or channels; four of the general one.
     // (65 rows and more of 128 channels: 256 that share tiles, or 128 where that leaves fewer of them empty: 256 queries of 7 heads after 131072
     // rows, 1792 rows a KV head, 631 us by 256, 667 by 128, 783 by 32 that do not share.)
-    p.rows = !p.mfma || M <= 16 || s.d_h == 256 || s.dtype == XKV_F32 ? 16 : M <= 64 || s.d_h != 128 ? 32 : (ceil_div(M, 128) & 1) ? 128 : 256;
+    p.rows = !p.mfma || M <= 16 || s.d_h == 256 || s.dtype == XKV_F32 ? 16 : M <= 64 || s.d_h != 128 ? 32 : 256;
     p.round = p.mfma ? 128 : 64;
     int slots = !p.mfma ? 1024 : p.rows == 256 || s.d_h == 256 ? 256 : 512;
     // Several sequences, whose lengths may differ: two workgroups one after the other where each still has 4096 rows of the cache, so that those of

@@ -625,18 +625,19 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void cache8_mfma_kernel(Cache
 }
 
 // ------------------------------------------------------------------------------------------
-// The same for many rows, 128 channels: 32 rows a wavefront, WAVES of them to a workgroup, which share tiles of 64 rows of the cache.  Codes are
-// converted once for all of them, on their way from memory to LDS, K to bf16 and V to fp16, two tiles in turn: while one is multiplied, the next one's codes are
-// converted and those after it requested.  V^T is read by the transposing LDS read.
-// LDS: 16-byte piece p of row t of K sits at p ^ (t % 16), 32-byte piece u of V at (u + t) % 8, so that neither the fragment reads (16
+// The same for many rows, 128 channels: 32 rows a wavefront, eight of them to a workgroup, which share tiles of 64 rows of the cache.  Codes are
+// converted once for all of them, on their way from memory to LDS, K to bf16 and V to fp16.  V^T is read by the transposing LDS read.  The logits of a tile are
+// multiplied beside the exponentials of the one before, so that the matrix cores and the vector units work at once; the tile after it is
+// converted beside that one's second product, and the next one requested.  Two tiles of K and three of V are in LDS.
+// LDS: 16-byte piece p of row t of K sits at p ^ (t % 16), 32-byte piece u of V at u ^ (t % 8), so that neither the fragment reads (16
 // rows at a time, one piece each) nor the transposing reads (4 rows at a time, two pieces each) meet in a bank.
 // ------------------------------------------------------------------------------------------
-template <int CODE, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void cache8_rows_kernel(Cache8Args a, bool direct)
+template <int CODE>
+__global__ __launch_bounds__(512, 2) void cache8_rows_kernel(Cache8Args a, bool direct)
 {
-    constexpr int D = 128, RT = 2, TILE = 64, KV = TILE * 2 * D, PIECES = 8 / WAVES;  // bytes of a tile of K or V; pieces of 16 codes of a thread
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * KV];
-    __shared__ uint32_t sm_odd[3][2];  // of this tile, the next one and the one after it
+    constexpr int D = 128, RT = 2, WAVES = 8, TILE = 64, KV = TILE * 2 * D;  // bytes of a tile of K or V
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[5 * KV];  // K, K, V, V, V
+    __shared__ uint32_t sm_odd[4][2];  // of this tile, the next one, the one after it and one that is cleared
     const Unit8 u = unit8(a);
     const int lane = lane_id(), w = wave_id(), n16 = lane & 15, kk = lane >> 4, n_rep = a.H_q / a.H_kv, M = a.N * n_rep;
     if (!u.some && !direct) return;  // (the merge knows)
@@ -644,20 +645,21 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_rows_kernel(Cache8Args a
     const uint8_t *K = a.K8 + head * a.L * D, *V = a.V8 + head * a.L * D;
     const float *ks = a.k_scales + head * a.n_c, *vs = a.v_scales + head * a.n_c, c = a.scale * kLog2e;
 
-    u32x4_t kr[PIECES], vr[PIECES];
-    auto request = [&](int t) __attribute__((always_inline)) {
-        const uint8_t *kb = K + (size_t)t * D, *vb = V + (size_t)t * D;
-        const int last = u.t_end - 1 - t;
-#pragma unroll
-        for (int i = 0; i < PIECES; ++i) {
-            const int p = (int)threadIdx.x + 64 * WAVES * i;
-            uint32_t off = 16 * p;
-            if (last < TILE - 1) off = (p / 8 < last ? p / 8 : last) * D + 16 * (p % 8);  // (behind the last one: that one again)
-            kr[i] = *reinterpret_cast<const u32x4_t *>(kb + off);
-            vr[i] = *reinterpret_cast<const u32x4_t *>(vb + off);
+    // this thread's 16 codes of a tile: of row p_row, from channel 16 p on.  WHOLE: no row is behind the last one (those are the last one again)
+    const int p_row = (int)threadIdx.x / 8, p = (int)threadIdx.x % 8;
+    u32x4_t kr, vr;
+    auto request = [&](int t, auto whole) __attribute__((always_inline)) {
+        uint32_t off = 16 * threadIdx.x;
+        if constexpr (!decltype(whole)::value) {
+            const int last = u.t_end - 1 - t;
+            off = (p_row < last ? p_row : last) * D + 16 * p;
         }
+        kr = *reinterpret_cast<const u32x4_t *>(K + (size_t)t * D + off);
+        vr = *reinterpret_cast<const u32x4_t *>(V + (size_t)t * D + off);
     };
-    if (u.some) request(u.t_begin);
+    constexpr std::true_type whole{};
+    constexpr std::false_type any{};
+    if (u.some) request(u.t_begin, any);
 
     // Q^T operands: lane (row n16, kk), product s, position e: channel 32 s + 8 kk + e
     bf16x8_t Q[RT][4];
@@ -672,6 +674,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_rows_kernel(Cache8Args a
 #pragma unroll
         for (int s = 0; s < 4; ++s) Q[rt][s] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t *>(q + 32 * s + 8 * kk));
     }
+    if (((u.tile * WAVES + w) * RT) * 16 >= M) least = most = 0;  // (no rows)
     least = -wave_all(-least, MaxOp());  // rows of the cache that all of this wavefront's rows see, ..
     least = __builtin_amdgcn_readfirstlane(least < u.t_end ? least : u.t_end);
     most = __builtin_amdgcn_readfirstlane(wave_all(most, MaxOp()));  // .. any of them, ..
@@ -686,40 +689,32 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_rows_kernel(Cache8Args a
         all = -wave_all(-all, MaxOp());
         all = __builtin_amdgcn_readfirstlane(all < u.t_end ? all : u.t_end);
     }
-    if (threadIdx.x < 6) sm_odd[threadIdx.x / 2][threadIdx.x % 2] = 0u;
+    if (threadIdx.x < 8) sm_odd[threadIdx.x / 2][threadIdx.x % 2] = 0u;
     __syncthreads();
 
-    // Converted codes of a tile into LDS.  NaN among the values of a tile that rows see different tokens of become zeros, and their tokens are noted.
-    auto store = [&](int t, int buf, int note) __attribute__((always_inline)) {
+    // Converted codes of a tile into LDS.  NaN among the values of a tile that rows see different tokens of become zeros, and their tokens are noted
+    // (WHOLE: all see all).
+    unsigned char *const to_k = smem + 256 * p_row + 16 * ((2 * p) ^ (p_row & 15)), *const to_v = smem + 2 * KV + 256 * p_row + 32 * (p ^ (p_row & 7));
+    auto store = [&](int t, int kbuf, int vbuf, int note, auto whole) __attribute__((always_inline)) {
+        *reinterpret_cast<bf16x8_t *>(to_k + KV * kbuf) = codes8<CODE>(kr[0], kr[1]);
+        *reinterpret_cast<bf16x8_t *>(smem + ((uint32_t)(to_k - smem) ^ 16u) + KV * kbuf) = codes8<CODE>(kr[2], kr[3]);
+        if (CODE == XKV_E4M3 && !decltype(whole)::value && t + TILE > all) {
+            uint32_t odd = 0;
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i) {
-            const int p = (int)threadIdx.x + 64 * WAVES * i, row = p / 8, x = p % 8;
-            unsigned char *kt = smem + 2 * KV * buf + 256 * row, *vt = kt + KV + 32 * ((x + row) & 7);
-            *reinterpret_cast<bf16x8_t *>(kt + 16 * ((2 * x) ^ (row & 15))) = codes8<CODE>(kr[i][0], kr[i][1]);
-            *reinterpret_cast<bf16x8_t *>(kt + 16 * ((2 * x + 1) ^ (row & 15))) = codes8<CODE>(kr[i][2], kr[i][3]);
-            if (CODE == XKV_E4M3 && t + TILE > all) {
-                uint32_t odd = 0;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t nan = (((vr[i][e] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) >> 7;
-                    odd |= nan;
-                    vr[i][e] &= ~(nan * 255u);
-                }
-                if (odd) atomicOr(&sm_odd[note][row >> 5], 1u << (row & 31));
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t nan = (((vr[e] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) >> 7;
+                odd |= nan;
+                vr[e] &= ~(nan * 255u);
             }
-            *reinterpret_cast<f16x8_t *>(vt) = values8<CODE>(vr[i][0], vr[i][1]);
-            *reinterpret_cast<f16x8_t *>(vt + 16) = values8<CODE>(vr[i][2], vr[i][3]);
+            if (odd) atomicOr(&sm_odd[note][p_row >> 5], 1u << (p_row & 31));
         }
+        *reinterpret_cast<f16x8_t *>(to_v + KV * vbuf) = values8<CODE>(vr[0], vr[1]);
+        *reinterpret_cast<f16x8_t *>(to_v + KV * vbuf + 16) = values8<CODE>(vr[2], vr[3]);
     };
 
-    uint32_t kat[4], vat[8];
-#pragma unroll
-    for (int f = 0; f < 4; ++f) kat[f] = 256 * n16 + 16 * ((4 * f + kk) ^ n16);
-    {
-        const int rl = 4 * kk + (n16 >> 2);
-#pragma unroll
-        for (int db = 0; db < 8; ++db) vat[db] = KV + 256 * rl + 32 * ((db + rl) & 7) + 8 * (lane & 3);
-    }
+    // fragment f of K is at kat ^ (64 f), block of 16 channels db of V at vat ^ (32 db)
+    const int rl = 4 * kk + (n16 >> 2);
+    const uint32_t kat = 256 * n16 + 16 * (kk ^ n16), vat = 256 * rl + 32 * (rl & 7) + 8 * (lane & 3);
     f32x4_t O[RT][8];
     float m_run[RT], l_run[RT], inv = kFarUp;
 #pragma unroll
@@ -729,7 +724,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_rows_kernel(Cache8Args a
 #pragma unroll
         for (int j = 0; j < 8; ++j) O[rt][j] = f32x4_t(0.0f);
     }
-    float ksr[4], vsr[4];  // of tokens 16 h + 4 kk .. + 3
+    float ksr[4], vsr[4];  // of tokens 16 h + 4 kk .. + 3 of a tile
     auto request_scales = [&](int t) __attribute__((always_inline)) {
         const int last = u.t_end - 1 - t;
 #pragma unroll
@@ -746,21 +741,26 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_rows_kernel(Cache8Args a
         }
     };
 
-    auto tile = [&](int t, const unsigned char *lds, int note, auto mixed) __attribute__((always_inline)) {
+    f32x4_t S[RT][4];
+    auto logits = [&](int kbuf, int h) __attribute__((always_inline)) {  // of tokens 16 h .. + 15
+        const unsigned char *lds = smem + KV * kbuf + 4096 * h;
+        f32x4_t x[RT];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) x[rt] = f32x4_t(0.0f);
+#pragma unroll
+        for (int f = 0; f < 4; ++f) {
+            const bf16x8_t kf = *reinterpret_cast<const bf16x8_t *>(lds + (kat ^ (64u * f)));
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) x[rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, Q[rt][f], x[rt], 0, 0, 0);
+        }
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) S[rt][h] = x[rt];
+    };
+
+    // A tile, whose logits are there; those of the next one, if there is any, take their place.
+    auto tile = [&](int t, int kbuf, int vbuf, int note, bool next, auto mixed, auto beside) __attribute__((always_inline)) {
         constexpr bool MIXED = decltype(mixed)::value;
-        f32x4_t S[RT][4];
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-            for (int h = 0; h < 4; ++h) S[rt][h] = f32x4_t(0.0f);
-#pragma unroll
-        for (int f = 0; f < 4; ++f)
-#pragma unroll
-            for (int h = 0; h < 4; ++h) {
-                const bf16x8_t kf = *reinterpret_cast<const bf16x8_t *>(lds + kat[f] + 4096 * h);
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) S[rt][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, Q[rt][f], S[rt][h], 0, 0, 0);
-            }
+        const unsigned char *lds = smem + KV * (2 + vbuf);
         float kc[4];
 #pragma unroll
         for (int h = 0; h < 4; ++h) kc[h] = ksr[h] * c;
@@ -805,47 +805,57 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_rows_kernel(Cache8Args a
                 m_run[rt] = m_new;
             }
         }
-        float lv[4], rv[4];
-#pragma unroll
-        for (int h = 0; h < 4; ++h) {
-            const float v = vsr[h] * inv < kLeast ? kLeast : vsr[h] * inv;  // (NaN stays)
-            lv[h] = __builtin_amdgcn_logf(v);
-            rv[h] = __builtin_amdgcn_rcpf(v);
-        }
         f16x8_t P[RT][2];
+        auto weights = [&](int h) __attribute__((always_inline)) {  // of tokens 16 h .. + 15
+            const float v = vsr[h] * inv < kLeast ? kLeast : vsr[h] * inv;  // (NaN stays)
+            const float lv = __builtin_amdgcn_logf(v), rv = __builtin_amdgcn_rcpf(v);
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            const float less = m_run[rt] == -INFINITY ? 0.0f : m_run[rt];
+            for (int rt = 0; rt < RT; ++rt) {
+                const float add = lv - (m_run[rt] == -INFINITY ? 0.0f : m_run[rt]);
+                f32x4_t z;
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                f32x8_t z;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int h = 2 * k + e / 4;
-                    z[e] = __builtin_amdgcn_exp2f(MIXED ? S[rt][h][e % 4] + (lv[h] - less) : fmaf(S[rt][h][e % 4], kc[h], lv[h] - less));
-                    if (MIXED) z[e] = seen[rt] >> (16 * h + e % 4) & 1u ? z[e] : 0.0f;  // (a scale that is not seen may be NaN)
+                for (int e = 0; e < 4; ++e) {
+                    z[e] = __builtin_amdgcn_exp2f(MIXED ? S[rt][h][e] + add : fmaf(S[rt][h][e], kc[h], add));
+                    if (MIXED) z[e] = seen[rt] >> (16 * h + e) & 1u ? z[e] : 0.0f;  // (a scale that is not seen may be NaN)
                 }
+                const float by = MIXED && !(seen[rt] >> (16 * h) & 0xFu) ? 0.0f : rv;
+                l_run[rt] = fmaf((z[0] + z[1]) + (z[2] + z[3]), by, l_run[rt]);
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const float by = MIXED && !(seen[rt] >> (16 * (2 * k + i)) & 0xFu) ? 0.0f : rv[2 * k + i];
-                    l_run[rt] = fmaf((z[4 * i] + z[4 * i + 1]) + (z[4 * i + 2] + z[4 * i + 3]), by, l_run[rt]);
-                }
-                P[rt][k] = __builtin_convertvector(z, f16x8_t);
+                for (int e = 0; e < 4; ++e) P[rt][h / 2][4 * (h % 2) + e] = (_Float16)z[e];
             }
-        }
+        };
+        if (next) {
 #pragma unroll
-        for (int db = 0; db < 8; ++db)
+            for (int h = 0; h < 4; ++h) {
+                weights(h);
+                logits(kbuf ^ 1, h);
+            }
+        } else {
+#pragma unroll
+            for (int h = 0; h < 4; ++h) weights(h);
+        }
+        f16x8_t v[2][2];
+        auto values = [&](int db) __attribute__((always_inline)) {
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 // position e of lane (channel, kk): token 32 k + 16 (e / 4) + 4 kk + e % 4, as in P
-                const unsigned char *from = lds + vat[db] + 8192 * k;
+                const unsigned char *from = lds + (vat ^ (32u * db)) + 8192 * k;
                 const s16x4_t a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)from);
                 const s16x4_t a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(from + 4096));
-                const f16x8_t v = __builtin_bit_cast(f16x8_t, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) O[rt][db] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, P[rt][k], O[rt][db], 0, 0, 0);
+                v[db % 2][k] = __builtin_bit_cast(f16x8_t, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
             }
-        if (CODE == XKV_E4M3 && t + TILE > all) {  // NaN of noted tokens to the rows that see them
+        };
+        values(0);
+        beside();
+#pragma unroll
+        for (int db = 0; db < 8; ++db) {
+            if (db < 7) values(db + 1);
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) O[rt][db] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[db % 2][k], P[rt][k], O[rt][db], 0, 0, 0);
+        }
+        if (CODE == XKV_E4M3 && MIXED) {  // NaN of noted tokens to the rows that see them
             for (int i = 0; i < 2; ++i)
                 for (uint32_t bits = __builtin_amdgcn_readfirstlane(sm_odd[note][i]); bits; bits &= bits - 1) {
                     const int j = t + 32 * i + __builtin_ctz(bits);
@@ -863,28 +873,50 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_rows_kernel(Cache8Args a
     };
 
     if (u.some) {
-        store(u.t_begin, 0, 0);
-        if (u.t_begin + TILE < u.t_end) request(u.t_begin + TILE);
+        store(u.t_begin, 0, 0, 0, any);
+        if (u.t_begin + TILE < u.t_end) request(u.t_begin + TILE, any);
         request_scales(u.t_begin);
     }
     lds_barrier();
-    int buf = 0, note = 0;
-    for (int t = u.t_begin; t < u.t_end; t += TILE, buf ^= 1) {
-        const unsigned char *lds = smem + 2 * KV * buf;
-        const bool next = t + TILE < u.t_end;
-        const int then = note < 2 ? note + 1 : 0;
-        if (CODE == XKV_E4M3 && threadIdx.x < 2) sm_odd[then < 2 ? then + 1 : 0][threadIdx.x] = 0u;  // (read before the last barrier, written after the next)
-        if (next) {
-            store(t + TILE, buf ^ 1, then);
-            if (t + 2 * TILE < u.t_end) request(t + 2 * TILE);
-        }
-        if (t + TILE <= least)
-            tile(t, lds, note, std::false_type{});
-        else if (t < most)
-            tile(t, lds, note, std::true_type{});
-        if (next) request_scales(t + TILE);
+    if (u.t_begin + TILE < u.t_end) {
+        store(u.t_begin + TILE, 1, 1, 1, any);
+        if (u.t_begin + 2 * TILE < u.t_end) request(u.t_begin + 2 * TILE, any);
+    }
+    if (u.some) {
+#pragma unroll
+        for (int h = 0; h < 4; ++h) logits(0, h);
+    }
+    lds_barrier();
+    int kbuf = 0, vbuf = 0, note = 0, t = u.t_begin;
+    auto then = [&]() __attribute__((always_inline)) {
         lds_barrier();
-        note = then;
+        kbuf ^= 1;
+        vbuf = vbuf < 2 ? vbuf + 1 : 0;
+        note = (note + 1) & 3;
+    };
+    for (; t + 4 * TILE <= all; t += TILE) {  // all rows see all of this tile and the next three
+        tile(t, kbuf, vbuf, note, true, std::false_type{}, [&]() __attribute__((always_inline)) {
+            store(t + 2 * TILE, kbuf, vbuf > 0 ? vbuf - 1 : 2, 0, whole);
+            request(t + 3 * TILE, whole);
+        });
+        request_scales(t + TILE);
+        then();
+    }
+    for (; t < u.t_end; t += TILE) {
+        const bool next = t + TILE < u.t_end;
+        if (CODE == XKV_E4M3 && threadIdx.x < 2) sm_odd[(note + 3) & 3][threadIdx.x] = 0u;  // (read before the last barrier, written after the next)
+        auto beside = [&]() __attribute__((always_inline)) {
+            if (t + 2 * TILE < u.t_end) {
+                store(t + 2 * TILE, kbuf, vbuf > 0 ? vbuf - 1 : 2, (note + 2) & 3, any);
+                if (t + 3 * TILE < u.t_end) request(t + 3 * TILE, any);
+            }
+        };
+        if (t < most)
+            tile(t, kbuf, vbuf, note, next, std::true_type{}, beside);
+        else  // (nor do its rows see anything further)
+            beside();
+        if (next) request_scales(t + TILE);
+        then();
     }
 
     const float undo = __uint_as_float((254u << 23) - __float_as_uint(inv));
@@ -1037,7 +1069,7 @@ hipError_t launch_mfma(const Cache8Args &a, bool direct, hipStream_t st)
     if (a.rows == 16) return once ? launch(cache8_mfma_kernel<T, CODE, D, 1, true>) : launch(cache8_mfma_kernel<T, CODE, D, 1, false>);
     if constexpr (sizeof(T) == 2 && D < 256) {
         if (a.rows == 32) return once ? launch(cache8_mfma_kernel<T, CODE, D, 2, true>) : launch(cache8_mfma_kernel<T, CODE, D, 2, false>);
-        if constexpr (D == 128) return a.rows == 128 ? launch(cache8_rows_kernel<CODE, 4>, 256) : launch(cache8_rows_kernel<CODE, 8>, 512);
+        if constexpr (D == 128) return launch(cache8_rows_kernel<CODE>, 512);
     }
     return hipErrorInvalidValue;
 }
