@@ -40,8 +40,10 @@ __device__ __forceinline__ int cache_rows(const Cache8Args &a, int seq)
 {
     if (!a.visible) return a.L;
     int n = 0;
-#pragma unroll 4
-    for (int i = 0; i < a.N; ++i) n = MaxOp()(n, a.visible[(size_t)seq * a.N + i]);
+    for (int i = 0; i < a.N; i += 8) {  // (at most 32 of them)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) n = MaxOp()(n, a.visible[(size_t)seq * a.N + (i + j < a.N ? i + j : i)]);
+    }
     return n < a.L ? n : a.L;
 }
 __device__ __forceinline__ int cache_tokens(const Cache8Args &, CacheMode, int n) { return n; }

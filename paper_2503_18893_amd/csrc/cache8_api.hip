@@ -62,23 +62,24 @@ xkv_status plan_cache8(const xkv_shape &s, int N, Cache8Plan &p)
     const long long M = (long long)N * p.n_rep;
     p.mfma = s.d_h == 64 || s.d_h == 128 || s.d_h == 256;
     // Rows of a workgroup.  Two workgroups of the matrix-core kernels to a compute unit, one of 256 rows or channels; four of the general one.
-    // (65 rows and more of 128 channels: 256 that share tiles, or 128 where that leaves fewer of them empty: 256 queries of 7 heads after 131072
-    // rows, 1792 rows a KV head, 631 us by 256, 667 by 128, 783 by 32 that do not share.)
-    p.rows = !p.mfma || M <= 16 || s.d_h == 256 || s.dtype == XKV_F32 ? 16 : M <= 64 || s.d_h != 128 ? 32 : 256;
+    // (More than 128 rows of 128 channels: 256 that share tiles.  Microseconds by 32 / by 256, 8 KV heads: 64 rows after 32768 rows of the cache 29 / 47, 96
+    // 41 / 50, 128 42 / 52, 192 73 / 61; four sequences of up to 65536 rows, 72 rows 132 / 197, 128 171 / 201, 192 243 / 208.)
+    p.rows = !p.mfma || M <= 16 || s.d_h == 256 || s.dtype == XKV_F32 ? 16 : M <= 128 || s.d_h != 128 ? 32 : 256;
     p.round = p.mfma ? 128 : 64;
     int slots = !p.mfma ? 1024 : p.rows == 256 || s.d_h == 256 ? 256 : 512;
     // Several sequences, whose lengths may differ: two workgroups one after the other where each still has 4096 rows of the cache, so that those of
     // short sequences fill in.  16 sequences of up to 65536 rows, 8 KV heads: 200 us with one, 195 with two, 197 with three.
     if (p.mfma && M <= 64 && batch > 1 && batch * s.H_kv * s.L >= 2LL * slots * 4096) slots *= 2;
     const int row_tiles = ceil_div(M, p.rows), longest = ceil_div(s.L, p.round);
-    // Few rows of queries: streams, cut by the lengths.  A cache of up to 512 rows is one part, whose result needs no merge: 4 heads after 512 rows of
+    // Up to 256 rows, of up to 32 queries, whose lengths every workgroup looks at: parts cut by the lengths.  A cache of up to 512 rows is one part, whose result needs no merge: 4 heads after 512 rows of
     // 128 channels in bf16 8.0 us, cut 9.2 (16 sequences with 32 heads 9.9, cut 13.7); after 1024 rows 11.4 and 9.4 (15.5 and 17.2).
-    p.by_length = M <= 64 && s.L > 512;
+    const bool one = M <= 64 && s.L <= 512;
+    p.by_length = !one && M <= 256 && N <= 32;
     if (p.by_length) {
         const long long all = batch * longest;
         p.parts = clampi(ceil_div(slots, s.H_kv * row_tiles), (int)batch, (int)(all < (1 << 30) ? all : 1 << 30));
         if (p.parts > batch + kMaxCacheParts - 1) p.parts = (int)batch + kMaxCacheParts - 1;
-    } else if (M <= 64) {
+    } else if (one) {
         p.parts = 1;
     } else {
         // Parts of a row tile: as few as fill the compute units well.  A part costs about what 4 rounds take beside its own.

@@ -21,6 +21,11 @@ struct Unit8 {
     int seq, g, tile, part, t_begin, t_end;
     bool some;
 };
+__device__ __forceinline__ Unit8 same_in_all_lanes(const Unit8 &u)
+{
+    auto same = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+    return Unit8{same(u.seq), same(u.g), same(u.tile), same(u.part), same(u.t_begin), same(u.t_end), same(u.some) != 0};
+}
 
 // The queries whose rows (query, head) a tile holds.
 __device__ __forceinline__ void tile_queries(const Cache8Args &a, int tile, int &first, int &last)
@@ -285,6 +290,12 @@ template <int CODE> __device__ __forceinline__ void codes_by_channel(const uint3
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) x[j] = __builtin_bit_cast(f16x8_t, y[j]);
+}
+
+// 4 B per lane from global memory into LDS at lds_base + lane * 4 (lds_base is wave-uniform); see copy16_global_to_lds.
+__device__ __forceinline__ void copy4_to_lds(const void *gptr, uint32_t lds_base)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(lds_base), "v"(gptr) : "memory", "m0");
 }
 
 // Words of a row of the cache; ONCE: past the caches, where nobody else reads them.
@@ -625,41 +636,57 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void cache8_mfma_kernel(Cache
 }
 
 // ------------------------------------------------------------------------------------------
-// The same for many rows, 128 channels: 32 rows a wavefront, eight of them to a workgroup, which share tiles of 64 rows of the cache.  Codes are
-// converted once for all of them, on their way from memory to LDS, K to bf16 and V to fp16.  V^T is read by the transposing LDS read.  The logits of a tile are
-// multiplied beside the exponentials of the one before, so that the matrix cores and the vector units work at once; the tile after it is
-// converted beside that one's second product, and the next one requested.  Two tiles of K and three of V are in LDS.
+// The same for many rows, 128 channels: 32 rows a wavefront, eight of them to a workgroup, which share tiles of 64 rows of the cache.  Codes go from
+// memory to LDS as they are, four tiles ahead, and are converted there once for all wavefronts, K to bf16 and V to fp16; V^T is read by
+// the transposing LDS read.  The logits of a tile are multiplied beside the exponentials of the one before, so that the matrix cores and the
+// vector units work at once; the tile after it is converted beside that one's second product.  Nothing in the loop waits for a load of
+// its own: scales take the way of the codes (a load into a register would first have to wait for all tiles that are under way).
+// 256 queries of 7 heads after 131072 rows (1792 rows a KV head): 506 us, 0.95 PFLOP/s of 4 d flops a logit (a 8192^3 library product 1.2); logits and
+// exponentials one after the other 631; codes and scales through registers 525; by 32 rows that share nothing 783.  With few rows a
+// tile still takes 2.4 us, the latency of its steps: the streams are faster up to 128 rows.
 // LDS: 16-byte piece p of row t of K sits at p ^ (t % 16), 32-byte piece u of V at u ^ (t % 8), so that neither the fragment reads (16
 // rows at a time, one piece each) nor the transposing reads (4 rows at a time, two pieces each) meet in a bank.
 // ------------------------------------------------------------------------------------------
 template <int CODE>
 __global__ __launch_bounds__(512, 2) void cache8_rows_kernel(Cache8Args a, bool direct)
 {
-    constexpr int D = 128, RT = 2, WAVES = 8, TILE = 64, KV = TILE * 2 * D;  // bytes of a tile of K or V
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[5 * KV];  // K, K, V, V, V
+    constexpr int D = 128, RT = 2, WAVES = 8, TILE = 64, KV = TILE * 2 * D, AHEAD = 4;  // bytes of a tile of K or V; tiles of codes under way
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[(5 + AHEAD) * KV];  // K, K, V, V, V, and codes of tiles that are under way (K and V)
+    __shared__ float sm_scale[8][64];  // of tile i in i % 8: of K, four tokens each, of V, and both again
     __shared__ uint32_t sm_odd[4][2];  // of this tile, the next one, the one after it and one that is cleared
-    const Unit8 u = unit8(a);
+    const Unit8 u = same_in_all_lanes(unit8(a));
     const int lane = lane_id(), w = wave_id(), n16 = lane & 15, kk = lane >> 4, n_rep = a.H_q / a.H_kv, M = a.N * n_rep;
     if (!u.some && !direct) return;  // (the merge knows)
     const size_t head = (size_t)u.seq * a.H_kv + u.g;
     const uint8_t *K = a.K8 + head * a.L * D, *V = a.V8 + head * a.L * D;
     const float *ks = a.k_scales + head * a.n_c, *vs = a.v_scales + head * a.n_c, c = a.scale * kLog2e;
 
-    // this thread's 16 codes of a tile: of row p_row, from channel 16 p on.  WHOLE: no row is behind the last one (those are the last one again)
+    // This thread's 16 codes of a tile, of row p_row, from channel 16 p on; they go straight to LDS, where only this wavefront reads them.
+    // WHOLE: no row is behind the last one (those are the last one again).
     const int p_row = (int)threadIdx.x / 8, p = (int)threadIdx.x % 8;
-    u32x4_t kr, vr;
-    auto request = [&](int t, auto whole) __attribute__((always_inline)) {
+    const uint32_t scale0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)&sm_scale[0][0];
+    const uint32_t raw0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem + 5 * KV + 1024 * w;
+    const float *const scales = lane & 16 ? vs : ks;
+    const int quad = 4 * (lane & 15);
+    auto request = [&](int t, int i, auto whole) __attribute__((always_inline)) {  // tile i
+        const int slot = i % AHEAD;
+        if (w == i % 8) {  // (a load more than the others have makes its waits longer)
+            const int last = u.t_end - 1 - t;
+            copy4_to_lds(scales + ((t + (decltype(whole)::value || quad < last ? quad : last)) >> a.shift), scale0 + 256 * (i % 8));
+        }
         uint32_t off = 16 * threadIdx.x;
         if constexpr (!decltype(whole)::value) {
             const int last = u.t_end - 1 - t;
             off = (p_row < last ? p_row : last) * D + 16 * p;
         }
-        kr = *reinterpret_cast<const u32x4_t *>(K + (size_t)t * D + off);
-        vr = *reinterpret_cast<const u32x4_t *>(V + (size_t)t * D + off);
+        copy16_to_lds(K + (size_t)t * D, off, raw0 + KV * slot);
+        copy16_to_lds(V + (size_t)t * D, off, raw0 + KV * slot + KV / 2);
     };
     constexpr std::true_type whole{};
     constexpr std::false_type any{};
-    if (u.some) request(u.t_begin, any);
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+        if (u.t_begin + i * TILE < u.t_end) request(u.t_begin + i * TILE, i, any);
 
     // Q^T operands: lane (row n16, kk), product s, position e: channel 32 s + 8 kk + e
     bf16x8_t Q[RT][4];
@@ -695,7 +722,16 @@ __global__ __launch_bounds__(512, 2) void cache8_rows_kernel(Cache8Args a, bool 
     // Converted codes of a tile into LDS.  NaN among the values of a tile that rows see different tokens of become zeros, and their tokens are noted
     // (WHOLE: all see all).
     unsigned char *const to_k = smem + 256 * p_row + 16 * ((2 * p) ^ (p_row & 15)), *const to_v = smem + 2 * KV + 256 * p_row + 32 * (p ^ (p_row & 7));
-    auto store = [&](int t, int kbuf, int vbuf, int note, auto whole) __attribute__((always_inline)) {
+    auto store = [&](int t, int i, int kbuf, int vbuf, auto whole) __attribute__((always_inline)) {
+        // (requests are answered in order: those of the tiles behind this one may be under way, others in between make the wait longer)
+        if (decltype(whole)::value || t + (AHEAD - 1) * TILE < u.t_end)
+            XKV_WAIT_VMCNT(2 * (AHEAD - 1));
+        else
+            XKV_WAIT_VMCNT(0);
+        asm volatile("" : : : "memory");
+        const unsigned char *raw = smem + 5 * KV + KV * (i % AHEAD) + 16 * threadIdx.x;
+        const u32x4_t kr = *reinterpret_cast<const u32x4_t *>(raw);
+        u32x4_t vr = *reinterpret_cast<const u32x4_t *>(raw + KV / 2);
         *reinterpret_cast<bf16x8_t *>(to_k + KV * kbuf) = codes8<CODE>(kr[0], kr[1]);
         *reinterpret_cast<bf16x8_t *>(smem + ((uint32_t)(to_k - smem) ^ 16u) + KV * kbuf) = codes8<CODE>(kr[2], kr[3]);
         if (CODE == XKV_E4M3 && !decltype(whole)::value && t + TILE > all) {
@@ -706,7 +742,7 @@ __global__ __launch_bounds__(512, 2) void cache8_rows_kernel(Cache8Args a, bool 
                 odd |= nan;
                 vr[e] &= ~(nan * 255u);
             }
-            if (odd) atomicOr(&sm_odd[note][p_row >> 5], 1u << (p_row & 31));
+            if (odd) atomicOr(&sm_odd[i % 4][p_row >> 5], 1u << (p_row & 31));
         }
         *reinterpret_cast<f16x8_t *>(to_v + KV * vbuf) = values8<CODE>(vr[0], vr[1]);
         *reinterpret_cast<f16x8_t *>(to_v + KV * vbuf + 16) = values8<CODE>(vr[2], vr[3]);
@@ -725,65 +761,62 @@ __global__ __launch_bounds__(512, 2) void cache8_rows_kernel(Cache8Args a, bool 
         for (int j = 0; j < 8; ++j) O[rt][j] = f32x4_t(0.0f);
     }
     float ksr[4], vsr[4];  // of tokens 16 h + 4 kk .. + 3 of a tile
-    auto request_scales = [&](int t) __attribute__((always_inline)) {
-        const int last = u.t_end - 1 - t;
+    auto scales_of = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
-            if (a.shift >= 4) {  // one for 16 tokens: the same in all lanes
-                const int at = (t + (16 * h < last ? 16 * h : last)) >> a.shift;
-                ksr[h] = ks[at];
-                vsr[h] = vs[at];
-            } else {
-                const int quad = 16 * h + 4 * kk, at = (t + (quad < last ? quad : last)) >> a.shift;
-                ksr[h] = ks[at];
-                vsr[h] = vs[at];
-            }
+            ksr[h] = sm_scale[i % 8][4 * h + kk];
+            vsr[h] = sm_scale[i % 8][16 + 4 * h + kk];
         }
     };
 
     f32x4_t S[RT][4];
-    auto logits = [&](int kbuf, int h) __attribute__((always_inline)) {  // of tokens 16 h .. + 15
+    // Logits of tokens 16 h .. + 15.  What is read from LDS is requested a step before it is used, and stays before that step's arithmetic.
+    bf16x8_t kf[2][4];
+    auto keys = [&](int kbuf, int h) __attribute__((always_inline)) {
         const unsigned char *lds = smem + KV * kbuf + 4096 * h;
+#pragma unroll
+        for (int f = 0; f < 4; ++f) kf[h % 2][f] = *reinterpret_cast<const bf16x8_t *>(lds + (kat ^ (64u * f)));
+    };
+    auto logits = [&](int h) __attribute__((always_inline)) {
         f32x4_t x[RT];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) x[rt] = f32x4_t(0.0f);
 #pragma unroll
-        for (int f = 0; f < 4; ++f) {
-            const bf16x8_t kf = *reinterpret_cast<const bf16x8_t *>(lds + (kat ^ (64u * f)));
+        for (int f = 0; f < 4; ++f)
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) x[rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, Q[rt][f], x[rt], 0, 0, 0);
-        }
+            for (int rt = 0; rt < RT; ++rt) x[rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[h % 2][f], Q[rt][f], x[rt], 0, 0, 0);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) S[rt][h] = x[rt];
     };
 
     // A tile, whose logits are there; those of the next one, if there is any, take their place.
-    auto tile = [&](int t, int kbuf, int vbuf, int note, bool next, auto mixed, auto beside) __attribute__((always_inline)) {
+    auto tile = [&](int t, int i, int kbuf, int vbuf, bool next, auto mixed, auto beside) __attribute__((always_inline)) {
         constexpr bool MIXED = decltype(mixed)::value;
         const unsigned char *lds = smem + KV * (2 + vbuf);
-        float kc[4];
+        if (next) keys(kbuf ^ 1, 0);
+        float kc[4], largest = vsr[0];
 #pragma unroll
-        for (int h = 0; h < 4; ++h) kc[h] = ksr[h] * c;
+        for (int h = 0; h < 4; ++h) {
+            kc[h] = ksr[h] * c;
+            largest = fmaxf(largest, vsr[h]);
+        }
         uint64_t seen[RT];
-        float top[RT], largest = fmaxf(fmaxf(vsr[0], vsr[1]), fmaxf(vsr[2], vsr[3]));
+        float top[RT];
         bool raise = !(largest * inv <= 128.0f);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             if (MIXED) {
-                const int left = sees[rt] < u.t_end ? sees[rt] - t : u.t_end - t;
+                const int left = (sees[rt] < u.t_end ? sees[rt] : u.t_end) - t;
                 seen[rt] = left >= 64 ? ~0ull : left > 0 ? (1ull << left) - 1ull : 0ull;
                 seen[rt] >>= 4 * kk;
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
                     S[rt][e / 4][e % 4] = seen[rt] >> (16 * (e / 4) + e % 4) & 1u ? S[rt][e / 4][e % 4] * kc[e / 4] : -INFINITY;
             }
-            float lo, hi, x[4];
+            float lo, hi, x = -INFINITY;
 #pragma unroll
-            for (int h = 0; h < 4; ++h) {
-                x[h] = largest4(S[rt][h]);
-                if (!MIXED) x[h] *= kc[h];  // (scales are not negative)
-            }
-            quarters(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), lo, hi);
+            for (int h = 0; h < 4; ++h) x = fmaxf(x, MIXED ? largest4(S[rt][h]) : largest4(S[rt][h]) * kc[h]);  // (scales are not negative)
+            quarters(x, lo, hi);
             halves(fmaxf(lo, hi), lo, hi);
             top[rt] = fmaxf(lo, hi);
             raise |= !(top[rt] - m_run[rt] <= 8.0f);
@@ -827,14 +860,16 @@ __global__ __launch_bounds__(512, 2) void cache8_rows_kernel(Cache8Args a, bool 
         if (next) {
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
+                if (h < 3) keys(kbuf ^ 1, h + 1);
+                __builtin_amdgcn_sched_barrier(0);
                 weights(h);
-                logits(kbuf ^ 1, h);
+                logits(h);
             }
         } else {
 #pragma unroll
             for (int h = 0; h < 4; ++h) weights(h);
         }
-        f16x8_t v[2][2];
+        f16x8_t v[3][2];
         auto values = [&](int db) __attribute__((always_inline)) {
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
@@ -842,23 +877,25 @@ __global__ __launch_bounds__(512, 2) void cache8_rows_kernel(Cache8Args a, bool 
                 const unsigned char *from = lds + (vat ^ (32u * db)) + 8192 * k;
                 const s16x4_t a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)from);
                 const s16x4_t a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(from + 4096));
-                v[db % 2][k] = __builtin_bit_cast(f16x8_t, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
+                v[db % 3][k] = __builtin_bit_cast(f16x8_t, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
             }
         };
         values(0);
+        values(1);
         beside();
 #pragma unroll
         for (int db = 0; db < 8; ++db) {
-            if (db < 7) values(db + 1);
+            if (db < 6) values(db + 2);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int k = 0; k < 2; ++k)
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) O[rt][db] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[db % 2][k], P[rt][k], O[rt][db], 0, 0, 0);
+                for (int rt = 0; rt < RT; ++rt) O[rt][db] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[db % 3][k], P[rt][k], O[rt][db], 0, 0, 0);
         }
         if (CODE == XKV_E4M3 && MIXED) {  // NaN of noted tokens to the rows that see them
-            for (int i = 0; i < 2; ++i)
-                for (uint32_t bits = __builtin_amdgcn_readfirstlane(sm_odd[note][i]); bits; bits &= bits - 1) {
-                    const int j = t + 32 * i + __builtin_ctz(bits);
+            for (int x = 0; x < 2; ++x)
+                for (uint32_t bits = __builtin_amdgcn_readfirstlane(sm_odd[i % 4][x]); bits; bits &= bits - 1) {
+                    const int j = t + 32 * x + __builtin_ctz(bits);
                     const uint8_t *v = V + (size_t)(j < u.t_end ? j : u.t_end - 1) * D + 4 * kk;
 #pragma unroll
                     for (int db = 0; db < 8; ++db)
@@ -872,60 +909,67 @@ __global__ __launch_bounds__(512, 2) void cache8_rows_kernel(Cache8Args a, bool 
         }
     };
 
-    if (u.some) {
-        store(u.t_begin, 0, 0, 0, any);
-        if (u.t_begin + TILE < u.t_end) request(u.t_begin + TILE, any);
-        request_scales(u.t_begin);
-    }
+    // Tile i of this part: its codes in i % AHEAD, converted ones in i % 2 (K) and i % 3 (V), scales in i % 8, notes in i % 4.
+    auto convert = [&](int t, int i, int kbuf, int vbuf) __attribute__((always_inline)) {
+        if (t >= u.t_end) return;
+        store(t, i, kbuf, vbuf, any);
+        wait_lds();
+        if (t + AHEAD * TILE < u.t_end) request(t + AHEAD * TILE, i + AHEAD, any);
+    };
+    convert(u.t_begin, 0, 0, 0);
     lds_barrier();
-    if (u.t_begin + TILE < u.t_end) {
-        store(u.t_begin + TILE, 1, 1, 1, any);
-        if (u.t_begin + 2 * TILE < u.t_end) request(u.t_begin + 2 * TILE, any);
-    }
+    convert(u.t_begin + TILE, 1, 1, 1);
     if (u.some) {
+        scales_of(0);
 #pragma unroll
-        for (int h = 0; h < 4; ++h) logits(0, h);
+        for (int h = 0; h < 4; ++h) {
+            keys(0, h);
+            logits(h);
+        }
     }
     lds_barrier();
-    int kbuf = 0, vbuf = 0, note = 0, t = u.t_begin;
+    int kbuf = 0, vbuf = 0, i = 0, t = u.t_begin;
     auto then = [&]() __attribute__((always_inline)) {
         lds_barrier();
         kbuf ^= 1;
         vbuf = vbuf < 2 ? vbuf + 1 : 0;
-        note = (note + 1) & 3;
+        ++i;
     };
-    for (; t + 4 * TILE <= all; t += TILE) {  // all rows see all of this tile and the next three
-        tile(t, kbuf, vbuf, note, true, std::false_type{}, [&]() __attribute__((always_inline)) {
-            store(t + 2 * TILE, kbuf, vbuf > 0 ? vbuf - 1 : 2, 0, whole);
-            request(t + 3 * TILE, whole);
+    for (; t + (AHEAD + 3) * TILE <= all; t += TILE) {  // all rows see all of the tiles that are dealt with here
+        tile(t, i, kbuf, vbuf, true, std::false_type{}, [&]() __attribute__((always_inline)) {
+            scales_of(i + 1);
+            store(t + 2 * TILE, i + 2, kbuf, vbuf > 0 ? vbuf - 1 : 2, whole);
+            wait_lds();
+            request(t + (2 + AHEAD) * TILE, i + 2 + AHEAD, whole);
         });
-        request_scales(t + TILE);
         then();
     }
     for (; t < u.t_end; t += TILE) {
-        const bool next = t + TILE < u.t_end;
-        if (CODE == XKV_E4M3 && threadIdx.x < 2) sm_odd[(note + 3) & 3][threadIdx.x] = 0u;  // (read before the last barrier, written after the next)
+        if (CODE == XKV_E4M3 && threadIdx.x < 2) sm_odd[(i + 3) % 4][threadIdx.x] = 0u;  // (read before the last barrier, written after the next)
         auto beside = [&]() __attribute__((always_inline)) {
-            if (t + 2 * TILE < u.t_end) {
-                store(t + 2 * TILE, kbuf, vbuf > 0 ? vbuf - 1 : 2, (note + 2) & 3, any);
-                if (t + 3 * TILE < u.t_end) request(t + 3 * TILE, any);
-            }
+            scales_of(i + 1);
+            convert(t + 2 * TILE, i + 2, kbuf, vbuf > 0 ? vbuf - 1 : 2);
         };
         if (t < most)
-            tile(t, kbuf, vbuf, note, next, std::true_type{}, beside);
+            tile(t, i, kbuf, vbuf, t + TILE < u.t_end, std::true_type{}, beside);
         else  // (nor do its rows see anything further)
             beside();
-        if (next) request_scales(t + TILE);
         then();
     }
 
     const float undo = __uint_as_float((254u << 23) - __float_as_uint(inv));
+    float den[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         float lo, hi;
         quarters(l_run[rt], lo, hi);
         halves(lo + hi, lo, hi);
-        const float den = lo + hi;
+        den[rt] = lo + hi;
+#pragma unroll
+        for (int db = 0; db < 8; ++db) O[rt][db] *= undo;
+    }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
         const int m = ((u.tile * WAVES + w) * RT + rt) * 16 + n16;
         if (m >= M) continue;
         const size_t row = ((size_t)(direct ? u.seq : u.part) * a.N + m / n_rep) * a.H_q + u.g * n_rep + m % n_rep;
@@ -935,15 +979,15 @@ __global__ __launch_bounds__(512, 2) void cache8_rows_kernel(Cache8Args a, bool 
                 typedef __attribute__((ext_vector_type(4))) uint16_t u16x4_t;
                 u16x4_t x;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = result<bf16_t>(sees[rt] == 0 ? 0.0f : undo * O[rt][db][e] / den);
+                for (int e = 0; e < 4; ++e) x[e] = result<bf16_t>(sees[rt] == 0 ? 0.0f : O[rt][db][e] / den[rt]);
                 *reinterpret_cast<u16x4_t *>((bf16_t *)a.out + row * D + 16 * db + 4 * kk) = x;
             } else {
-                *reinterpret_cast<f32x4_t *>(a.part_o + row * D + 16 * db + 4 * kk) = undo * O[rt][db];
+                *reinterpret_cast<f32x4_t *>(a.part_o + row * D + 16 * db + 4 * kk) = O[rt][db];
             }
         }
         if (!direct && kk == 0) {
             a.part_ml[2 * row] = m_run[rt];
-            a.part_ml[2 * row + 1] = den;
+            a.part_ml[2 * row + 1] = den[rt];
         }
     }
 }
