@@ -35,18 +35,21 @@ __device__ __forceinline__ int visible8(const Cache8Args &a, int seq, int i)
     return n < 0 ? 0 : n < a.L ? n : a.L;
 }
 
-// Rows that any query of a sequence sees, for cache_unit.
-__device__ __forceinline__ int cache_rows(const Cache8Args &a, int seq)
+// What cache_unit needs to cut by length: `rows` (LDS, [batch]) are the rows that any query of a sequence sees; NULL: one query of each, or all.
+struct Cache8Cut {
+    const int *rows;
+    const int32_t *visible;
+    int32_t *table;
+    int L, H_kv, batch, round, parts;
+};
+__device__ __forceinline__ int cache_rows(const Cache8Cut &a, int seq)
 {
-    if (!a.visible) return a.L;
-    int n = 0;
-    for (int i = 0; i < a.N; i += 8) {  // (at most 32 of them)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) n = MaxOp()(n, a.visible[(size_t)seq * a.N + (i + j < a.N ? i + j : i)]);
-    }
-    return n < a.L ? n : a.L;
+    const int n = a.rows ? a.rows[seq] : a.visible ? a.visible[seq] : a.L;
+    return n < 0 ? 0 : n < a.L ? n : a.L;
 }
-__device__ __forceinline__ int cache_tokens(const Cache8Args &, CacheMode, int n) { return n; }
+__device__ __forceinline__ int cache_tokens(const Cache8Cut &, CacheMode, int n) { return n; }
+
+constexpr int kCutBatch = 1024, kCutQueries = 16384;  // sequences, and queries of all of them, up to which parts are cut by length
 
 struct Cache8Plan {
     int n_rep, n_c, shift;

@@ -66,28 +66,30 @@ xkv_status plan_cache8(const xkv_shape &s, int N, Cache8Plan &p)
     // 41 / 50, 128 42 / 52, 192 73 / 61; four sequences of up to 65536 rows, 72 rows 132 / 197, 128 171 / 201, 192 243 / 208.)
     p.rows = !p.mfma || M <= 16 || s.d_h == 256 || s.dtype == XKV_F32 ? 16 : M <= 128 || s.d_h != 128 ? 32 : 256;
     p.round = p.mfma ? 128 : 64;
-    int slots = !p.mfma ? 1024 : p.rows == 256 || s.d_h == 256 ? 256 : 512;
-    // Several sequences, whose lengths may differ: two workgroups one after the other where each still has 4096 rows of the cache, so that those of
-    // short sequences fill in.  16 sequences of up to 65536 rows, 8 KV heads: 200 us with one, 195 with two, 197 with three.
-    if (p.mfma && M <= 64 && batch > 1 && batch * s.H_kv * s.L >= 2LL * slots * 4096) slots *= 2;
+    const int slots = !p.mfma ? 1024 : p.rows == 256 || s.d_h == 256 ? 256 : 512;
     const int row_tiles = ceil_div(M, p.rows), longest = ceil_div(s.L, p.round);
-    // Up to 256 rows, of up to 32 queries, whose lengths every workgroup looks at: parts cut by the lengths.  A cache of up to 512 rows is one part, whose result needs no merge: 4 heads after 512 rows of
-    // 128 channels in bf16 8.0 us, cut 9.2 (16 sequences with 32 heads 9.9, cut 13.7); after 1024 rows 11.4 and 9.4 (15.5 and 17.2).
-    const bool one = M <= 64 && s.L <= 512;
-    p.by_length = !one && M <= 256 && N <= 32;
-    if (p.by_length) {
-        const long long all = batch * longest;
-        p.parts = clampi(ceil_div(slots, s.H_kv * row_tiles), (int)batch, (int)(all < (1 << 30) ? all : 1 << 30));
-        if (p.parts > batch + kMaxCacheParts - 1) p.parts = (int)batch + kMaxCacheParts - 1;
-    } else if (one) {
+    const long long units = (long long)s.H_kv * row_tiles;  // workgroups of a part
+    // A cache of up to 512 rows and few queries, or many sequences: one part, whose result needs no merge.  4 heads after 512 rows of 128 channels in bf16 8.0 us, cut 9.2 (16
+    // sequences with 32 heads 9.9, cut 13.7); after 1024 rows 11.4 and 9.4 (15.5 and 17.2).
+    const bool one = s.L <= 512 && (M <= 64 || units * batch >= 64);
+    // Otherwise, where sequences alone do not fill the compute units, parts are cut by the lengths, for which every workgroup looks at those of all
+    // queries (unless they are very many).  Four sequences of up to 65536 rows, 1024 rows of queries, 128 tiles of them 777 us, tiles cut in
+    // equal parts 1094; 16 of up to 4096, 512 tiles 243, not cut 175.
+    p.by_length = !one && units * batch < slots && batch <= kCutBatch && (N == 1 || batch * N <= kCutQueries);
+    if (one) {
         p.parts = 1;
+    } else if (batch > 1 && p.by_length) {
+        // Several sequences, whose lengths may differ: two workgroups one after the other where each still has 8192 rows of the cache, so that those of
+        // short sequences fill in.  16 sequences of up to 65536 rows, 8 KV heads: 200 us with one, 195 with two, 197 with three.
+        const int rounds = p.mfma && row_tiles == 1 && batch * units * s.L >= 2LL * slots * 8192 ? 2 : 1;
+        const long long all = batch * longest, most = all < batch + kMaxCacheParts - 1 ? all : batch + kMaxCacheParts - 1;
+        p.parts = clampi((int)(rounds * slots / units), (int)batch, (int)most);
     } else {
-        // Parts of a row tile: as few as fill the compute units well.  A part costs about what 4 rounds take beside its own.
-        const long long units = (long long)s.H_kv * row_tiles * batch;
+        // As few as fill the compute units well.  A part costs about what 4 rounds take beside its own.
         long long best = 0;
         p.parts = 1;
-        for (int parts = 1; parts <= 64 && parts <= longest; ++parts) {
-            const long long time = ((units * parts + slots - 1) / slots) * (ceil_div(longest, parts) + 4);
+        for (int parts = 1; parts <= kMaxCacheParts && parts <= longest; ++parts) {
+            const long long time = ((units * batch * parts + slots - 1) / slots) * (ceil_div(longest, parts) + 4);
             if (parts == 1 || time < best) best = time, p.parts = parts;
         }
     }

@@ -19,7 +19,7 @@ constexpr float kLog2e = 1.44269504088896340736f;
 // What a workgroup takes: query rows tile * rows .. of KV head g of sequence seq, rows t_begin .. t_end - 1 of the cache.
 struct Unit8 {
     int seq, g, tile, part, t_begin, t_end;
-    bool some;
+    bool some;  // whether the merge reads this part (it may have no rows all the same)
 };
 __device__ __forceinline__ Unit8 same_in_all_lanes(const Unit8 &u)
 {
@@ -53,8 +53,20 @@ __device__ __forceinline__ Unit8 unit8(const Cache8Args &a)
     Unit8 u{};
     const int tiles = ceil_div_dev(a.N * (a.H_q / a.H_kv), a.rows);
     if (a.by_length) {
-        const CacheUnit c = cache_unit(a, CacheMode::weights, tiles);
-        u.seq = c.seq, u.g = c.g, u.tile = c.tile, u.part = c.part, u.t_begin = c.t_begin, u.t_end = c.t_end, u.some = c.some;
+        __shared__ int sm_rows[kCutBatch];
+        const bool many = a.N > 1 && a.visible;
+        if (many) {  // every workgroup looks at all of them
+            for (int i = (int)threadIdx.x; i < a.batch; i += (int)blockDim.x) sm_rows[i] = 0;
+            __syncthreads();
+            for (int i = (int)threadIdx.x; i < a.batch * a.N; i += (int)blockDim.x) atomicMax(&sm_rows[i / a.N], a.visible[i]);
+            __syncthreads();
+        }
+        const CacheUnit c = cache_unit(Cache8Cut{many ? sm_rows : nullptr, a.visible, a.table, a.L, a.H_kv, a.batch, a.round, a.parts}, CacheMode::weights, tiles);
+        u.seq = c.seq, u.g = c.g, u.tile = tiles - 1 - c.tile, u.part = c.part, u.t_begin = c.t_begin, u.t_end = c.t_end, u.some = c.some;
+        if (many && u.some) {  // (of a prompt the tiles see different numbers of rows)
+            const int n = tile_sees(a, u.seq, u.tile);
+            u.t_end = n < u.t_end ? n : u.t_end;
+        }
         return u;
     }
     // workgroups go to the eight XCDs in turn: the row tiles of a part, which share its rows of the cache, to one XCD, one after the other
@@ -77,6 +89,19 @@ __device__ __forceinline__ Unit8 unit8(const Cache8Args &a)
     return u;
 }
 
+// A part that has no rows for this tile.
+__device__ __forceinline__ void leave_nothing(const Cache8Args &a, const Unit8 &u)
+{
+    const int n_rep = a.H_q / a.H_kv, M = a.N * n_rep;
+    for (int i = (int)threadIdx.x; i < a.rows; i += (int)blockDim.x) {
+        const int m = u.tile * a.rows + i;
+        if (m >= M) break;
+        const size_t slot = ((size_t)u.part * a.N + m / n_rep) * a.H_q + u.g * n_rep + m % n_rep;
+        a.part_ml[2 * slot] = -INFINITY;
+        a.part_ml[2 * slot + 1] = 0.0f;
+    }
+}
+
 template <int CODE> __device__ __forceinline__ float value8(uint8_t x)
 {
     return CODE == XKV_E4M3 ? __builtin_amdgcn_cvt_f32_fp8((int)x, 0) : (float)(int8_t)x;
@@ -96,6 +121,7 @@ __global__ __launch_bounds__(256) void cache8_general_kernel(Cache8Args a)
     constexpr int TOGETHER = 16 / JP;  // rows of a wavefront that are requested together
     const Unit8 u = unit8(a);
     if (!u.some) return;  // (the merge knows)
+    if (u.t_begin >= u.t_end) return leave_nothing(a, u);
     const int lane = lane_id(), w = wave_id(), n_rep = a.H_q / a.H_kv, d = a.d_h, d4 = (d + 3) / 4 * 4, pitch = general_pitch(d);
     const int M = a.N * n_rep;
     float *kt = smem_f, *vt = kt + kGenTokens * pitch, *qs = vt + kGenTokens * pitch, *ps = qs + kGenRows * d4;
@@ -335,6 +361,7 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void cache8_mfma_kernel(Cache
     const Unit8 u = unit8(a);
     const int lane = lane_id(), w = wave_id(), n16 = lane & 15, kk = lane >> 4, n_rep = a.H_q / a.H_kv, M = a.N * n_rep;
     if (!u.some && !direct) return;  // (the merge knows)
+    if (u.t_begin >= u.t_end && !direct) return leave_nothing(a, u);
     const size_t head = (size_t)u.seq * a.H_kv + u.g;
     const uint8_t *K = a.K8 + head * a.L * D, *V = a.V8 + head * a.L * D;
     const float *ks = a.k_scales + head * a.n_c, *vs = a.v_scales + head * a.n_c, c = a.scale * kLog2e;
@@ -657,6 +684,7 @@ __global__ __launch_bounds__(512, 2) void cache8_rows_kernel(Cache8Args a, bool 
     const Unit8 u = same_in_all_lanes(unit8(a));
     const int lane = lane_id(), w = wave_id(), n16 = lane & 15, kk = lane >> 4, n_rep = a.H_q / a.H_kv, M = a.N * n_rep;
     if (!u.some && !direct) return;  // (the merge knows)
+    if (u.t_begin >= u.t_end && !direct) return leave_nothing(a, u);
     const size_t head = (size_t)u.seq * a.H_kv + u.g;
     const uint8_t *K = a.K8 + head * a.L * D, *V = a.V8 + head * a.L * D;
     const float *ks = a.k_scales + head * a.n_c, *vs = a.v_scales + head * a.n_c, c = a.scale * kLog2e;
@@ -919,7 +947,7 @@ __global__ __launch_bounds__(512, 2) void cache8_rows_kernel(Cache8Args a, bool 
     convert(u.t_begin, 0, 0, 0);
     lds_barrier();
     convert(u.t_begin + TILE, 1, 1, 1);
-    if (u.some) {
+    if (u.t_begin < u.t_end) {
         scales_of(0);
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
@@ -1051,7 +1079,8 @@ __global__ __launch_bounds__(256) void cache8_merge_kernel(Cache8Args a, int lg,
 #pragma unroll
         for (int u = 0; u < BATCH; ++u) {
             const int s = s0 + u * step;
-            if (s < parts) acc += sm_w[grp][s] * v[u];
+            const float wt = s < parts ? sm_w[grp][s] : 0.0f;
+            acc += wt == 0.0f ? vec_t(0.0f) : wt * v[u];  // (a part without rows left nothing)
         }
     }
     if (share) {
@@ -1092,7 +1121,7 @@ hipError_t launch_general(const Cache8Args &a, hipStream_t st)
 {
     const size_t lds = (2 * (size_t)kGenTokens * general_pitch(a.d_h) + (size_t)kGenRows * ((a.d_h + 3) / 4 * 4) + 4 * 4 * kGenTokens) * sizeof(float);
     auto launch = [&](auto kernel, DynamicLdsOnce &attr) {
-        const hipError_t e = attr.ensure((const void *)kernel, 160 * 1024);  // (at most 150 KiB, at 256 channels)
+        const hipError_t e = attr.ensure((const void *)kernel, 150 * 1024);  // (what 256 channels take)
         if (e != hipSuccess) return e;
         hipLaunchKernelGGL(kernel, unit_grid(a), dim3(256), lds, st, a);
         return hipGetLastError();
