@@ -17,7 +17,7 @@ struct Cache8Args {
     const void *q;                     // [batch][N][H_q][d_h]
     const int32_t *visible;            // [batch][N] (nullable: L)
     void *out;
-    // Partials, [part][N][H_q] rows of d_h numbers and of (maximum, sum).
+    // Partials, [part][N][H_q] rows of d_h numbers and of (maximum, sum); NULL: there is one part of everything, whose results go to out.
     float *part_o, *part_ml;
     int32_t *table;                    // by_length: as in CacheArgs
     int L, H_kv, H_q, d_h, batch, N, n_c;
@@ -54,7 +54,7 @@ constexpr int kCutBatch = 1024, kCutQueries = 16384;  // sequences, and queries 
 struct Cache8Plan {
     int n_rep, n_c, shift;
     int rows, round, parts;
-    bool mfma, by_length;
+    bool mfma, by_length, direct;
     float scale;
     size_t off_table, off_part_o, off_part_ml, total;
 };

@@ -93,7 +93,9 @@ xkv_status plan_cache8(const xkv_shape &s, int N, Cache8Plan &p)
             if (parts == 1 || time < best) best = time, p.parts = parts;
         }
     }
-    const size_t part_rows = (size_t)p.parts * (p.by_length ? 1 : batch) * N * s.H_q;
+    // Where there is one part of every row tile, and a workgroup for it also if it has no rows, results leave at once.
+    p.direct = p.parts == 1 && (!p.by_length || batch == 1);
+    const size_t part_rows = p.direct ? 0 : (size_t)p.parts * (p.by_length ? 1 : batch) * N * s.H_q;
     size_t off = align_up(((size_t)batch + 1) * sizeof(int32_t), 256);
     p.off_part_o = off;
     off = align_up(off + part_rows * s.d_h * sizeof(float), 256);
@@ -218,8 +220,10 @@ xkv_status xkv_cache8_decode(const xkv_shape *shape, const void *K8, const void 
     a.visible = visible;
     a.out = out;
     a.table = (int32_t *)((char *)workspace + p.off_table);
-    a.part_o = (float *)((char *)workspace + p.off_part_o);
-    a.part_ml = (float *)((char *)workspace + p.off_part_ml);
+    if (!p.direct) {
+        a.part_o = (float *)((char *)workspace + p.off_part_o);
+        a.part_ml = (float *)((char *)workspace + p.off_part_ml);
+    }
     a.L = s.L;
     a.H_kv = s.H_kv;
     a.H_q = s.H_q;

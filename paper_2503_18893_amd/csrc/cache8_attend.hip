@@ -115,13 +115,13 @@ template <int CODE> __device__ __forceinline__ float value8(uint8_t x)
 __host__ __device__ inline int general_pitch(int d) { return ((d + 3) / 4 | 1) * 4; }  // floats; an odd number of 16-byte pieces
 
 template <typename T, int CODE, int JP>
-__global__ __launch_bounds__(256) void cache8_general_kernel(Cache8Args a)
+__global__ __launch_bounds__(256) void cache8_general_kernel(Cache8Args a, bool direct)
 {
     extern __shared__ __attribute__((aligned(16))) float smem_f[];
     constexpr int TOGETHER = 16 / JP;  // rows of a wavefront that are requested together
     const Unit8 u = unit8(a);
-    if (!u.some) return;  // (the merge knows)
-    if (u.t_begin >= u.t_end) return leave_nothing(a, u);
+    if (!u.some && !direct) return;  // (the merge knows)
+    if (u.t_begin >= u.t_end && !direct) return leave_nothing(a, u);
     const int lane = lane_id(), w = wave_id(), n_rep = a.H_q / a.H_kv, d = a.d_h, d4 = (d + 3) / 4 * 4, pitch = general_pitch(d);
     const int M = a.N * n_rep;
     float *kt = smem_f, *vt = kt + kGenTokens * pitch, *qs = vt + kGenTokens * pitch, *ps = qs + kGenRows * d4;
@@ -219,13 +219,17 @@ __global__ __launch_bounds__(256) void cache8_general_kernel(Cache8Args a)
     for (int r = 0; r < 4; ++r) {
         if (m0 + r >= M) break;
         const int m = m0 + r;
-        const size_t slot = ((size_t)u.part * a.N + m / n_rep) * a.H_q + u.g * n_rep + m % n_rep;
+        const size_t slot = ((size_t)(direct ? u.seq : u.part) * a.N + m / n_rep) * a.H_q + u.g * n_rep + m % n_rep;
 #pragma unroll
         for (int jj = 0; jj < JP; ++jj) {
             const int j = lane + jj * kWave;
-            if (j < d) a.part_o[slot * d + j] = o[r][jj];
+            if (j >= d) continue;
+            if (direct)
+                ((T *)a.out)[slot * d + j] = result<T>(sees[r] == 0 ? 0.0f : o[r][jj] / den[r]);
+            else
+                a.part_o[slot * d + j] = o[r][jj];
         }
-        if (lane == 0) {
+        if (!direct && lane == 0) {
             a.part_ml[2 * slot] = mx[r];
             a.part_ml[2 * slot + 1] = den[r];
         }
@@ -1117,13 +1121,13 @@ dim3 unit_grid(const Cache8Args &a)
 }
 
 template <typename T, int CODE>
-hipError_t launch_general(const Cache8Args &a, hipStream_t st)
+hipError_t launch_general(const Cache8Args &a, bool direct, hipStream_t st)
 {
     const size_t lds = (2 * (size_t)kGenTokens * general_pitch(a.d_h) + (size_t)kGenRows * ((a.d_h + 3) / 4 * 4) + 4 * 4 * kGenTokens) * sizeof(float);
     auto launch = [&](auto kernel, DynamicLdsOnce &attr) {
         const hipError_t e = attr.ensure((const void *)kernel, 150 * 1024);  // (what 256 channels take)
         if (e != hipSuccess) return e;
-        hipLaunchKernelGGL(kernel, unit_grid(a), dim3(256), lds, st, a);
+        hipLaunchKernelGGL(kernel, unit_grid(a), dim3(256), lds, st, a, direct);
         return hipGetLastError();
     };
     static DynamicLdsOnce attr[3];
@@ -1153,7 +1157,7 @@ hipError_t launch_of(Cache8Args a, bool matrix, bool direct, hipStream_t st)
     if (matrix)
         return a.d_h == 64 ? launch_mfma<T, CODE, 64>(a, direct, st) : a.d_h == 128 ? launch_mfma<T, CODE, 128>(a, direct, st)
                                                                                      : launch_mfma<T, CODE, 256>(a, direct, st);
-    return launch_general<T, CODE>(a, st);
+    return launch_general<T, CODE>(a, direct, st);
 }
 
 }  // namespace
@@ -1162,8 +1166,7 @@ hipError_t launch_cache8_attend(const xkv_shape &s, const Cache8Args &given, int
 {
     Cache8Args a = given;
     const bool matrix = mfma && a.shift >= 2 && ((uintptr_t)a.K8 | (uintptr_t)a.V8 | (uintptr_t)a.q) % 16 == 0;
-    // one part of every row tile, and a workgroup for it also where it has no rows
-    const bool direct = matrix && a.parts == 1 && (!a.by_length || a.batch == 1);
+    const bool direct = !a.part_o;
     if (!matrix) a.rows = kGenRows;  // (its rounds divide those of the plan)
     const hipError_t e = s.dtype == XKV_F32 ? code == XKV_E4M3 ? launch_of<float, XKV_E4M3>(a, matrix, direct, st) : launch_of<float, XKV_INT8>(a, matrix, direct, st)
                        : code == XKV_E4M3   ? launch_of<bf16_t, XKV_E4M3>(a, matrix, direct, st)

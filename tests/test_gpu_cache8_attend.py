@@ -113,6 +113,17 @@ CASES = {
     "bf16_prompt_64": ("bf16", 2, 4, 64, 400, 16, [list(range(300, 400))], 1.0),
     "bf16_peaked": ("bf16", 2, 4, 128, 2000, 32, [[2000], [1500]], 12.0),
     "bf16_long": ("bf16", 1, 4, 128, 20011, 32, [[20011]], 1.0),
+    "bf16_twenty_rows": ("bf16", 2, 4, 128, 1300, 32, [[1300, 1299, 1298, 1297, 1296], [5, 4, 3, 2, 1]], 1.0),
+    "bf16_three_row_tiles": ("bf16", 2, 7, 128, 900, 16, [list(range(889, 901)), list(range(12))], 1.0),
+    "bf16_256_many_rows": ("bf16", 1, 8, 256, 700, 64, [[700, 690, 1, 0, 699], [64, 65, 66, 67, 68]], 1.0),
+    "bf16_64_twenty_rows": ("bf16", 2, 4, 64, 1300, 16, [[1300, 1299, 1298, 1297, 1296], [5, 4, 3, 2, 1]], 1.0),
+    "bf16_odd_width_chain": ("bf16", 2, 5, 72, 800, 8, [list(range(791, 801)), list(range(-5, 5))], 1.0),
+    "bf16_odd_width_prompt": ("bf16", 1, 2, 100, 300, 16, [list(range(1, 301))], 1.0),
+    "f32_chain": ("f32", 2, 4, 128, 1500, 32, [list(range(1481, 1501)), list(range(20))], 1.0),
+    "f32_64_prompt": ("f32", 1, 4, 64, 600, 8, [list(range(1, 257)), list(range(340, 596))], 1.0),
+    "f32_256_chain": ("f32", 1, 3, 256, 600, 16, [[598, 599, 600], [1, 0, 2]], 1.0),
+    "f32_odd_width_chain": ("f32", 2, 3, 30, 700, 2, [[700, 1, 0, 699], [64, 65, 66, 67]], 1.0),
+    "bf16_one_head_prompt": ("bf16", 2, 1, 128, 500, 32, [list(range(301, 501))], 1.0),
     "bf16_all_of_it": ("bf16", 2, 4, 128, 515, 32, None, 1.0),
 }
 
@@ -335,3 +346,60 @@ def test_more_than_two_gigabytes_of_codes():
             want, reach = p @ vv, p @ vv.abs()
             # sums over 2^21 rows in fp32, of parts of at most 2^13 rows each in lanes: 2^-24 (2^10 + 2^8) relative, exponentials 2^-20, and bf16
             assert ((out[b, 0, h].double().cpu() - want).abs() <= (2.0 ** -13 + 2.0 ** -7) * reach).all()
+
+
+@pytest.mark.parametrize("code", ["e4m3", "int8"])
+def test_long_parts_of_many_rows(code):
+    """More workgroups than compute units, so that each takes all rows of a cache: the loop over tiles that all queries see, and the rest.  NaN codes
+    and scales in both, that some or all queries see."""
+    s, c, N, L = shape_of(8, 4, 128, 1200, 16, "bf16"), 16, 128, 1200
+    seen = [[L - N - 30 + 1 + i - 7 * b for i in range(N)] for b in range(16)]
+    g, *state = cache(s, code, c, [max(x) for x in seen], 12)
+    q = torch.randn((16, N, 32, 128), generator=g).bfloat16()
+    out = run(s, code, c, seen, q, state)
+
+    def part(b, h):
+        one = shape_of(1, 4, 128, L, 1, "bf16")
+        check(one, code, c, [seen[b]], q[b:b + 1, :, 4 * h:4 * h + 4], [x[b:b + 1, h:h + 1] for x in state], out[b:b + 1, :, 4 * h:4 * h + 4], f"{b} {h}")
+
+    for b, h in ((0, 0), (3, 7), (9, 2), (15, 5)):
+        part(b, h)
+    bad = [x.clone() for x in state]
+    hit = torch.zeros_like(out, dtype=torch.bool)
+    hit[2, :, 4:8] = True                       # a scale of values, in the middle: all of them
+    bad[3][2, 1, 20] = float("nan")
+    t = seen[4][60] // c * c                    # a scale of keys that half of them see
+    bad[2][4, 3, t // c] = float("nan")
+    for i in range(N):
+        hit[4, i, 12:16] = t < seen[4][i]
+    if code == "e4m3":
+        bad[1].view(torch.uint8)[6, 0, 100, 33] = 0x7F  # a value that all see, ..
+        hit[6, :, 0:4, 33] = True
+        for t, ch in ((seen[7][50], 5), (seen[7][50] + 1, 127), (seen[7][90], 5)):  # .. and some that some see
+            bad[1].view(torch.uint8)[7, 7, t, ch] = 0xFF
+            for i in range(N):
+                if t < seen[7][i]:
+                    hit[7, i, 28:32, ch] = True
+    again = run(s, code, c, seen, q, bad)
+    assert torch.equal(again.isnan(), hit)
+    assert torch.equal(again[~hit], out[~hit])
+
+
+@pytest.mark.parametrize("dtype,d,N", [("bf16", 128, 1), ("bf16", 128, 50), ("f32", 64, 1), ("bf16", 40, 2)])
+@pytest.mark.parametrize("code", ["e4m3", "int8"])
+def test_scales_of_all_sizes(dtype, d, N, code):
+    """Blocks of zeros, blocks that are 2^20 times larger than others, in ascending order and mixed, and tiny and huge ones altogether."""
+    s, c, L = shape_of(1, 4, d, 640, 3, dtype), 16, 640
+    seen = [[L - N + 1 + i for i in range(N)]] * 3
+    g, *state = cache(s, code, c, [L] * 3, 13)
+    q = torch.randn((3, N, 4, d), generator=g).to(DT[dtype])
+    by = torch.stack([2.0 ** torch.linspace(-10, 10, 40).round(), 2.0 ** torch.randint(-10, 11, (40,), generator=g).float(), torch.full((40,), 2.0 ** 80)])
+    state[3] = state[3] * by[:, None]
+    state[2][:, :, 5] = 0.0
+    state[3][:, :, 7] = 0.0
+    state[3][2, :, ::2] *= 2.0 ** -6
+    check(s, code, c, seen, q, state, run(s, code, c, seen, q, state), "scales")
+    state[3] = torch.full_like(state[3], 2.0 ** -90)
+    check(s, code, c, seen, q, state, run(s, code, c, seen, q, state), "tiny scales")
+    state[3].zero_()
+    assert (run(s, code, c, seen, q, state) == 0).all()
