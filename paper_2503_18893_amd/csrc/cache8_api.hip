@@ -79,11 +79,10 @@ xkv_status plan_cache8(const xkv_shape &s, int N, Cache8Plan &p)
     if (one) {
         p.parts = 1;
     } else if (batch > 1 && p.by_length) {
-        // Several sequences, whose lengths may differ: two workgroups one after the other where each still has 8192 rows of the cache, so that those of
-        // short sequences fill in.  16 sequences of up to 65536 rows, 8 KV heads: 200 us with one, 195 with two, 197 with three.
-        const int rounds = p.mfma && row_tiles == 1 && batch * units * s.L >= 2LL * slots * 8192 ? 2 : 1;
+        // (More of them, so that those of short sequences fill in, do not pay: 16 sequences of 4096 to 65536 rows, 8 KV heads, 197 us, with 1.5 times as
+        // many 195, twice 211, three times 198; three of up to 40001, 4 KV heads, 23.9, 26.5, 28.8, 29.2.)
         const long long all = batch * longest, most = all < batch + kMaxCacheParts - 1 ? all : batch + kMaxCacheParts - 1;
-        p.parts = clampi((int)(rounds * slots / units), (int)batch, (int)most);
+        p.parts = clampi((int)(slots / units), (int)batch, (int)most);
     } else {
         // As few as fill the compute units well.  A part costs about what 4 rounds take beside its own.
         long long best = 0;
