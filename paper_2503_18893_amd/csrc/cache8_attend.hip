@@ -237,11 +237,11 @@ __global__ __launch_bounds__(256) void cache8_general_kernel(Cache8Args a, bool 
 }
 
 // ------------------------------------------------------------------------------------------
-// Matrix-core path: bf16, D channels, blocks of at least 4 rows.  A wavefront takes tiles of 32 rows of the cache on its own and 16 RT rows (query,
+// Matrix-core path: D channels.  A wavefront takes tiles of 32 rows of the cache on its own and 16 RT rows (query,
 // head):
 //   S^T [32 tokens x rows] = codes of K x Q^T (bf16),  P^T = exp2(c ks S^T - m),  O^T [channels x rows] += codes of V^T x (vs P^T) (fp16)
 // Codes are bf16 and fp16 numbers as they are (3 or 7 bits of mantissa), so both products take them exactly, and the scales, one for four tokens of
-// a lane, multiply logits and weights.  A lane holds one row of S^T, P^T and O^T (rows n16), so that the statistics are its own, and P^T is the
+// a lane (FINE: blocks of one or two rows, one for each), multiply logits and weights.  A lane holds one row of S^T, P^T and O^T (rows n16), so that the statistics are its own, and P^T is the
 // second product's operand as it comes.  Keys and values go from memory to registers: a lane's pieces of K are its operands but for the
 // conversion; of V it reads the tokens that it has weights of, D / 16 channels of each (a row of the cache is read by 16 lanes), and pairs
 // up neighbouring tokens by permuting bytes.
@@ -351,11 +351,13 @@ __device__ __forceinline__ float largest4(const f32x4_t &x) { return fmaxf(fmaxf
 constexpr float kFarUp = 0x1p126f;  // `inv` before any scale was met
 constexpr float kLeast = 0x1p-60f;  // scales by `inv` that are less count as this: their weights are zeros in fp16
 
-template <typename T, int CODE, int D, int RT, bool ONCE>
+template <typename T, int CODE, int D, int RT, bool ONCE, bool FINE>
 __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void cache8_mfma_kernel(Cache8Args a, bool direct)
 {
     constexpr bool F32 = sizeof(T) == 4;
     constexpr int TERMS = F32 ? 3 : 1;  // of a query
+    constexpr int SCALES = FINE ? 8 : 2;  // of a lane's eight tokens: each has its own, or four have one
+    constexpr bool AFTER = F32 || FINE;   // weights are multiplied with scales after the exponential
     static_assert(!F32 || RT == 1, "queries in registers");
     constexpr int KP = D / 64, VW = D / 64, JC = D / 16, STEPS = D / 32, PITCH = D / 4;  // pieces of K, words of V, channels of a lane; products; 16-byte pieces of a row
     constexpr bool Q_LDS = RT > 1;
@@ -372,8 +374,15 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void cache8_mfma_kernel(Cache
 
     Words<4> kr[2][KP];
     Words<VW> vr[8];
-    float ksr[2], vsr[2];
+    float ksr[SCALES], vsr[SCALES];
     const uint32_t k_off = n16 * D + 16 * kk, v_off = 4 * kk * D + 4 * VW * n16;
+    auto request_scales = [&](float (&r)[SCALES], const float *from, int t, int last) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < SCALES; ++i) {
+            const int row = FINE ? 16 * (i / 4) + 4 * kk + i % 4 : 16 * i + 4 * kk;
+            r[i] = from[(t + (row < last ? row : last)) >> a.shift];
+        }
+    };
     auto request_k = [&](int t) __attribute__((always_inline)) {
         const uint8_t *base = K + (size_t)t * D;
         const int last = u.t_end - 1 - t;  // (rows behind the last one: that one again)
@@ -383,9 +392,8 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void cache8_mfma_kernel(Cache
             const uint32_t off = last >= 31 ? k_off + 16 * h * D : (row < last ? row : last) * D + 16 * kk;
 #pragma unroll
             for (int f = 0; f < KP; ++f) kr[h][f] = load_words<4, ONCE>(base + off + 64 * f);
-            const int quad = 16 * h + 4 * kk;
-            ksr[h] = ks[(t + (quad < last ? quad : last)) >> a.shift];
         }
+        request_scales(ksr, ks, t, last);
     };
     auto request_v = [&](int t) __attribute__((always_inline)) {
         const uint8_t *base = V + (size_t)t * D;
@@ -396,11 +404,7 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void cache8_mfma_kernel(Cache
             const uint32_t off = last >= 31 ? v_off + (16 * (e / 4) + e % 4) * D : (row < last ? row : last) * D + 4 * VW * n16;
             vr[e] = load_words<VW, ONCE>(base + off);
         }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int quad = 16 * h + 4 * kk;
-            vsr[h] = vs[(t + (quad < last ? quad : last)) >> a.shift];
-        }
+        request_scales(vsr, vs, t, last);
     };
     constexpr int STEP = 128;  // of a workgroup
     int t = u.t_begin + 32 * w;
@@ -475,12 +479,19 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void cache8_mfma_kernel(Cache
                 }
             }
         }
-        const float kc[2] = {ksr[0] * c, ksr[1] * c};
+        // of element e of the lane's eight: scale e, or e / 4
+        auto of = [](int e) { return FINE ? e : e / 4; };
+        float kc[SCALES], largest = vsr[0];
+#pragma unroll
+        for (int i = 0; i < SCALES; ++i) {
+            kc[i] = ksr[i] * c;
+            largest = fmaxf(largest, vsr[i]);
+        }
         if (next) request_k(t + STEP);
         // element v of half h: token t + 16 h + 4 kk + v
         uint32_t seen[RT];
         float top[RT];
-        bool raise = !(fmaxf(vsr[0], vsr[1]) * inv <= 128.0f);
+        bool raise = !(largest * inv <= 128.0f);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             if (MIXED) {
@@ -489,13 +500,16 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void cache8_mfma_kernel(Cache
                 seen[rt] >>= 4 * kk;
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    S[rt][e / 4][e % 4] = seen[rt] >> (16 * (e / 4) + e % 4) & 1u ? S[rt][e / 4][e % 4] * kc[e / 4] : -INFINITY;
+                    S[rt][e / 4][e % 4] = seen[rt] >> (16 * (e / 4) + e % 4) & 1u ? S[rt][e / 4][e % 4] * kc[of(e)] : -INFINITY;
+            } else if (FINE) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) S[rt][e / 4][e % 4] *= kc[of(e)];
             }
             float lo, hi, most[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 most[h] = largest4(S[rt][h]);
-                if (!MIXED) most[h] *= kc[h];  // (scales are not negative)
+                if (!MIXED && !FINE) most[h] *= kc[h];  // (scales are not negative)
             }
             quarters(fmaxf(most[0], most[1]), lo, hi);
             halves(fmaxf(lo, hi), lo, hi);
@@ -503,7 +517,7 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void cache8_mfma_kernel(Cache
             raise |= !(top[rt] - m_run[rt] <= 8.0f);
         }
         if (__ballot(raise)) {
-            const float largest = wave_all(fmaxf(vsr[0], vsr[1]), MaxOp());  // (NaN is passed over)
+            largest = wave_all(largest, MaxOp());  // (NaN is passed over)
             float less = 1.0f;
             if (largest * inv > 128.0f && largest < INFINITY) {
                 const float now = __uint_as_float((254u + 6u - (__float_as_uint(largest) >> 23 & 0xFFu)) << 23);  // 2^6 by its power of two
@@ -519,13 +533,13 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void cache8_mfma_kernel(Cache
                 m_run[rt] = m_new;
             }
         }
-        // vs P = exp2(z - m + log2 vs), whose sum by 1 / vs is that of the weights (fp32: one after the other)
+        // vs P = exp2(z - m + log2 vs), whose sum by 1 / vs is that of the weights (AFTER: one after the other)
         float lv[2], rv[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const float v = vsr[h] * inv < kLeast ? kLeast : vsr[h] * inv;  // (NaN stays)
-            lv[h] = F32 ? 0.0f : __builtin_amdgcn_logf(v);
-            rv[h] = F32 ? 1.0f : __builtin_amdgcn_rcpf(v);
+            const float v = AFTER ? 1.0f : vsr[h] * inv < kLeast ? kLeast : vsr[h] * inv;  // (NaN stays)
+            lv[h] = AFTER ? 0.0f : __builtin_amdgcn_logf(v);
+            rv[h] = AFTER ? 1.0f : __builtin_amdgcn_rcpf(v);
         }
         f16x8_t P[RT], R[RT];  // .. (fp32) and what P leaves
 #pragma unroll
@@ -534,7 +548,7 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void cache8_mfma_kernel(Cache
             f32x8_t z;
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                z[e] = __builtin_amdgcn_exp2f(MIXED ? S[rt][e / 4][e % 4] + add[e / 4] : fmaf(S[rt][e / 4][e % 4], kc[e / 4], add[e / 4]));
+                z[e] = __builtin_amdgcn_exp2f(MIXED || FINE ? S[rt][e / 4][e % 4] + add[e / 4] : fmaf(S[rt][e / 4][e % 4], kc[of(e)], add[e / 4]));
             if (MIXED) {  // (a scale that is not seen may be NaN)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) z[e] = seen[rt] >> (16 * (e / 4) + e % 4) & 1u ? z[e] : 0.0f;
@@ -544,9 +558,9 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void cache8_mfma_kernel(Cache
                 const float by = MIXED && !(seen[rt] >> (16 * h) & 0xFu) ? 0.0f : rv[h];
                 l_run[rt] = fmaf((z[4 * h] + z[4 * h + 1]) + (z[4 * h + 2] + z[4 * h + 3]), by, l_run[rt]);
             }
-            if constexpr (F32) {
+            if constexpr (AFTER) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) z[e] *= MIXED && !(seen[rt] >> (16 * (e / 4)) & 0xFu) ? 0.0f : vsr[e / 4] * inv;
+                for (int e = 0; e < 8; ++e) z[e] *= MIXED && !(seen[rt] >> (16 * (e / 4) + e % 4) & 1u) ? 0.0f : vsr[of(e)] * inv;
             }
             P[rt] = __builtin_convertvector(z, f16x8_t);
             if constexpr (F32) R[rt] = __builtin_convertvector(z - __builtin_convertvector(P[rt], f32x8_t), f16x8_t);
@@ -1143,9 +1157,10 @@ hipError_t launch_mfma(const Cache8Args &a, bool direct, hipStream_t st)
         return hipGetLastError();
     };
     const bool once = a.rows >= a.N * (a.H_q / a.H_kv);
-    if (a.rows == 16) return once ? launch(cache8_mfma_kernel<T, CODE, D, 1, true>) : launch(cache8_mfma_kernel<T, CODE, D, 1, false>);
+    if (a.shift < 2) return launch(cache8_mfma_kernel<T, CODE, D, 1, false, true>);
+    if (a.rows == 16) return once ? launch(cache8_mfma_kernel<T, CODE, D, 1, true, false>) : launch(cache8_mfma_kernel<T, CODE, D, 1, false, false>);
     if constexpr (sizeof(T) == 2 && D < 256) {
-        if (a.rows == 32) return once ? launch(cache8_mfma_kernel<T, CODE, D, 2, true>) : launch(cache8_mfma_kernel<T, CODE, D, 2, false>);
+        if (a.rows == 32) return once ? launch(cache8_mfma_kernel<T, CODE, D, 2, true, false>) : launch(cache8_mfma_kernel<T, CODE, D, 2, false, false>);
         if constexpr (D == 128) return launch(cache8_rows_kernel<CODE>, 512);
     }
     return hipErrorInvalidValue;
@@ -1165,9 +1180,9 @@ hipError_t launch_of(Cache8Args a, bool matrix, bool direct, hipStream_t st)
 hipError_t launch_cache8_attend(const xkv_shape &s, const Cache8Args &given, int code, bool mfma, hipStream_t st)
 {
     Cache8Args a = given;
-    const bool matrix = mfma && a.shift >= 2 && ((uintptr_t)a.K8 | (uintptr_t)a.V8 | (uintptr_t)a.q) % 16 == 0;
+    const bool matrix = mfma && ((uintptr_t)a.K8 | (uintptr_t)a.V8 | (uintptr_t)a.q) % 16 == 0;
     const bool direct = !a.part_o;
-    if (!matrix) a.rows = kGenRows;  // (its rounds divide those of the plan)
+    if (!matrix || a.shift < 2) a.rows = kGenRows;  // (.. of the plan's 16, 32 or 256; its rounds divide the plan's)
     const hipError_t e = s.dtype == XKV_F32 ? code == XKV_E4M3 ? launch_of<float, XKV_E4M3>(a, matrix, direct, st) : launch_of<float, XKV_INT8>(a, matrix, direct, st)
                        : code == XKV_E4M3   ? launch_of<bf16_t, XKV_E4M3>(a, matrix, direct, st)
                                             : launch_of<bf16_t, XKV_INT8>(a, matrix, direct, st);

@@ -123,6 +123,9 @@ CASES = {
     "f32_64_prompt": ("f32", 1, 4, 64, 600, 8, [list(range(1, 257)), list(range(340, 596))], 1.0),
     "f32_256_chain": ("f32", 1, 3, 256, 600, 16, [[598, 599, 600], [1, 0, 2]], 1.0),
     "f32_odd_width_chain": ("f32", 2, 3, 30, 700, 2, [[700, 1, 0, 699], [64, 65, 66, 67]], 1.0),
+    "bf16_rows_of_their_own_chain": ("bf16", 2, 7, 128, 1300, 1, [list(range(1291, 1301)), list(range(10))], 1.0),
+    "bf16_pairs_prompt": ("bf16", 1, 4, 64, 400, 2, [list(range(1, 101)), list(range(301, 401))], 1.0),
+    "bf16_256_rows_of_their_own": ("bf16", 1, 4, 256, 600, 1, [[600, 599], [0, 1]], 1.0),
     "bf16_one_head_prompt": ("bf16", 2, 1, 128, 500, 32, [list(range(301, 501))], 1.0),
     "bf16_all_of_it": ("bf16", 2, 4, 128, 515, 32, None, 1.0),
 }
@@ -158,10 +161,11 @@ def test_visible_outside_the_cache_counts_as_the_nearer_end():
 
 
 @pytest.mark.parametrize("code", ["e4m3", "int8"])
-@pytest.mark.parametrize("dtype,d,N", [("f32", 64, 3), ("bf16", 128, 1), ("bf16", 128, 4), ("bf16", 128, 40)])
-def test_nan_reaches_those_that_see_it(dtype, d, N, code):
+@pytest.mark.parametrize("dtype,d,N,c", [("f32", 64, 3, 16), ("bf16", 128, 1, 16), ("bf16", 128, 4, 16), ("bf16", 128, 40, 16), ("bf16", 128, 5, 1), ("f32", 128, 5, 2),
+                                         ("bf16", 48, 3, 8), ("bf16", 64, 12, 4)])
+def test_nan_reaches_those_that_see_it(dtype, d, N, c, code):
     """A NaN scale of keys or values, and (e4m3) a NaN code: rows of NaN, or one channel, for the queries that see it, and nothing for the others."""
-    s, c, L = shape_of(2, 4, d, 400, 2, dtype), 16, 400
+    s, L = shape_of(2, 4, d, 400, 2, dtype), 400
     seen = [list(range(300 - N + 1, 301))] * 2
     g, *state = cache(s, code, c, [L, L], 8)
     q = torch.randn((2, N, 8, d), generator=g).to(DT[dtype])
