@@ -44,19 +44,37 @@ template <typename T, int VEC> struct Piece {
     T x[VEC];
 };
 
+// Over the LANES lanes (16, 32, 64) that work together, in all of them.
+template <int LANES, typename T, typename OP> __device__ __forceinline__ T lanes_all(T v, OP op)
+{
+    if constexpr (LANES == 64) return wave_all(v, op);
+    auto with = [&](uint32_t o) { v = op(v, __builtin_bit_cast(T, o)); };
+    with(lanes_by<0xB1>(__builtin_bit_cast(uint32_t, v)));
+    with(lanes_by<0x4E>(__builtin_bit_cast(uint32_t, v)));
+    with(lanes_by<0x141>(__builtin_bit_cast(uint32_t, v)));
+    with(lanes_by<0x140>(__builtin_bit_cast(uint32_t, v)));
+    if constexpr (LANES == 32) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+        v = op(__builtin_bit_cast(T, (uint32_t)r[0]), __builtin_bit_cast(T, (uint32_t)r[1]));
+    }
+    return v;
+}
+
 // ------------------------------------------------------------------------------------------
-// WAVES wavefronts take a block of a KV head of K or V: first the largest magnitude of its new rows, then their codes.  A thread's pieces, up to KEPT of
-// them, stay in registers between the two; a larger block's are read again.  Codes of older rows are only touched where the scale grows.
+// THREADS threads (part of a wavefront, one, or four) take a block of a KV head of K or V: first the largest magnitude of its new rows, then their codes.
+// A thread's pieces, up to KEPT of them, stay in registers between the two; a larger block's are read again.  Codes of older rows are
+// only touched where the scale grows.  Long appends are bound by their bytes: 32768 tokens of 8 KV heads, bf16 to e4m3, blocks of 32 rows, 40 us, 5.0 TB/s
+// (48 with divisions in the place of `quotient`); one token of 16 sequences 3.5 us, a chain of two loads, the maximum and the quotients.
 // ------------------------------------------------------------------------------------------
-template <typename T, int CODE, int VEC, int WAVES>
+template <typename T, int CODE, int VEC, int THREADS, int KEPT>
 __global__ __launch_bounds__(256) void cache8_append_kernel(Cache8Append a, unsigned units)
 {
-    constexpr int KEPT = VEC > 1 ? 8 : 16, THREADS = 64 * WAVES;
+    constexpr int WAVES = THREADS / kWave;  // (0: part of one)
     __shared__ float sm_top[WAVES > 1 ? WAVES : 1];
     __shared__ int sm_odd[WAVES > 1 ? WAVES : 1];
-    const unsigned unit = WAVES > 1 ? blockIdx.x : blockIdx.x * 4 + (unsigned)wave_id();
+    const unsigned unit = THREADS == 256 ? blockIdx.x : THREADS == 64 ? blockIdx.x * 4 + (unsigned)wave_id() : blockIdx.x * (256 / THREADS) + threadIdx.x / THREADS;
     if (unit >= units) return;
-    const int lane = WAVES > 1 ? (int)threadIdx.x : lane_id(), g = (int)(unit % a.H_kv), of = (int)(unit / a.H_kv % 2), rest = (int)(unit / (2 * a.H_kv));
+    const int lane = (int)threadIdx.x % THREADS, g = (int)(unit % a.H_kv), of = (int)(unit / a.H_kv % 2), rest = (int)(unit / (2 * a.H_kv));
     const int place = rest % a.blocks, b = rest / a.blocks;
     int n = a.lengths ? a.lengths[b] : 0, count = a.counts ? a.counts[b] : a.N;
     n = n < 0 ? 0 : n < a.L ? n : a.L;
@@ -118,8 +136,8 @@ __global__ __launch_bounds__(256) void cache8_append_kernel(Cache8Append a, unsi
                 top = fmaxf(top, v);
             }
     }
-    top = wave_all(top, MaxOp());
-    odd = __ballot(odd) != 0;
+    top = lanes_all<THREADS < kWave ? THREADS : kWave>(top, MaxOp());
+    odd = lanes_all<THREADS < kWave ? THREADS : kWave>((int)odd, MaxOp()) != 0;
     if constexpr (WAVES > 1) {
         if (lane_id() == 0) sm_top[wave_id()] = top, sm_odd[wave_id()] = odd;
         __syncthreads();
@@ -200,15 +218,20 @@ hipError_t launch_append(const Cache8Append &a, hipStream_t st)
     constexpr int WIDE = 16 / sizeof(T);
     const unsigned units = (unsigned)a.blocks * 2 * a.H_kv * a.batch;  // (at most 2^31 - 1)
     const bool wide = wide_ok(a, (int)sizeof(T));
-    // a wavefront where a block's new rows fit its registers, four where they do not
-    const long long rows = a.N < (1LL << a.shift) ? a.N : 1LL << a.shift;
-    const bool four = rows * (a.d_h / (wide ? WIDE : 1)) > (wide ? 8 : 16) * kWave;
-    auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3(four ? units : (units + 3) / 4), dim3(256), 0, st, a, units);
+    // As few threads as hold a block's new rows in registers, and as few registers as that takes.  32768 tokens of 8 KV heads, bf16: blocks of 64 rows by four
+    // wavefronts 49 us, by one 59, of 32 78 and 40; blocks of 8 rows in 2 pieces a thread 47, with room for 8 76;
+    // blocks of one row by 16 lanes 74, by 64 268.
+    const long long rows = a.N < (1LL << a.shift) ? a.N : 1LL << a.shift, pieces = rows * (a.d_h / (wide ? WIDE : 1));
+    auto launch = [&](auto kernel, int threads) {
+        const unsigned of = 256 / threads;
+        hipLaunchKernelGGL(kernel, dim3((units + of - 1) / of), dim3(256), 0, st, a, units);
         return hipGetLastError();
     };
-    if (wide) return four ? launch(cache8_append_kernel<T, CODE, WIDE, 4>) : launch(cache8_append_kernel<T, CODE, WIDE, 1>);
-    return four ? launch(cache8_append_kernel<T, CODE, 1, 4>) : launch(cache8_append_kernel<T, CODE, 1, 1>);
+    if (!wide) return pieces <= 16 * kWave ? launch(cache8_append_kernel<T, CODE, 1, 64, 16>, 64) : launch(cache8_append_kernel<T, CODE, 1, 256, 16>, 256);
+    return pieces <= 16 ? launch(cache8_append_kernel<T, CODE, WIDE, 16, 1>, 16) : pieces <= 32 ? launch(cache8_append_kernel<T, CODE, WIDE, 32, 1>, 32)
+         : pieces <= kWave ? launch(cache8_append_kernel<T, CODE, WIDE, 64, 1>, 64) : pieces <= 2 * kWave ? launch(cache8_append_kernel<T, CODE, WIDE, 64, 2>, 64)
+         : pieces <= 4 * kWave ? launch(cache8_append_kernel<T, CODE, WIDE, 64, 4>, 64) : pieces <= 8 * kWave ? launch(cache8_append_kernel<T, CODE, WIDE, 64, 8>, 64)
+                                                                                        : launch(cache8_append_kernel<T, CODE, WIDE, 256, 8>, 256);
 }
 
 }  // namespace

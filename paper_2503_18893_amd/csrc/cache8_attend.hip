@@ -110,7 +110,7 @@ template <int CODE> __device__ __forceinline__ float value8(uint8_t x)
 // ------------------------------------------------------------------------------------------
 // General path, any type, width and block.  A round takes 64 rows of the cache, whose keys and values, with their scales, go to LDS in single precision.
 // For the logits a lane multiplies one of the keys with the four queries of its wavefront; for the sums lanes run over the channels, and
-// the weights go through LDS.
+// the weights go through LDS.  Far from its bytes: one query of 4 heads on each of 8 KV heads after 32768 rows of 96 channels, 107 us (10 at the rate of a copy).
 // ------------------------------------------------------------------------------------------
 __host__ __device__ inline int general_pitch(int d) { return ((d + 3) / 4 | 1) * 4; }  // floats; an odd number of 16-byte pieces
 
@@ -247,7 +247,11 @@ __global__ __launch_bounds__(256) void cache8_general_kernel(Cache8Args a, bool 
 // up neighbouring tokens by permuting bytes.
 // The maximum is only raised when a logit outgrows it by 2^8.  Weights times scales enter as fp16, 2^-12: `inv`, a power of two, brings the largest scale met
 // so far to between 2^6 and 2^7, so that they are at most 2^15, and down to 2^-20 of that scale keep their 11 bits (what is smaller is held to 2^-32 of it).
-// Beside the output's own rounding, 2^-9 root mean square of its value, that is not seen: 0.0017 of the root mean square against 64 bits with and without.
+// Beside the output's own rounding that is not seen: the error against 64 bits is 0.0017 of the results' root mean square, with bf16 pairs in its place as well.
+// fp32: a query is three terms of bf16, a weight two of fp16, and scales are multiplied in after the exponential.
+// It is a stream: one query after 32768 rows of 8 KV heads, 67 MB, 15 us with its start and end (6.4 TB/s with 16 sequences of 65536); 16 heads 15, 20 rows 20,
+// 32 rows 23; from there on row tiles of their own, which read the same rows of the cache (64 rows 24, 128 38).  A wavefront takes 0.8 to 1.3 us a tile, a
+// chain of products, a maximum and exponentials; two of them to a vector unit keep 64 KB a compute unit under way.
 // ------------------------------------------------------------------------------------------
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8_t;
 typedef __attribute__((ext_vector_type(2))) _Float16 f16x2_t;
@@ -1041,7 +1045,8 @@ __global__ __launch_bounds__(512, 2) void cache8_rows_kernel(Cache8Args a, bool 
 // ------------------------------------------------------------------------------------------
 // Merge.  A group of 2^lg lanes covers the columns of a row (query, head), VEC a lane.  Where there are many rows, a group per row; where there are few,
 // the groups of a workgroup share a row's partials and are added up in LDS: latency is all there is to it then, and the first partials are
-// requested before their weights are known.  Partials of parts that have no rows were not written and are not read.
+// requested before their weights are known.  Partials of parts that have no rows were not written and are not read.  64 parts of 32 rows 4.4 us, most of
+// it a launch's own time; a group per row there 9.
 // ------------------------------------------------------------------------------------------
 template <typename T, int VEC>
 __global__ __launch_bounds__(256) void cache8_merge_kernel(Cache8Args a, int lg, int share, int rows)
