@@ -121,3 +121,20 @@ def test_strides_are_checked():
     # in place: as it lies
     assert rotate(s, q_out=2 << 20, q_at=at(4 * 48 * 128, 48 * 128, 128)) == BAD
     assert rotate(s0, q_out=2 << 20, q_at=at(4 * 48 * 128, 48 * 128, 128), q_out_at=at(4 * 48 * 128, 48 * 128, 128)) == xb.XKV_OK
+
+
+def test_the_binding_wants_rows():
+    import torch
+    s, f = shape(batch=0), torch.zeros(64, dtype=torch.float64)
+    x = torch.zeros((1, 2, 8, 128), dtype=torch.bfloat16)
+    xb.xkv_rotate(s, 128, "half", "forward", 1.0, f, None, 2, None, None, x, x, stream=0)
+    for bad in (x[0], x[:, :, :, ::2], x.transpose(2, 3)):
+        with pytest.raises(ValueError):
+            xb.xkv_rotate(s, 128, "half", "forward", 1.0, f, None, 2, None, None, bad, x, stream=0)
+        with pytest.raises(ValueError):
+            xb.xkv_cache8_append(s, x, bad, None, None, 2, "int8", 16, x, x, f, f, stream=0)
+    for name in ("halves", 0):
+        with pytest.raises(KeyError):
+            xb.xkv_rotate(s, 128, name, "forward", 1.0, f, None, 2, None, None, x, x, stream=0)
+    with pytest.raises(xb.XkvError):
+        xb.xkv_rotate(shape(), 128, "half", "forward", 1.0, f, None, 0, None, None, x, x, stream=0)

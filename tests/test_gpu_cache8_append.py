@@ -184,3 +184,25 @@ def test_codes_that_are_not_aligned():
             ref.append(new[0, :, g].float(), 0, 20, codes[0, g], scales[0, g], c, "e4m3")
     same([K8.contiguous()] + dev[1:], state, "not aligned")
     assert (room[:3] == 0).all()
+
+
+def test_no_strides_are_contiguous_rows():
+    """NULL in the place of strides, as a C program may pass it: rows one after the other, [batch][N][heads][d_h]; here and in xkv_rotate."""
+    import ctypes
+    s = shape_of(3, 64, 90, 2, "bf16")
+    K, V = (torch.randn((2, 20, 3, 64)).bfloat16() for _ in "KV")
+    state = empty(s, 16, "int8", 9)
+    dev, Kd, Vd = [x.cuda() for x in state], K.cuda(), V.cuda()
+    lib, st = xb.load(), torch.cuda.current_stream().cuda_stream
+    assert lib.xkv_cache8_append(s.ref, Kd.data_ptr(), None, Vd.data_ptr(), None, None, None, 20, 1, 16, *(x.data_ptr() for x in dev), st) == 0
+    for new, codes, scales in ((K, state[0], state[2]), (V, state[1], state[3])):
+        for b in range(2):
+            for g in range(3):
+                ref.append(new[b, :, g].float(), 0, 20, codes[b, g], scales[b, g], 16, "int8")
+    same(dev, state, "no strides")
+    f = ref.frequencies(64, 1e4).cuda()
+    a, b = torch.empty_like(Kd), torch.empty_like(Kd)
+    xb.xkv_rotate(s, 64, "half", "forward", 1.0, f, None, 20, None, None, Kd, a)
+    nothing = ctypes.c_void_p(0)
+    assert lib.xkv_rotate(s.ref, 64, 0, 0, 1.0, f.data_ptr(), None, 20, nothing, None, nothing, None, Kd.data_ptr(), None, b.data_ptr(), None, st) == 0
+    assert torch.equal(a, b)

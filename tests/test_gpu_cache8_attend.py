@@ -126,6 +126,8 @@ CASES = {
     "bf16_rows_of_their_own_chain": ("bf16", 2, 7, 128, 1300, 1, [list(range(1291, 1301)), list(range(10))], 1.0),
     "bf16_pairs_prompt": ("bf16", 1, 4, 64, 400, 2, [list(range(1, 101)), list(range(301, 401))], 1.0),
     "bf16_256_rows_of_their_own": ("bf16", 1, 4, 256, 600, 1, [[600, 599], [0, 1]], 1.0),
+    "f32_200": ("f32", 1, 3, 200, 300, 16, [[300, 7]], 1.0),
+    "bf16_255": ("bf16", 2, 3, 255, 900, 32, [[900], [450]], 1.0),
     "bf16_one_head_prompt": ("bf16", 2, 1, 128, 500, 32, [list(range(301, 501))], 1.0),
     "bf16_all_of_it": ("bf16", 2, 4, 128, 515, 32, None, 1.0),
 }
@@ -150,6 +152,18 @@ def test_many_sequences_and_a_scale():
     g, *state = cache(s, "e4m3", 16, [x[0] for x in visible], 1)
     q = torch.randn((70, 1, 4, 128), generator=g).bfloat16()
     check(s, "e4m3", 16, visible, q, state, run(s, "e4m3", 16, visible, q, state), "many sequences")
+
+
+@pytest.mark.parametrize("batch,N,L,d", [(70, 2, 700, 128), (1100, 1, 600, 64), (1, 16500, 700, 128), (40, 30, 900, 64)])
+def test_many_sequences_and_queries(batch, N, L, d):
+    """Around what is cut by length: more sequences than lanes, than are cut at all, more queries than are looked at."""
+    s = shape_of(1, 1, d, L, batch, "bf16")
+    g = torch.Generator().manual_seed(batch + N)
+    visible = torch.randint(-3, L + 4, (batch, N), generator=g)
+    visible[0, 0] = L
+    _, *state = cache(s, "int8", 32, [L] * batch, 1)
+    q = torch.randn((batch, N, 1, d), generator=g).bfloat16()
+    check(s, "int8", 32, visible.tolist(), q, state, run(s, "int8", 32, visible.tolist(), q, state), f"{batch} x {N}")
 
 
 def test_visible_outside_the_cache_counts_as_the_nearer_end():
