@@ -450,7 +450,7 @@ XKV_API xkv_status xkv_evict(const xkv_shape *shape, const void *K, const void *
  *   not both); the rows of d_h numbers may lie anywhere: `*_at` (HOST pointers, nullable: contiguous as above) give the numbers from one
  *   sequence, token and head to the next, so that slices of a projection's result, drafted keys [batch][H_kv][N][d_h] and rows of a cache
  *   are taken as they lie.  Strides are not negative; rows of an output must not overlap (in the order of their strides each reaches
- *   beyond all that is inside it).  In place: out = in with the same strides; otherwise outputs must not overlap inputs.  positions
+ *   beyond all that is inside it).  In place: out = in with the same strides; otherwise outputs must not overlap inputs, nor one another.  positions
  *   [batch][N] int32 (device, nullable: 0 .. N - 1).  frequencies [d_rot / 2] double (device).  Angles are taken in double precision,
  *   the rest in fp32, rounded once.  shape->G, r_k, r_v, L, k, scale are ignored.
  * xkv_rope_frequencies: such a table, once per model (frequencies: device, [d_rot / 2]).  f_j = theta^(-2j / d_rot), and for contexts that are
@@ -485,7 +485,7 @@ XKV_API xkv_status xkv_rotate(const xkv_shape *shape, int32_t d_rot, int32_t lay
  * xkv_cache8_append: the new rows K, V [batch][N][H_kv][d_h] in shape->dtype (`*_at` as in xkv_rotate) of every sequence go to its rows lengths[b],
  *   lengths[b] + 1, .. .  lengths [batch] int32 (device, nullable: 0) are the rows in use before; counts [batch] (device, nullable: N) how many of a
  *   sequence's N rows there are, the others are padding; both count as the nearer of their bounds (0 and L, 0 and N) and rows beyond L are
- *   dropped.  The caller raises its lengths afterwards.  For a block that gets rows, a the largest magnitude of those:
+ *   dropped.  The caller raises its lengths afterwards.  A block is one workgroup's: few large blocks take long.  For a block that gets rows, a the largest magnitude of those:
  *     no rows in use before, or a scale of 0:  s = max(a / H, 2^-126), or 0 where a = 0
  *     otherwise:  s = 2^i times its scale with the smallest i >= 0 for which a <= H s (in fp32); where i > 0 its rows in use get the codes of
  *       2^-i of their values, so that an int8 row, however often its block's scale grows, is off by at most one step of it
@@ -494,7 +494,7 @@ XKV_API xkv_status xkv_rotate(const xkv_shape *shape, int32_t d_rot, int32_t lay
  * xkv_cache8_decode: query i of sequence b, q [batch][N][H_q][d_h], attends to the first visible[b][i] rows (device int32 [batch][N], nullable: all L; counts as
  *   the nearer of 0 and L): a token after a cache, a drafted chain, or the tokens of a prompt, each with the rows up to its own.
  *     z_t = scale k_scale[t / c] <q, K8_t>,  out = sum_t softmax(z)_t v_scale[t / c] V8_t;  out [batch][N][H_q][d_h] in shape->dtype.
- *   Zeros for a query that sees nothing.  Sums and statistics are fp32.  A weight times its scale enters the sums held to 2^-12 (fp32 shapes: 2^-22), or to
+ *   Zeros for a query that sees nothing.  out must not overlap what is read.  Sums and statistics are fp32.  A weight times its scale enters the sums held to 2^-12 (fp32 shapes: 2^-22), or to
  *   2^-31 of the largest such product that a workgroup's rows can have where that is more; results are rounded once.  A NaN in a code or scale that a query
  *   sees gives NaN, one that it does not see does not reach it.  Scales are numbers from 2^-100 to 2^100, 0 or NaN: infinities, and products
  *   of a weight with a smaller scale, need not come out as the formula says.

@@ -11,6 +11,12 @@ template <typename T> __device__ __forceinline__ T result(float x);
 template <> __device__ __forceinline__ float result<float>(float x) { return x; }
 template <> __device__ __forceinline__ bf16_t result<bf16_t>(float x) { return __builtin_bit_cast(bf16_t, (__bf16)x); }
 
+// Grids of up to 2^31 workgroups of 256 threads: a launch takes less than 2^32 threads in a direction, so more than 2^22 workgroups lie in rows of
+// as many, the last of which may reach beyond the end.
+constexpr int kLongGrid = 22;
+inline dim3 long_grid(unsigned n) { return n <= 1u << kLongGrid ? dim3(n) : dim3(1u << kLongGrid, ((n - 1) >> kLongGrid) + 1); }
+__device__ __forceinline__ unsigned long_grid_unit() { return blockIdx.x + (blockIdx.y << kLongGrid); }
+
 struct Cache8Args {
     const uint8_t *K8, *V8;            // [batch][H_kv][L][d_h]
     const float *k_scales, *v_scales;  // [batch][H_kv][n_c]

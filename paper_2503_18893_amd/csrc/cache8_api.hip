@@ -84,10 +84,10 @@ xkv_status plan_cache8(const xkv_shape &s, int N, Cache8Plan &p)
         const long long all = batch * longest, most = all < batch + kMaxCacheParts - 1 ? all : batch + kMaxCacheParts - 1;
         p.parts = clampi((int)(slots / units), (int)batch, (int)most);
     } else {
-        // As few as fill the compute units well.  A part costs about what 4 rounds take beside its own.
+        // As few as fill the compute units well (one where units alone do that 64 times over).  A part costs about what 4 rounds take beside its own.
         long long best = 0;
         p.parts = 1;
-        for (int parts = 1; parts <= kMaxCacheParts && parts <= longest; ++parts) {
+        for (int parts = 1; parts <= kMaxCacheParts && parts <= longest && units * batch * (parts - 1) < 64 * slots; ++parts) {
             const long long time = ((units * batch * parts + slots - 1) / slots) * (ceil_div(longest, parts) + 4);
             if (parts == 1 || time < best) best = time, p.parts = parts;
         }

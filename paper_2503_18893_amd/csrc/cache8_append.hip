@@ -72,7 +72,8 @@ __global__ __launch_bounds__(256) void cache8_append_kernel(Cache8Append a, unsi
     constexpr int WAVES = THREADS / kWave;  // (0: part of one)
     __shared__ float sm_top[WAVES > 1 ? WAVES : 1];
     __shared__ int sm_odd[WAVES > 1 ? WAVES : 1];
-    const unsigned unit = THREADS == 256 ? blockIdx.x : THREADS == 64 ? blockIdx.x * 4 + (unsigned)wave_id() : blockIdx.x * (256 / THREADS) + threadIdx.x / THREADS;
+    const unsigned group = long_grid_unit();
+    const unsigned unit = THREADS == 256 ? group : THREADS == 64 ? group * 4 + (unsigned)wave_id() : group * (256 / THREADS) + threadIdx.x / THREADS;
     if (unit >= units) return;
     const int lane = (int)threadIdx.x % THREADS, g = (int)(unit % a.H_kv), of = (int)(unit / a.H_kv % 2), rest = (int)(unit / (2 * a.H_kv));
     const int place = rest % a.blocks, b = rest / a.blocks;
@@ -224,7 +225,7 @@ hipError_t launch_append(const Cache8Append &a, hipStream_t st)
     const long long rows = a.N < (1LL << a.shift) ? a.N : 1LL << a.shift, pieces = rows * (a.d_h / (wide ? WIDE : 1));
     auto launch = [&](auto kernel, int threads) {
         const unsigned of = 256 / threads;
-        hipLaunchKernelGGL(kernel, dim3((units + of - 1) / of), dim3(256), 0, st, a, units);
+        hipLaunchKernelGGL(kernel, long_grid((units + of - 1) / of), dim3(256), 0, st, a, units);
         return hipGetLastError();
     };
     if (!wide) return pieces <= 16 * kWave ? launch(cache8_append_kernel<T, CODE, 1, 64, 16>, 64) : launch(cache8_append_kernel<T, CODE, 1, 256, 16>, 256);

@@ -53,7 +53,9 @@ __global__ __launch_bounds__(kRopeThreads) void rotate_kernel(RotateArgs a, int 
     constexpr int ROWS = 4;
     extern __shared__ float2 sm_unit[];  // [tokens][d_rot / 2]
     const int m = a.d_rot / 2, groups = (a.N + tokens - 1) / tokens;
-    const int b = (int)(blockIdx.x / (unsigned)groups), first = (int)(blockIdx.x % (unsigned)groups) * tokens;
+    const unsigned unit = long_grid_unit();
+    const int b = (int)(unit / (unsigned)groups), first = (int)(unit % (unsigned)groups) * tokens;
+    if (b >= a.batch) return;
     const int here = a.N - first < tokens ? a.N - first : tokens, heads = a.heads[0] + a.heads[1], rows = here * heads;
     const int turned = m / PAIRS, items = turned + (a.d_h - a.d_rot) / VEC;
     const int i = (int)threadIdx.x & ((1 << lg_width) - 1), row0 = (int)threadIdx.x >> lg_width, step = kRopeThreads >> lg_width;
@@ -142,7 +144,7 @@ hipError_t launch_rotate_of(const RotateArgs &a, bool interleaved, hipStream_t s
     while (tokens < 8 && ((a.heads[0] + a.heads[1]) * tokens << lg) < kRopeThreads) tokens *= 2;
     const unsigned groups = (unsigned)((a.N + tokens - 1) / tokens);
     auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3(groups * (unsigned)a.batch), dim3(kRopeThreads), (size_t)tokens * m * sizeof(float2), st, a, tokens, lg);
+        hipLaunchKernelGGL(kernel, long_grid(groups * (unsigned)a.batch), dim3(kRopeThreads), (size_t)tokens * m * sizeof(float2), st, a, tokens, lg);
         return hipGetLastError();
     };
     if (wide) return interleaved ? launch(rotate_kernel<T, WIDE, true>) : launch(rotate_kernel<T, WIDE, false>);

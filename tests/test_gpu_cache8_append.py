@@ -206,3 +206,17 @@ def test_no_strides_are_contiguous_rows():
     nothing = ctypes.c_void_p(0)
     assert lib.xkv_rotate(s.ref, 64, 0, 0, 1.0, f.data_ptr(), None, 20, nothing, None, nothing, None, Kd.data_ptr(), None, b.data_ptr(), None, st) == 0
     assert torch.equal(a, b)
+
+
+def test_more_workgroups_than_a_launch_has_in_one_direction():
+    """2^25 rows and more, each its own block, four a workgroup of 256 threads, of keys and values: 2^32 threads."""
+    N = (1 << 25) + 4099
+    s = shape_of(1, 1, N, 1, "bf16")
+    K, V = (torch.randn((1, N, 1, 1), device="cuda").bfloat16() for _ in "KV")
+    codes = [torch.full((1, 1, N, 1), 77, dtype=torch.uint8, device="cuda") for _ in "KV"]
+    scales = [torch.full((1, 1, N), 5.0, device="cuda") for _ in "KV"]
+    xb.xkv_cache8_append(s, K, V, None, None, N, "int8", 1, codes[0], codes[1], scales[0], scales[1])
+    for x, y, z in ((K, codes[0], scales[0]), (V, codes[1], scales[1])):
+        x, code = x.flatten().double(), y.flatten().view(torch.int8)
+        assert torch.equal(code, (127 * x.sign()).to(torch.int8))  # a row of one number is its own largest
+        assert bool(((z.flatten().double() * 127 - x.abs()).abs() <= x.abs() * 2.0**-24).all())  # one quotient in fp32

@@ -168,3 +168,17 @@ def test_infinities_and_nan_stay_in_their_pairs():
     want[0, 1, 0, [3, 19]] = True
     want[0, 2, 0, 40] = True  # not turned
     assert torch.equal(bad, want) and out[0, 1, 0, 3].isnan() and out[0, 2, 0, 40] == float("inf")
+
+
+def test_more_workgroups_than_a_launch_has_in_one_direction():
+    """2^27 tokens and more of one pair, eight a workgroup of 256 threads: 2^32 threads."""
+    N = (1 << 27) + 101
+    s = shape_of(1, 1, 2, 1, "bf16")
+    x = torch.randn((1, N, 1, 2), device="cuda").bfloat16()
+    f = ref.frequencies(2, 1e4)
+    out = torch.empty_like(x)
+    xb.xkv_rotate(s, 2, "half", "forward", 1.0, f.cuda(), None, N, x, out, None, None)
+    for start in (0, (1 << 25) - 50, (1 << 26) - 50, (1 << 27) - 50, N - 100):
+        p = torch.arange(start, start + 100)
+        want, bound = ref.rotate(x[:, start:start + 100].cpu(), p[None].to(torch.int32), f, "half", "forward", 1.0)
+        within(out[:, start:start + 100], want, bound, f"tokens from {start}")
