@@ -89,7 +89,7 @@ __device__ __forceinline__ Unit8 unit8(const Cache8Args &a)
     return u;
 }
 
-// A part that has no rows for this tile.
+// A part that has no rows for this tile: a sum that none has, by which the merge knows that there is no output.
 __device__ __forceinline__ void leave_nothing(const Cache8Args &a, const Unit8 &u)
 {
     const int n_rep = a.H_q / a.H_kv, M = a.N * n_rep;
@@ -98,7 +98,7 @@ __device__ __forceinline__ void leave_nothing(const Cache8Args &a, const Unit8 &
         if (m >= M) break;
         const size_t slot = ((size_t)u.part * a.N + m / n_rep) * a.H_q + u.g * n_rep + m % n_rep;
         a.part_ml[2 * slot] = -INFINITY;
-        a.part_ml[2 * slot + 1] = 0.0f;
+        a.part_ml[2 * slot + 1] = -1.0f;
     }
 }
 
@@ -1045,7 +1045,8 @@ __global__ __launch_bounds__(512, 2) void cache8_rows_kernel(Cache8Args a, bool 
 // ------------------------------------------------------------------------------------------
 // Merge.  A group of 2^lg lanes covers the columns of a row (query, head), VEC a lane.  Where there are many rows, a group per row; where there are few,
 // the groups of a workgroup share a row's partials and are added up in LDS: latency is all there is to it then, and the first partials are
-// requested before their weights are known.  Partials of parts that have no rows were not written and are not read.  64 parts of 32 rows 4.4 us, most of
+// requested before their weights are known.  Partials of parts that have no rows were not written and do not count; all others do, also with a
+// weight of zero: a NaN among a row's values is in its output alone, however little the part weighs.  64 parts of 32 rows 4.4 us, most of
 // it a launch's own time; a group per row there 9.
 // ------------------------------------------------------------------------------------------
 template <typename T, int VEC>
@@ -1088,9 +1089,10 @@ __global__ __launch_bounds__(256) void cache8_merge_kernel(Cache8Args a, int lg,
     for (int s = l; s < parts; s += width) m = fmaxf(m, ml[2 * s * stride]);
     for (int off = 1; off < width; off <<= 1) m = fmaxf(m, __shfl_xor(m, off, kWave));
     for (int s = l; s < parts; s += width) {
-        const float top = ml[2 * s * stride], wt = top == -INFINITY ? 0.0f : exp2f(top - m);
-        sm_w[grp][s] = wt;
-        den = fmaf(top == -INFINITY ? 1.0f : wt, ml[2 * s * stride + 1], den);  // (a part without a maximum: 0, or NaN)
+        const float top = ml[2 * s * stride], sum = ml[2 * s * stride + 1], wt = top == -INFINITY ? 0.0f : exp2f(top - m);
+        const bool left = sum < 0.0f;  // (nothing)
+        sm_w[grp][s] = left ? -1.0f : wt;
+        den = left ? den : fmaf(top == -INFINITY ? 1.0f : wt, sum, den);  // (a part without a maximum: 0, or NaN)
     }
     for (int off = 1; off < width; off <<= 1) den += __shfl_xor(den, off, kWave);
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");  // (a group is part of a wavefront)
@@ -1102,8 +1104,8 @@ __global__ __launch_bounds__(256) void cache8_merge_kernel(Cache8Args a, int lg,
 #pragma unroll
         for (int u = 0; u < BATCH; ++u) {
             const int s = s0 + u * step;
-            const float wt = s < parts ? sm_w[grp][s] : 0.0f;
-            acc += wt == 0.0f ? vec_t(0.0f) : wt * v[u];  // (a part without rows left nothing)
+            const float wt = s < parts ? sm_w[grp][s] : -1.0f;
+            acc += wt < 0.0f ? vec_t(0.0f) : wt * v[u];
         }
     }
     if (share) {
