@@ -76,6 +76,10 @@ class Shape:
         """c() by reference, made once: a call that is made for every token takes longer to set up than to run otherwise."""
         return ctypes.byref(self.c())
 
+    def __getstate__(self):
+        """Copies and pickles hold the fields; `ref` is an address in this process, and made again there."""
+        return {k: v for k, v in self.__dict__.items() if k != "ref"}
+
     @staticmethod
     def of(w, **kw) -> "Shape":
         """From a synth.Workload (or anything with the same field names)."""

@@ -138,3 +138,16 @@ def test_the_binding_wants_rows():
             xb.xkv_rotate(s, 128, name, "forward", 1.0, f, None, 2, None, None, x, x, stream=0)
     with pytest.raises(xb.XkvError):
         xb.xkv_rotate(shape(), 128, "half", "forward", 1.0, f, None, 0, None, None, x, x, stream=0)
+
+
+def test_a_shape_that_was_used_can_be_copied_and_pickled():
+    """It goes to worker processes, or into a checkpoint's configuration, before and after calls alike."""
+    import copy
+    import dataclasses
+    import pickle
+    s = shape(scale=0.25)
+    xb.xkv_cache8_workspace_bytes(s, 3)
+    for other in (pickle.loads(pickle.dumps(s)), copy.deepcopy(s), copy.copy(s), dataclasses.replace(s)):
+        assert other == s and hash(other) == hash(s) and other is not s
+        assert vars(other) == dataclasses.asdict(s)
+        assert xb.xkv_cache8_workspace_bytes(other, 3) == xb.xkv_cache8_workspace_bytes(s, 3)
