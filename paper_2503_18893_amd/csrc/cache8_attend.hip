@@ -1030,7 +1030,7 @@ __global__ __launch_bounds__(512, 2) void cache8_rows_kernel(Cache8Args a, bool 
                 u16x4_t x;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) x[e] = result<bf16_t>(sees[rt] == 0 ? 0.0f : O[rt][db][e] / den[rt]);
-                *reinterpret_cast<u16x4_t *>((bf16_t *)a.out + row * D + 16 * db + 4 * kk) = x;
+                __builtin_memcpy((bf16_t *)a.out + row * D + 16 * db + 4 * kk, &x, sizeof x);  // (wherever `out` lies)
             } else {
                 *reinterpret_cast<f32x4_t *>(a.part_o + row * D + 16 * db + 4 * kk) = O[rt][db];
             }

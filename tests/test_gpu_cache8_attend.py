@@ -421,3 +421,21 @@ def test_scales_of_all_sizes(dtype, d, N, code):
     check(s, code, c, seen, q, state, run(s, code, c, seen, q, state), "tiny scales")
     state[3].zero_()
     assert (run(s, code, c, seen, q, state) == 0).all()
+
+
+@pytest.mark.parametrize("dtype,d,N,L,batch", [("bf16", 128, 40, 400, 32), ("bf16", 128, 1, 400, 2), ("f32", 64, 2, 400, 1), ("bf16", 128, 40, 900, 2), ("bf16", 60, 3, 400, 2)])
+def test_results_that_are_not_aligned(dtype, d, N, L, batch):
+    """`out` an element behind a multiple of 16 bytes, with something before and behind it: tiles of 256 rows that leave results at once, other
+    kernels that do, and results of the merge."""
+    s, c = shape_of(2, 4, d, L, batch, dtype), 16
+    seen = [[L - N + 1 + i - b for i in range(N)] for b in range(batch)]
+    g, *state = cache(s, "e4m3", c, [max(x) for x in seen], 14)
+    q = torch.randn((batch, N, 8, d), generator=g).to(DT[dtype])
+    want = run(s, "e4m3", c, seen, q, state)
+    check(s, "e4m3", c, seen, q, state, want, "aligned")
+    room = torch.full((want.numel() + 16,), 7.0, dtype=DT[dtype], device="cuda")
+    out = room[1:1 + want.numel()].view(want.shape)
+    K8, V8, ks, vs = (x.cuda() for x in state)
+    xb.xkv_cache8_decode(s, K8, V8, ks, vs, "e4m3", c, torch.tensor(seen, dtype=torch.int32, device="cuda"), q.cuda(), N, out, workspace(s, N))
+    assert torch.equal(out.cpu(), want)
+    assert room[0] == 7.0 and (room[1 + want.numel():] == 7.0).all()
