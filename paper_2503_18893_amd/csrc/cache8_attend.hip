@@ -740,22 +740,19 @@ __global__ __launch_bounds__(512, 2) void cache8_rows_kernel(Cache8Args a, bool 
 
     // Q^T operands: lane (row n16, kk), product s, position e: channel 32 s + 8 kk + e
     bf16x8_t Q[RT][4];
-    int sees[RT], least = 0x7FFFFFFF, most = 0;
+    int sees[RT], most = 0;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         const int m = ((u.tile * WAVES + w) * RT + rt) * 16 + n16, m_in = m < M ? m : M - 1, i = m_in / n_rep;
         const bf16_t *q = (const bf16_t *)a.q + (((size_t)u.seq * a.N + i) * a.H_q + u.g * n_rep + m_in % n_rep) * D;
         sees[rt] = visible8(a, u.seq, i);
-        least = sees[rt] < least ? sees[rt] : least;
         most = sees[rt] > most ? sees[rt] : most;
 #pragma unroll
         for (int s = 0; s < 4; ++s) Q[rt][s] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t *>(q + 32 * s + 8 * kk));
     }
-    if (((u.tile * WAVES + w) * RT) * 16 >= M) least = most = 0;  // (no rows)
-    least = -wave_all(-least, MaxOp());  // rows of the cache that all of this wavefront's rows see, ..
-    least = __builtin_amdgcn_readfirstlane(least < u.t_end ? least : u.t_end);
-    most = __builtin_amdgcn_readfirstlane(wave_all(most, MaxOp()));  // .. any of them, ..
-    int all = 0x7FFFFFFF;                                            // .. all rows of the workgroup
+    if (((u.tile * WAVES + w) * RT) * 16 >= M) most = 0;             // (no rows)
+    most = __builtin_amdgcn_readfirstlane(wave_all(most, MaxOp()));  // rows of the cache that any of this wavefront's rows sees, ..
+    int all = 0x7FFFFFFF;                                            // .. and all rows of the workgroup
     {
         int first, last;
         tile_queries(a, u.tile, first, last);
