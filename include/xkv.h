@@ -452,7 +452,7 @@ XKV_API xkv_status xkv_evict(const xkv_shape *shape, const void *K, const void *
  *   are taken as they lie.  Strides are not negative; rows of an output must not overlap (in the order of their strides each reaches
  *   beyond all that is inside it).  In place: out = in with the same strides; otherwise outputs must not overlap inputs, nor one another.  positions
  *   [batch][N] int32 (device, nullable: 0 .. N - 1).  frequencies [d_rot / 2] double (device).  Angles are taken in double precision,
- *   the rest in fp32, rounded once.  shape->G, r_k, r_v, L, k, scale are ignored.
+ *   the rest in fp32, rounded once.  shape->G, r_k, r_v, L, k, scale are ignored (numbers that are valid in a shape: positive ones, k <= L, and scale >= 0).
  * xkv_rope_frequencies: such a table, once per model (frequencies: device, [d_rot / 2]).  f_j = theta^(-2j / d_rot), and for contexts that are
  *   longer than those a model was trained on, by `factor` (the other arguments are ignored where they are not named):
  *     XKV_ROPE_PLAIN   as it is               XKV_ROPE_LINEAR  f_j / factor
@@ -495,11 +495,13 @@ XKV_API xkv_status xkv_rotate(const xkv_shape *shape, int32_t d_rot, int32_t lay
  *   the nearer of 0 and L): a token after a cache, a drafted chain, or the tokens of a prompt, each with the rows up to its own.
  *     z_t = scale k_scale[t / c] <q, K8_t>,  out = sum_t softmax(z)_t v_scale[t / c] V8_t;  out [batch][N][H_q][d_h] in shape->dtype.
  *   Zeros for a query that sees nothing.  out must not overlap what is read.  Sums and statistics are fp32.  A weight times its scale enters the sums held to 2^-12 (fp32 shapes: 2^-22), or to
- *   2^-31 of the largest such product that a workgroup's rows can have where that is more; results are rounded once.  A NaN in a code or scale that a query
- *   sees gives NaN, one that it does not see does not reach it.  Scales are numbers from 2^-100 to 2^100, 0 or NaN: infinities, and products
- *   of a weight with a smaller scale, need not come out as the formula says.
+ *   2^-31 of the largest such product that a workgroup's rows can have, or to 2^-151, where one of these is more: a block whose scale is 2^20 times that of others costs those
+ *   some of their bits, whatever it weighs, in the queries that share its workgroup.  Results are rounded once.  A NaN in a code or scale that a query
+ *   sees gives NaN, one that it does not see does not reach it.  Scales are 0, NaN or numbers from 2^-126 to 2^123, as xkv_cache8_append writes them (others
+ *   need not come out as the formula says).  The sums are divided by that of the weights at their end, so the largest magnitude of a value that a query sees, times the rows
+ *   that it sees, is at most 2^119; beyond, results may be infinite or NaN.
  *   Results do not depend on the order in which workgroups run.  workspace: xkv_cache8_workspace_bytes(shape, N) bytes, 256-byte aligned.
- * shape->G, r_k, r_v, k are ignored.  XKV_ERR_INVALID_ARG for N < 1, c < 1, a code that is none of the two, strides as in xkv_rotate (negative);
+ * shape->G, r_k, r_v, k are ignored (positive numbers, k <= L), and by xkv_cache8_append scale (>= 0).  XKV_ERR_INVALID_ARG for N < 1, c < 1, a code that is none of the two, strides as in xkv_rotate (negative);
  * XKV_ERR_UNSUPPORTED for c that is not a power of two, L > 2^30, batch * N * H_q > 2^26, or more than 2^31 - 1 workgroups of blocks that an append can touch.
  */
 typedef enum { XKV_E4M3 = 0, XKV_INT8 = 1 } xkv_code;

@@ -246,7 +246,8 @@ __global__ __launch_bounds__(256) void cache8_general_kernel(Cache8Args a, bool 
 // conversion; of V it reads the tokens that it has weights of, D / 16 channels of each (a row of the cache is read by 16 lanes), and pairs
 // up neighbouring tokens by permuting bytes.
 // The maximum is only raised when a logit outgrows it by 2^8.  Weights times scales enter as fp16, 2^-12: `inv`, a power of two, brings the largest scale met
-// so far to between 2^6 and 2^7, so that they are at most 2^15, and down to 2^-20 of that scale keep their 11 bits (what is smaller is held to 2^-32 of it).
+// so far to between 2^6 and 2^7, so that they are at most 2^15, and down to 2^-20 of that scale keep their 11 bits (what is smaller is held to 2^-31 of it;
+// scales below 2^-119 stay as `inv` begins, 2^126, and their weights are held to 2^-151).
 // Beside the output's own rounding that is not seen: the error against 64 bits is 0.0017 of the results' root mean square, with bf16 pairs in its place as well.
 // fp32: a query is three terms of bf16, a weight two of fp16, and scales are multiplied in after the exponential.
 // It is a stream: one query after 32768 rows of 8 KV heads, 67 MB, 15 us with its start and end (6.4 TB/s with 16 sequences of 65536); 16 heads 15, 20 rows 20,

@@ -439,3 +439,60 @@ def test_results_that_are_not_aligned(dtype, d, N, L, batch):
     xb.xkv_cache8_decode(s, K8, V8, ks, vs, "e4m3", c, torch.tensor(seen, dtype=torch.int32, device="cuda"), q.cuda(), N, out, workspace(s, N))
     assert torch.equal(out.cpu(), want)
     assert room[0] == 7.0 and (room[1 + want.numel():] == 7.0).all()
+
+
+
+def appended(s, code, c, K, V):
+    """K8, V8, k_scales, v_scales on the CPU as two appends leave them: rows up to the middle of a block, then the others."""
+    n_c, L = -(-s.L // c), s.L
+    kind = {"e4m3": torch.float8_e4m3fn, "int8": torch.int8}[code]
+    state = [torch.zeros((s.batch, s.H_kv, L, s.d_h), dtype=torch.uint8, device="cuda").view(kind) for _ in "KV"]
+    state += [torch.zeros((s.batch, s.H_kv, n_c), device="cuda") for _ in "KV"]
+    n = L // 2 // c * c + c // 2
+    for at, m in ((0, n), (n, L - n)):
+        lengths = torch.full((s.batch,), at, dtype=torch.int32, device="cuda")
+        xb.xkv_cache8_append(s, K[:, at:at + m].cuda(), V[:, at:at + m].cuda(), lengths, None, m, code, c, *state)
+    return [x.cpu() for x in state]
+
+
+# magnitude of values, of some blocks' values (others: the first), of keys (queries: what brings logits back to the ordinary)
+SIZES = {"tiny": (1e-38, 1e-38, 1.0), "small": (3e-37, 1e-38, 1.0), "large": (2.0 ** 104, 2.0 ** 104, 1.0), "large_and_tiny": (2.0 ** 104, 1e-38, 1.0), "large_and_one": (2.0 ** 104, 1.0, 1.0),
+         "large_keys": (1.0, 1.0, 2.0 ** 100), "tiny_keys": (1.0, 1.0, 2.0 ** -100), "peaked": (1e-37, 1e-37, 12.0)}
+
+
+@pytest.mark.parametrize("code", ["e4m3", "int8"])
+@pytest.mark.parametrize("dtype,d,N,c", [("bf16", 128, 1, 16), ("bf16", 128, 5, 16), ("bf16", 128, 40, 32), ("bf16", 64, 3, 2), ("f32", 64, 3, 16), ("f32", 128, 2, 1), ("bf16", 72, 2, 8),
+                                         ("f32", 72, 2, 8)])
+@pytest.mark.parametrize("size", list(SIZES))
+def test_whatever_append_writes_is_read(size, dtype, d, N, c, code):
+    """Caches as xkv_cache8_append writes them, from the smallest scale, 2^-126, to sums next to the largest numbers.
+
+    Beside what check() allows: where the largest scale is below 2^-119, `inv` stays 2^126, and half a step of a weight times its scale, 2^-25 there, is
+    2^-151; sums of numbers below 2^-126 are rounded to steps of 2^-149, at most once a row of the cache and a few times a part; a result in
+    bf16 below 2^-126 to steps of 2^-133.  All of it relative to a sum of weights of at least 1."""
+    L, batch = 2200, 2
+    values, others, keys = SIZES[size]
+    s = shape_of(2, 4, d, L, batch, dtype)
+    g = torch.Generator().manual_seed(len(size) + N)
+    K, V = (torch.randn((batch, L, 2, d), generator=g) for _ in "KV")
+    K, V = (K * keys).to(DT[dtype]), V.clamp(-4, 4)
+    some = (torch.arange(L) // 96 % 3 == 1)[None, :, None, None]
+    V = torch.where(some, V * others, V * values).to(DT[dtype])
+    q = (torch.randn((batch, N, 8, d), generator=g) / (keys if not 1.0 <= keys <= 16.0 else 1.0)).to(DT[dtype])
+    state = appended(s, code, c, K, V)
+    if size in ("tiny", "small"):
+        assert state[3].min() == 2.0 ** -126
+    assert 2200 * (ref8.rows(state[1], state[3], c).abs().max().item()) <= 2.0 ** 119
+    seen = [[L - N + 1 + i - 300 * b for i in range(N)] for b in range(batch)]
+    out = run(s, code, c, seen, q, state)
+    for b in range(batch):
+        n = max(seen[b])
+        sees = (torch.arange(n)[None] < torch.tensor(seen[b])[:, None]).repeat_interleave(4, 0)
+        for h in range(2):
+            # (the reference's bound has a floor of 1e-30: values 2^80 times larger, all of it exact in double precision)
+            want, _, bound, _ = ref.attend(q[b, :, 4 * h:4 * h + 4].reshape(-1, d), ref8.rows(state[0], state[2], c)[b, h, :n],
+                                           ref8.rows(state[1], state[3], c)[b, h, :n] * 2.0 ** 80, sees, d ** -0.5)
+            codes = state[1][b, h, :n].float().abs().double().sum(0)
+            bound = bound * 2.0 ** -80 + max(2.0 ** -31 * state[3][b, h, : -(-n // c)].max().item(), 2.0 ** -151) * codes + (n + 64) * 2.0 ** -150
+            bound = bound + (2.0 ** -134 if dtype == "bf16" else 0.0)
+            within(out[b, :, 4 * h:4 * h + 4].reshape(-1, d), want * 2.0 ** -80, bound, f"{size} {b} {h}")
