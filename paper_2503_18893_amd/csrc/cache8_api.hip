@@ -63,7 +63,10 @@ xkv_status plan_cache8(const xkv_shape &s, int N, Cache8Plan &p)
     p.mfma = s.d_h == 64 || s.d_h == 128 || s.d_h == 256;
     // Rows of a workgroup.  Two workgroups of the matrix-core kernels to a compute unit, one of 256 rows or channels; four of the general one.
     // (More than 128 rows of 128 channels: 256 that share tiles.  Microseconds by 32 / by 256, 8 KV heads: 64 rows after 32768 rows of the cache 29 / 47, 96
-    // 41 / 50, 128 42 / 52, 192 73 / 61; four sequences of up to 65536 rows, 72 rows 132 / 197, 128 171 / 201, 192 243 / 208.)
+    // 41 / 50, 128 42 / 52, 192 73 / 61; four sequences of up to 65536 rows, 72 rows 132 / 197, 128 171 / 201, 192 243 / 208.  By 16 / by 32, one sequence of 32768 rows, int8:
+    // 128 channels, 4 rows 20 / 23, 20 rows 25 / 26, 64 rows 39 / 32, 128 65 / 49; 64 channels 17 / 19, 21 / 21, 30 / 25, 48 / 37; 256 channels, where 32 rows leave
+    // no registers for the stream, 32 / 84, 44 / 88, 72 / 146, 129 / 228.  fp32: a query's three terms take the registers of 32 rows; 4, 20, 64 and 256 rows
+    // of 128 channels 22, 29, 45 and 135.)
     p.rows = !p.mfma || M <= 16 || s.d_h == 256 || s.dtype == XKV_F32 ? 16 : M <= 128 || s.d_h != 128 ? 32 : 256;
     p.round = p.mfma ? 128 : 64;
     const int slots = !p.mfma ? 1024 : p.rows == 256 || s.d_h == 256 ? 256 : 512;
@@ -74,7 +77,8 @@ xkv_status plan_cache8(const xkv_shape &s, int N, Cache8Plan &p)
     const bool one = s.L <= 512 && (M <= 64 || units * batch >= 64);
     // Otherwise, where sequences alone do not fill the compute units, parts are cut by the lengths, for which every workgroup looks at those of all
     // queries (unless they are very many).  Four sequences of up to 65536 rows, 1024 rows of queries, 128 tiles of them 777 us, tiles cut in
-    // equal parts 1094; 16 of up to 4096, 512 tiles 243, not cut 175.
+    // equal parts 1094; 16 of up to 4096, 512 tiles 243, not cut 175.  (Where sequences take most of the slots, or all of them, parts are coarse beside their differences:
+    // lengths from 16384 / b to 16384, 8 KV heads, b = 32 4.8 TB/s, 48 4.1, 64 4.8, 80 and more 6.2 to 6.4; 16 4.7, most of which is the start and end of 60 us.)
     p.by_length = !one && units * batch < slots && batch <= kCutBatch && (N == 1 || batch * N <= kCutQueries);
     if (one) {
         p.parts = 1;

@@ -63,8 +63,10 @@ template <int LANES, typename T, typename OP> __device__ __forceinline__ T lanes
 // ------------------------------------------------------------------------------------------
 // THREADS threads (part of a wavefront, one, or four) take a block of a KV head of K or V: first the largest magnitude of its new rows, then their codes.
 // A thread's pieces, up to KEPT of them, stay in registers between the two; a larger block's are read again.  Codes of older rows are
-// only touched where the scale grows.  Long appends are bound by their bytes: 32768 tokens of 8 KV heads, bf16 to e4m3, blocks of 32 rows, 40 us, 5.0 TB/s
-// (48 with divisions in the place of `quotient`); one token of 16 sequences 3.5 us, a chain of two loads, the maximum and the quotients.
+// only touched where the scale grows.  Long appends are bound by their bytes: 32768 tokens of 8 KV heads, bf16 to e4m3, blocks of 32 rows, 41 us, 4.9 TB/s
+// (48 with divisions in the place of `quotient`); one token of 16 sequences 4.4 us, a chain of two loads, the maximum and the quotients.  Blocks of one or two rows
+// 74: a lane has one piece under way, and a scale is 4 bytes of a store of its own.  A block is one workgroup's, so that few large ones do not fill the card: of 256 rows 54, 1024 70,
+// 4096 220, one for a head 1710.
 // ------------------------------------------------------------------------------------------
 template <typename T, int CODE, int VEC, int THREADS, int KEPT>
 __global__ __launch_bounds__(256) void cache8_append_kernel(Cache8Append a, unsigned units)

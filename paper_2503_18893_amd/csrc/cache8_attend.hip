@@ -691,7 +691,7 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void cache8_mfma_kernel(Cache
 // the transposing LDS read.  The logits of a tile are multiplied beside the exponentials of the one before, so that the matrix cores and the
 // vector units work at once; the tile after it is converted beside that one's second product.  Nothing in the loop waits for a load of
 // its own: scales take the way of the codes (a load into a register would first have to wait for all tiles that are under way).
-// 256 queries of 7 heads after 131072 rows (1792 rows a KV head): 506 us, 0.95 PFLOP/s of 4 d flops a logit (a 8192^3 library product 1.2); logits and
+// 256 queries of 7 heads after 131072 rows (1792 rows a KV head): 508 us with the merge, 492 without, 0.95 PFLOP/s of 4 d flops a logit (a 8192^3 library product 1.2); logits and
 // exponentials one after the other 631; codes and scales through registers 525; by 32 rows that share nothing 783.  With few rows a
 // tile still takes 2.4 us, the latency of its steps: the streams are faster up to 128 rows.
 // LDS: 16-byte piece p of row t of K sits at p ^ (t % 16), 32-byte piece u of V at u ^ (t % 8), so that neither the fragment reads (16
